@@ -58,8 +58,10 @@ typedef struct CUstream_st* ws_stream_t;
 typedef struct ws_csr_s* ws_csr_t;
 
 typedef enum {
-  WS_F32 = 1, /* float  */
-  WS_F64 = 2  /* double */
+  WS_F32 = 1,  /* float  */
+  WS_F64 = 2,  /* double */
+  WS_BF16 = 3, /* bfloat16: dense rows and matrices of the routing operations only */
+  WS_F16 = 4   /* half:     the same */
 } ws_dtype_t;
 
 typedef enum {
@@ -356,6 +358,79 @@ ws_status_t ws_set_tuning(int key, int64_t value);
  * negative nrows, WS_ERR_CUDA if a CUDA call fails.
  */
 ws_status_t ws_rowptr_scan_static(int64_t* rowptr, int64_t nrows, ws_stream_t stream);
+
+/*
+ * Routing matrices.  An nrows x ncols CSR matrix R with a row per token and a
+ * column per expert (or adapter), float values, few entries a row.  (The paper
+ * has no counterpart: these calls serve layers that send rows of dense
+ * matrices along a sparse matrix.)  The calls below take device pointers, queue
+ * their work on `stream` and return without waiting; they allocate nothing
+ * and can be captured in a graph.  Argument errors are found on the host
+ * before anything is queued.  Dense matrices are row-major with unit stride
+ * within a row and `ld` values from row to row.  ncols <= 1024, nrows, nnz and
+ * the number of dense rows <= INT32_MAX, rows of at most 2^24 values.
+ * Entries whose column is not in [0, ncols) take no part: they have slot -1 and
+ * gradient 0, and the slots they leave over come last and hold zero rows.
+ * rowptr is read within [0, nnz] whatever it holds.
+ *
+ * ws_topk_route -- R from logits (rows x cols, float, bfloat16 or half): row i
+ * holds the k largest logits of row i (ties to the lowest column), by
+ * ascending column, with the weights exp(l - max) / sum of exp(l - max), the sum over the k chosen
+ * (normalize != 0) or over all columns (0), in 32 bits.  A logit of -inf has
+ * weight 0 and is chosen last; a row of nothing else has weights 0.  NaN counts
+ * as the largest value and makes the row's weights NaN.  Writes rowptr
+ * (int64[rows + 1] = 0, k, 2 k, ...), colidx and vals ([rows * k]).
+ * 1 <= k <= min(cols, 32), cols <= 1024.
+ *
+ * ws_topk_route_backward -- gradient of the logits (rows x cols, their type,
+ * row stride ldg) from the gradient gvals of vals; colidx and vals as
+ * ws_topk_route wrote them.  The choice of columns counts as fixed.  logits
+ * are read only where normalize is 0 (may be NULL otherwise).
+ */
+ws_status_t ws_topk_route(const void* logits, int64_t rows, int64_t cols, int64_t ld, ws_dtype_t dtype, int k,
+                          int normalize, int64_t* rowptr, int32_t* colidx, float* vals, ws_stream_t stream);
+ws_status_t ws_topk_route_backward(const void* logits, int64_t rows, int64_t cols, int64_t ld, ws_dtype_t dtype,
+                                   int k, int normalize, const int32_t* colidx, const float* vals,
+                                   const float* gvals, void* glogits, int64_t ldg, ws_stream_t stream);
+
+/* A routing matrix and its transpose: all arrays are the caller's. */
+typedef struct ws_routing {
+  int64_t nrows, ncols, nnz;
+  const int64_t* rowptr; /* [nrows + 1] */
+  const int32_t* colidx; /* [nnz], strictly increasing within a row */
+  const float* vals;     /* [nnz]; read by combine and its gradient only */
+  int64_t* offsets;      /* [ncols + 1]: first slot of every column (the row pointer of R^T) */
+  int32_t* rows;         /* [nnz]: row of every slot (the columns of R^T, ascending within a column) */
+  int32_t* entries;      /* [nnz]: entry of R in every slot */
+  int32_t* slots;        /* [nnz]: slot of every entry of R */
+} ws_routing;
+
+/*
+ * ws_routing_build -- fills offsets, rows, entries and slots: the entries of R
+ * sorted by column, rows in order within a column.  `scratch` holds
+ * ws_routing_scratch(nrows, ncols) bytes (0 for few rows: NULL then).
+ */
+int64_t ws_routing_scratch(int64_t nrows, int64_t ncols);
+ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch_bytes, ws_stream_t stream);
+
+/*
+ * Dense rows along R, each row `width` values of `dtype` (float, bfloat16, half):
+ *   dispatch           xs[slot] = x[row]                     x: nrows rows, xs: nnz rows in slot order
+ *   dispatch_backward  gx[i] = sum over row i of gxs[slot]
+ *   combine            y[i] = sum over row i of value * ys[slot]
+ *   combine_backward   gys[slot] = value * gy[row],  gvals[entry] = <gy[row], ys[slot]>
+ * Sums are held in 32 bits, in the order of the entries, and rounded once; rows
+ * of R without entries give zero rows.  Outputs may not overlap inputs.
+ */
+ws_status_t ws_routing_dispatch(const ws_routing* r, const void* x, int64_t ldx, void* xs, int64_t ldxs,
+                                int64_t width, ws_dtype_t dtype, ws_stream_t stream);
+ws_status_t ws_routing_dispatch_backward(const ws_routing* r, const void* gxs, int64_t ldgxs, void* gx, int64_t ldgx,
+                                         int64_t width, ws_dtype_t dtype, ws_stream_t stream);
+ws_status_t ws_routing_combine(const ws_routing* r, const void* ys, int64_t ldys, void* y, int64_t ldy,
+                               int64_t width, ws_dtype_t dtype, ws_stream_t stream);
+ws_status_t ws_routing_combine_backward(const ws_routing* r, const void* gy, int64_t ldgy, const void* ys,
+                                        int64_t ldys, void* gys, int64_t ldgys, float* gvals, int64_t width,
+                                        ws_dtype_t dtype, ws_stream_t stream);
 
 #ifdef __cplusplus
 }

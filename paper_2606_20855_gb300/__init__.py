@@ -1,6 +1,7 @@
 """GB300 (sm_103a) SpGEMM: C = A*B for CSR matrices, computed by hand-written CUDA kernels;
 also the elementwise operations C = A + B and C = A .* B and the sparse
-matrix - sparse vector product y = A x.
+matrix - sparse vector product y = A x, and the operations of layers that send
+rows of dense matrices along a sparse routing matrix (``routing``).
 
 The C ABI lives in include/ws_spgemm.h and libws_spgemm.so (built by
 ``paper_2606_20855_gb300.build``).  ``_abi`` is the ctypes binding with the
@@ -9,9 +10,14 @@ this package loads nothing; the library is loaded on first use.
 """
 
 __all__ = ["DeviceCSR", "SpGEMM", "SpGEMMOuter", "spgemm", "spgemm_outer", "submatrix", "Ewise", "ewise", "SpMSpV", "spmspv"]
+_ROUTING = ["Routing", "topk_route", "topk_route_backward"]
+__all__ += _ROUTING
 
 
 def __getattr__(name):
+    if name in _ROUTING:
+        from . import routing as _r
+        return getattr(_r, name)
     if name in __all__:
         from . import spgemm as _m
         return getattr(_m, name)

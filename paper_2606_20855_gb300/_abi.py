@@ -15,6 +15,8 @@ LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libws_spgem
 
 WS_F32 = 1
 WS_F64 = 2
+WS_BF16 = 3
+WS_F16 = 4
 
 STATUS_NAMES = {
     0: "WS_OK",
@@ -50,7 +52,21 @@ SIGNATURES = [
     ("ws_csr_submatrix_numeric", _i32, [_p, _p, _p, _p, _p]),
     ("ws_spgemm_outer_symbolic", _i32, [_p, _p, _p, _i32, ctypes.POINTER(_i64), _p]),
     ("ws_spgemm_outer_numeric", _i32, [_p, _p, _p, _p, _p, _p]),
+    ("ws_topk_route", _i32, [_p, _i64, _i64, _i64, _i32, _i32, _i32, _p, _p, _p, _p]),
+    ("ws_topk_route_backward", _i32, [_p, _i64, _i64, _i64, _i32, _i32, _i32, _p, _p, _p, _p, _i64, _p]),
+    ("ws_routing_scratch", _i64, [_i64, _i64]),
+    ("ws_routing_build", _i32, [_p, _p, _i64, _p]),
+    ("ws_routing_dispatch", _i32, [_p, _p, _i64, _p, _i64, _i64, _i32, _p]),
+    ("ws_routing_dispatch_backward", _i32, [_p, _p, _i64, _p, _i64, _i64, _i32, _p]),
+    ("ws_routing_combine", _i32, [_p, _p, _i64, _p, _i64, _i64, _i32, _p]),
+    ("ws_routing_combine_backward", _i32, [_p, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i32, _p]),
 ]
+
+
+class WsRouting(ctypes.Structure):
+    """struct ws_routing (device pointers as integers)."""
+    _fields_ = [("nrows", _i64), ("ncols", _i64), ("nnz", _i64), ("rowptr", _p), ("colidx", _p), ("vals", _p),
+                ("offsets", _p), ("rows", _p), ("entries", _p), ("slots", _p)]
 
 EWISE_OPS = {"add": 1, "mul": 2}  # ws_ewise_op_t
 
@@ -205,3 +221,43 @@ def ws_rowptr_scan_static(rowptr: int, nrows: int, stream: int) -> None:
     status = load().ws_rowptr_scan_static(rowptr or None, nrows, stream or None)
     if status != 0:
         raise WsError("ws_rowptr_scan_static", status, STATUS_NAMES.get(status, str(status)))
+
+
+def ws_topk_route(logits: int, rows: int, cols: int, ld: int, dtype: int, k: int, normalize: bool, rowptr: int,
+                  colidx: int, vals: int, stream: int) -> None:
+    _check("ws_topk_route", load().ws_topk_route(logits, rows, cols, ld, dtype, k, normalize, rowptr, colidx, vals,
+                                                 stream))
+
+
+def ws_topk_route_backward(logits: int, rows: int, cols: int, ld: int, dtype: int, k: int, normalize: bool,
+                           colidx: int, vals: int, gvals: int, glogits: int, ldg: int, stream: int) -> None:
+    _check("ws_topk_route_backward", load().ws_topk_route_backward(logits, rows, cols, ld, dtype, k, normalize, colidx,
+                                                                   vals, gvals, glogits, ldg, stream))
+
+
+def ws_routing_scratch(nrows: int, ncols: int) -> int:
+    return load().ws_routing_scratch(nrows, ncols)
+
+
+def ws_routing_build(r, scratch: int, scratch_bytes: int, stream: int) -> None:
+    _check("ws_routing_build", load().ws_routing_build(r, scratch, scratch_bytes, stream))
+
+
+def ws_routing_dispatch(r, x: int, ldx: int, xs: int, ldxs: int, width: int, dtype: int, stream: int) -> None:
+    _check("ws_routing_dispatch", load().ws_routing_dispatch(r, x, ldx, xs, ldxs, width, dtype, stream))
+
+
+def ws_routing_dispatch_backward(r, gxs: int, ldgxs: int, gx: int, ldgx: int, width: int, dtype: int,
+                                 stream: int) -> None:
+    _check("ws_routing_dispatch_backward", load().ws_routing_dispatch_backward(r, gxs, ldgxs, gx, ldgx, width, dtype,
+                                                                               stream))
+
+
+def ws_routing_combine(r, ys: int, ldys: int, y: int, ldy: int, width: int, dtype: int, stream: int) -> None:
+    _check("ws_routing_combine", load().ws_routing_combine(r, ys, ldys, y, ldy, width, dtype, stream))
+
+
+def ws_routing_combine_backward(r, gy: int, ldgy: int, ys: int, ldys: int, gys: int, ldgys: int, gvals: int,
+                                width: int, dtype: int, stream: int) -> None:
+    _check("ws_routing_combine_backward", load().ws_routing_combine_backward(r, gy, ldgy, ys, ldys, gys, ldgys, gvals,
+                                                                             width, dtype, stream))

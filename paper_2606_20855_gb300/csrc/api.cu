@@ -27,6 +27,7 @@
 #include <utility>
 #include <vector>
 
+#include "routing.cuh"
 #include "ws_internal.cuh"
 #include "ws_spgemm.h"
 
@@ -1406,6 +1407,22 @@ ws_status_t outer_numeric_impl(ws_csr_s* C, cudaStream_t s) {
 }
 
 }  // namespace
+
+// The error text of the calls on routing matrices (routing_api.cu).
+namespace wsk {
+ws_status_t routing_fail(ws_status_t st, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof(buf), fmt, ap);
+  va_end(ap);
+  try {
+    g_last_error = buf;
+  } catch (...) {  // no memory for the text; the status stands
+  }
+  return st;
+}
+}  // namespace wsk
 
 extern "C" {
 

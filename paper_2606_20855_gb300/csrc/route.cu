@@ -1,0 +1,217 @@
+// Rows of a routing matrix chosen from logits, and the gradient of that choice.
+//
+// Row i of R holds the k largest of row i's E logits l (ties to the lowest
+// column) with the weights
+//   normalize       v_j = exp(l_j - m) / sum over the chosen of exp(l - m)
+//   else            v_j = exp(l_j - m) / sum over all columns of exp(l - m),   m = the row's largest logit.
+// A logit of -inf has weight 0 and is chosen last; a row of nothing else has
+// weights 0, not 0 / 0.  NaN counts as the largest value and makes the row's
+// weights NaN.  With g the gradient of v and a = sum over the chosen of v g,
+//   normalize       dl_j = v_j (g_j - a) at the chosen columns, 0 elsewhere
+//   else            dl_j = p_j (g_j [j chosen] - a) at every column, p the softmax over all.
+// Exponentials and sums are held in 32 bits whatever the logits' type; the
+// gradient of a 16-bit logit is rounded once, when it is stored.
+#include <cmath>
+
+#include "routing.cuh"
+
+namespace wsk {
+namespace {
+
+constexpr int kRouteWarps = 8;
+
+// Order of floats as unsigned numbers: NaN last of all, -0 as +0; 0 is below -inf and marks "no logit".
+__device__ __forceinline__ uint32_t order_key(float f) {
+  const uint32_t u = __float_as_uint(f + 0.0f);
+  return f != f ? 0xffffffffu : u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+
+// V consecutive logits of a row from column `at` on; -inf and key 0 past the row's end.
+template <typename T, int V>
+__device__ __forceinline__ void load_row(const T* row, int at, int cols, bool vec, float (&f)[V]) {
+  constexpr int N = V * sizeof(T) >= 16 ? 16 / sizeof(T) : V;
+  if (vec && at + V <= cols) {
+#pragma unroll
+    for (int i = 0; i < V; i += N) {
+      float part[N];
+      unpack<T, N>(*reinterpret_cast<const Pack<T, N>*>(row + at + i), part);
+#pragma unroll
+      for (int j = 0; j < N; ++j) f[i + j] = part[j];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) f[i] = at + i < cols ? to_f32<T>(row[at + i]) : -INFINITY;
+  }
+}
+
+// A warp per row; a lane holds V consecutive logits, so that among equal
+// logits the lowest lane holds the lowest column and a ballot settles ties.
+template <typename T, int V>
+__global__ void __launch_bounds__(32 * kRouteWarps)
+    topk_route_kernel(const T* __restrict__ logits, int64_t rows, int cols, int64_t ld, bool vec, int k,
+                      bool normalize, int64_t* __restrict__ rowptr, int32_t* __restrict__ colidx,
+                      float* __restrict__ vals) {
+  const int lane = threadIdx.x & 31;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  float f[V];
+  load_row<T, V>(logits + row * ld, lane * V, cols, vec, f);
+  uint32_t key[V];
+  uint32_t best = 0;
+  int where = 0;
+#pragma unroll
+  for (int i = V - 1; i >= 0; --i) {
+    key[i] = lane * V + i < cols ? order_key(f[i]) : 0u;
+    if (key[i] >= best) best = key[i], where = i;
+  }
+  uint32_t my_key = 0;
+  int my_col = 0x7fffffff;
+  for (int r = 0; r < k; ++r) {
+    const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+    const int owner = __ffs(__ballot_sync(0xffffffffu, best == top)) - 1;
+    const int col = __shfl_sync(0xffffffffu, lane * V + where, owner);
+    if (lane == r) my_key = top, my_col = col;
+    if (lane == owner) {  // the logit leaves; the lane's next best
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        if (i == where) key[i] = 0;
+      best = 0;
+#pragma unroll
+      for (int i = V - 1; i >= 0; --i)
+        if (key[i] >= best) best = key[i], where = i;
+    }
+  }
+  const float mine = my_key == 0xffffffffu ? NAN : __uint_as_float(my_key & 0x80000000u ? my_key & 0x7fffffffu : ~my_key);
+  float m = __shfl_sync(0xffffffffu, mine, 0);
+  if (m == -INFINITY) m = 0.0f;
+  const float e = lane < k ? expf(mine - m) : 0.0f;
+  float total = e;
+  if (!normalize) {
+    total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) total += expf(f[i] - m);  // 0 past the row's end
+  }
+  total = warp_sum(total);
+  int rank = 0;  // places by column
+  for (int r = 0; r < k; ++r) rank += __shfl_sync(0xffffffffu, my_col, r) < my_col;
+  const int64_t at = row * k;
+  if (lane < k) {
+    colidx[at + rank] = my_col;
+    vals[at + rank] = total == 0.0f ? 0.0f : e / total;
+  }
+  if (lane == 0) {
+    rowptr[row] = at;
+    if (row == rows - 1) rowptr[rows] = at + k;
+  }
+}
+
+template <typename T, int V>
+__global__ void __launch_bounds__(32 * kRouteWarps)
+    topk_route_backward_kernel(const T* __restrict__ logits, int64_t rows, int cols, int64_t ld, bool vec, int k,
+                               bool normalize, const int32_t* __restrict__ colidx, const float* __restrict__ vals,
+                               const float* __restrict__ gvals, T* __restrict__ glogits, int64_t ldg, bool vecg) {
+  constexpr int N = V * sizeof(T) >= 16 ? 16 / sizeof(T) : V;
+  const int lane = threadIdx.x & 31;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
+  if (row >= rows) return;
+  float v = 0.0f, g = 0.0f;
+  int col = -1;
+  if (lane < k) {
+    col = colidx[row * k + lane];
+    v = vals[row * k + lane];
+    g = gvals[row * k + lane];
+  }
+  const float a = warp_sum(v * g);
+  float out[V];
+  if (normalize) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] = 0.0f;
+  } else {
+    load_row<T, V>(logits + row * ld, lane * V, cols, vec, out);
+    uint32_t best = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) best = max(best, order_key(out[i]));
+    const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+    float m = top == 0xffffffffu ? NAN : __uint_as_float(top & 0x80000000u ? top & 0x7fffffffu : ~top);
+    if (m == -INFINITY) m = 0.0f;
+    float total = 0.0f;
+#pragma unroll
+    for (int i = 0; i < V; ++i) total += out[i] = expf(out[i] - m);
+    total = warp_sum(total);
+    const float scale = total == 0.0f ? 0.0f : -a / total;
+#pragma unroll
+    for (int i = 0; i < V; ++i) out[i] *= scale;
+  }
+  T* dst = glogits + row * ldg;
+  if (vecg && lane * V + V <= cols) {
+#pragma unroll
+    for (int i = 0; i < V; i += N) {
+      float part[N];
+#pragma unroll
+      for (int j = 0; j < N; ++j) part[j] = out[i + j];
+      *reinterpret_cast<Pack<T, N>*>(dst + lane * V + i) = pack<T, N>(part);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (lane * V + i < cols) dst[lane * V + i] = from_f32<T>(out[i]);
+  }
+  __syncwarp();  // the chosen columns over what the row's lanes stored
+  if (static_cast<unsigned>(col) < static_cast<unsigned>(cols)) dst[col] = from_f32<T>(v * (g - a));
+}
+
+template <typename F>
+void for_values(int cols, F f) {
+  if (cols <= 32) f(std::integral_constant<int, 1>());
+  else if (cols <= 64) f(std::integral_constant<int, 2>());
+  else if (cols <= 128) f(std::integral_constant<int, 4>());
+  else if (cols <= 256) f(std::integral_constant<int, 8>());
+  else if (cols <= 512) f(std::integral_constant<int, 16>());
+  else f(std::integral_constant<int, 32>());
+}
+
+template <typename F>
+void for_type(ws_dtype_t dt, F f) {
+  if (dt == WS_F32) f(float());
+  else if (dt == WS_BF16) f(__nv_bfloat16());
+  else f(__half());
+}
+
+// Whether V values from every V-th column of every row may be moved as packs.
+bool packs(const void* p, int64_t ld, int V, int size) {
+  const int64_t bytes = V * size < 16 ? V * size : 16;
+  return reinterpret_cast<uintptr_t>(p) % bytes == 0 && ld * size % bytes == 0;
+}
+
+}  // namespace
+
+void launch_topk_route(const void* logits, int64_t rows, int cols, int64_t ld, ws_dtype_t dt, int k, bool normalize,
+                       int64_t* rowptr, int32_t* colidx, float* vals, cudaStream_t s) {
+  const unsigned grid = static_cast<unsigned>((rows + kRouteWarps - 1) / kRouteWarps);
+  for_type(dt, [&](auto t) {
+    using T = decltype(t);
+    for_values(cols, [&](auto v) {
+      constexpr int V = decltype(v)::value;
+      topk_route_kernel<T, V><<<grid, 32 * kRouteWarps, 0, s>>>(static_cast<const T*>(logits), rows, cols, ld,
+                                                                packs(logits, ld, V, sizeof(T)), k, normalize, rowptr,
+                                                                colidx, vals);
+    });
+  });
+}
+
+void launch_topk_route_backward(const void* logits, int64_t rows, int cols, int64_t ld, ws_dtype_t dt, int k,
+                                bool normalize, const int32_t* colidx, const float* vals, const float* gvals,
+                                void* glogits, int64_t ldg, cudaStream_t s) {
+  const unsigned grid = static_cast<unsigned>((rows + kRouteWarps - 1) / kRouteWarps);
+  for_type(dt, [&](auto t) {
+    using T = decltype(t);
+    for_values(cols, [&](auto v) {
+      constexpr int V = decltype(v)::value;
+      topk_route_backward_kernel<T, V><<<grid, 32 * kRouteWarps, 0, s>>>(
+          static_cast<const T*>(logits), rows, cols, ld, packs(logits, ld, V, sizeof(T)), k, normalize, colidx, vals,
+          gvals, static_cast<T*>(glogits), ldg, packs(glogits, ldg, V, sizeof(T)));
+    });
+  });
+}
+
+}  // namespace wsk

@@ -1,0 +1,463 @@
+// A routing matrix R transposed, and rows of dense matrices moved along it.
+//
+// R has a row per token and a column per expert.  Sorted by column (rows in
+// order within a column) its entries are the rows of R^T: entry (i, e) has
+//   slot = offsets[e] + entries of column e in the rows before i.
+// A row stores a column at most once, so within a tile of 32 W rows an entry
+// is one bit of a W-word bitmap per column, and the count of the rows before it
+// is a population count: no sort, no order of atomics that matters.
+//
+// Rows move along R and R^T:
+//   dispatch            xs[slot] = x[row]
+//   its gradient        gx[i] = sum over row i of gxs[slot]
+//   combine             y[i] = sum over row i of v ys[slot]
+//   its gradient        gys[slot] = v gy[row],  gv = <gy[row], ys[slot]>
+// All four go by the rows of R: a row's own side is read or written once, in
+// one place, and sums of a row are taken in the order of its entries in 32 bits
+// (one rounding, when stored), so equal inputs give equal bits.
+// Entries whose column is no column of R have slot -1 and take no part.
+#include <climits>
+
+#include "routing.cuh"
+#include "ws_internal.cuh"
+
+namespace wsk {
+namespace {
+
+// ---------------------------------------------------------------- R transposed
+
+constexpr int kBuildWarps = 16;
+constexpr int kTileRows = 32 * kBuildWarps;
+constexpr int kOneLaunchRows = 2 * kTileRows;  // rows that one CTA takes alone
+
+// Marks the columns of the tile's rows: bit i of mask[warp * cols + e] is row 32 warp + i.
+// With `place`, the second walk: pre[warp * cols + e] holds the slot of the warp's first entry of column e.
+template <bool place>
+__device__ __forceinline__ void walk_tile(const ws_routing& r, int64_t row0, int cols, uint32_t* mask, const int* pre) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t first = row0 + 32 * warp;
+  if (first >= r.nrows) return;
+  int begin = 0, end = 0;
+  entry_range(r.rowptr, min(first + lane, r.nrows - 1), r.nnz, &begin, &end);
+  if (first + lane >= r.nrows) begin = end;
+  const int lo = __shfl_sync(0xffffffffu, begin, 0);
+  const int hi = __shfl_sync(0xffffffffu, end, 31);
+  for (int64_t base = lo; base < hi; base += 32) {
+    const int64_t e = base + lane;
+    int row = 0;  // rows of the warp that end at or before e
+#pragma unroll
+    for (int step = 16; step; step >>= 1) {
+      const int last = __shfl_sync(0xffffffffu, end, row + step - 1);
+      if (last <= e) row += step;
+    }
+    if (e < hi && first + row < r.nrows) {
+      const int col = r.colidx[e];
+      const bool in = static_cast<unsigned>(col) < static_cast<unsigned>(cols);
+      uint32_t* word = mask + warp * cols + col;
+      if (!place) {
+        if (in) atomicOr(word, 1u << row);
+      } else {
+        int slot = -1;
+        if (in) {
+          slot = pre[warp * cols + col] + __popc(*word & ((1u << row) - 1u));
+          r.rows[slot] = static_cast<int32_t>(first + row);
+          r.entries[slot] = static_cast<int32_t>(e);
+        }
+        r.slots[e] = slot;
+      }
+    }
+  }
+}
+
+// Entries of every column in the rows [begin, end), added to cnt (shared).
+__device__ __forceinline__ void count_rows(const ws_routing& r, int64_t begin, int64_t end, int cols, uint32_t* mask,
+                                           int* cnt) {
+  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
+    for (int i = threadIdx.x; i < kBuildWarps * cols; i += blockDim.x) mask[i] = 0;
+    __syncthreads();
+    walk_tile<false>(r, row0, cols, mask, nullptr);
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) {
+      int n = 0;
+#pragma unroll
+      for (int w = 0; w < kBuildWarps; ++w) n += __popc(mask[w * cols + e]);
+      cnt[e] += n;
+    }
+    __syncthreads();
+  }
+}
+
+// Places the entries of the rows [begin, end); next[e] (shared) is the next slot of column e.
+__device__ __forceinline__ void place_rows(const ws_routing& r, int64_t begin, int64_t end, int cols, uint32_t* mask,
+                                           int* pre, int* next) {
+  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
+    for (int i = threadIdx.x; i < kBuildWarps * cols; i += blockDim.x) mask[i] = 0;
+    __syncthreads();
+    walk_tile<false>(r, row0, cols, mask, nullptr);
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) {
+      int n = next[e];
+#pragma unroll
+      for (int w = 0; w < kBuildWarps; ++w) {
+        pre[w * cols + e] = n;
+        n += __popc(mask[w * cols + e]);
+      }
+      next[e] = n;
+    }
+    __syncthreads();
+    walk_tile<true>(r, row0, cols, mask, pre);
+    __syncthreads();
+  }
+}
+
+// total[e] (shared) becomes the first slot of column e; returns the number of placed entries.
+__device__ __forceinline__ int scan_columns(int cols, int* total, int* scratch) {
+  int sum = 0;
+  for (int e0 = 0; e0 < cols; e0 += blockDim.x) {
+    const int e = e0 + threadIdx.x;
+    const int n = e < cols ? total[e] : 0;
+    int all = 0;
+    const int before = block_exclusive_scan(n, scratch, &all);
+    if (e < cols) total[e] = sum + before;
+    sum += all;
+  }
+  __syncthreads();
+  return sum;
+}
+
+// Offsets of all columns, and -1 in the slots that entries of no column leave over.
+__device__ __forceinline__ void write_offsets(const ws_routing& r, int cols, const int* first, int placed) {
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) r.offsets[e] = first[e];
+  if (threadIdx.x == 0) r.offsets[cols] = placed;
+  for (int64_t i = placed + static_cast<int64_t>(threadIdx.x); i < r.nnz; i += blockDim.x) r.rows[i] = r.entries[i] = -1;
+}
+
+// Shared memory of the build kernels: mask and pre [kBuildWarps][cols], next [cols].
+size_t build_smem(int cols) { return (2 * kBuildWarps + 1) * static_cast<size_t>(cols) * sizeof(int); }
+
+__global__ void __launch_bounds__(kTileRows) routing_small_kernel(ws_routing r, int cols) {
+  extern __shared__ int sm[];
+  __shared__ int scratch[32];
+  uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
+  int* pre = sm + kBuildWarps * cols;
+  int* next = pre + kBuildWarps * cols;
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = 0;
+  count_rows(r, 0, r.nrows, cols, mask, next);
+  __syncthreads();
+  const int placed = scan_columns(cols, next, scratch);
+  write_offsets(r, cols, next, placed);
+  __syncthreads();
+  place_rows(r, 0, r.nrows, cols, mask, pre, next);
+}
+
+__global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, int cols, int64_t chunk, int32_t* counts) {
+  extern __shared__ int sm[];
+  uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
+  int* cnt = sm + kBuildWarps * cols;
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) cnt[e] = 0;
+  const int64_t begin = chunk * blockIdx.x;
+  count_rows(r, begin, min(begin + chunk, r.nrows), cols, mask, cnt);
+  __syncthreads();
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) counts[static_cast<int64_t>(blockIdx.x) * cols + e] = cnt[e];
+}
+
+// Every CTA adds up the counts of all chunks by itself (a few hundred KB from L2, the threads split over the chunks):
+// a launch less than a scan of its own.
+__global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, int cols, int64_t chunk,
+                                                                  const int32_t* counts) {
+  extern __shared__ int sm[];
+  __shared__ int scratch[32];
+  uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
+  int* pre = sm + kBuildWarps * cols;
+  int* next = pre + kBuildWarps * cols;
+  int* before = sm;       // [cols], entries of the chunks before this one: taken out of use before the masks
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = before[e] = 0;
+  __syncthreads();
+  const int groups = cols >= static_cast<int>(blockDim.x) ? 1 : blockDim.x / cols;
+  const int g = static_cast<int>(threadIdx.x) / cols;
+  for (int e = threadIdx.x - g * cols; g < groups && e < cols; e += blockDim.x) {
+    int total = 0, mine = 0;
+#pragma unroll 8
+    for (int c = g; c < static_cast<int>(gridDim.x); c += groups) {
+      const int n = counts[static_cast<int64_t>(c) * cols + e];
+      total += n;
+      if (c < static_cast<int>(blockIdx.x)) mine += n;
+    }
+    atomicAdd(&next[e], total);
+    atomicAdd(&before[e], mine);
+  }
+  __syncthreads();
+  const int placed = scan_columns(cols, next, scratch);
+  if (blockIdx.x == 0) write_offsets(r, cols, next, placed);
+  __syncthreads();
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
+  __syncthreads();
+  const int64_t begin = chunk * blockIdx.x;
+  place_rows(r, begin, min(begin + chunk, r.nrows), cols, mask, pre, next);
+}
+
+// ------------------------------------------------------------------ rows moved
+
+constexpr int kMoveThreads = 256;
+constexpr int kMoveWarps = kMoveThreads / 32;
+
+// The slot of entry e, or -1.
+__device__ __forceinline__ int slot_of(const ws_routing& r, int e) {
+  const int s = r.slots[e];
+  return static_cast<unsigned>(s) < static_cast<unsigned>(r.nnz) ? s : -1;
+}
+
+// The rows behind the placed entries (there are some only if entries have no column) are zero:
+// team `team` of `teams`, whose members go by `lane` of `lanes`, clears every teams-th of them.
+template <typename P>
+__device__ __forceinline__ void zero_rest(const ws_routing& r, char* rows, int64_t ld, int packs, int64_t team,
+                                          int64_t teams, int lane, int lanes) {
+  for (int64_t s = r.offsets[r.ncols] + team; s < r.nnz; s += teams)
+    for (int i = lane; i < packs; i += lanes) *reinterpret_cast<P*>(rows + s * ld + i * static_cast<int64_t>(sizeof(P))) = P{};
+}
+
+// A warp per (row, segment of 32 U packs): the segment is read once and stored to every slot of the row.
+template <typename P, int U>
+__global__ void __launch_bounds__(kMoveThreads)
+    dispatch_kernel(ws_routing r, const char* __restrict__ x, int64_t ldx, char* __restrict__ xs, int64_t ldxs,
+                    int packs, int segs) {
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5);
+  zero_rest<P>(r, xs, ldxs, packs, unit, static_cast<int64_t>(gridDim.x) * kMoveWarps, threadIdx.x & 31, 32);
+  const int64_t row = unit / segs;
+  if (row >= r.nrows) return;
+  const int at = static_cast<int>(unit - row * segs) * 32 * U + (threadIdx.x & 31);
+  int begin, end;
+  entry_range(r.rowptr, row, r.nnz, &begin, &end);
+  P v[U];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+    if (at + 32 * u < packs) v[u] = *reinterpret_cast<const P*>(x + row * ldx + (at + 32 * u) * static_cast<int64_t>(sizeof(P)));
+  for (int e = begin; e < end; ++e) {
+    const int s = slot_of(r, e);
+    if (s < 0) continue;
+    char* dst = xs + s * ldxs;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (at + 32 * u < packs) *reinterpret_cast<P*>(dst + (at + 32 * u) * static_cast<int64_t>(sizeof(P))) = v[u];
+  }
+}
+
+// A thread per (row, pack): sums over the row's entries, kBatch loads in flight.
+template <typename T, int N, bool weighted>
+__global__ void __launch_bounds__(kMoveThreads)
+    combine_kernel(ws_routing r, const T* __restrict__ ys, int64_t ldys, T* __restrict__ y, int64_t ldy, int packs,
+                   int segs) {
+  constexpr int kBatch = 4;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5);
+  const int64_t row = unit / segs;
+  if (row >= r.nrows) return;
+  const int at = static_cast<int>(unit - row * segs) * 32 + (threadIdx.x & 31);
+  if (at >= packs) return;
+  int begin, end;
+  entry_range(r.rowptr, row, r.nnz, &begin, &end);
+  float acc[N] = {};
+  for (int e0 = begin; e0 < end; e0 += kBatch) {
+    Pack<T, N> p[kBatch];
+    float w[kBatch];
+    bool on[kBatch];
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      const int s = e0 + j < end ? slot_of(r, e0 + j) : -1;
+      on[j] = s >= 0;
+      if (on[j]) {
+        p[j] = *reinterpret_cast<const Pack<T, N>*>(ys + s * ldys + at * N);
+        w[j] = weighted ? r.vals[e0 + j] : 1.0f;
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (!on[j]) continue;
+      float f[N];
+      unpack<T, N>(p[j], f);
+#pragma unroll
+      for (int i = 0; i < N; ++i) acc[i] = weighted ? fmaf(w[j], f[i], acc[i]) : acc[i] + f[i];
+    }
+  }
+  *reinterpret_cast<Pack<T, N>*>(y + row * ldy + at * N) = pack<T, N>(acc);
+}
+
+// A CTA per row: gy's row is read once for each group of four entries, whose
+// products with it are summed by the CTA in a fixed order.
+constexpr int kDotThreads = 128;
+constexpr int kDotGroup = 4;
+
+template <typename T, int N>
+__global__ void __launch_bounds__(kDotThreads)
+    combine_backward_kernel(ws_routing r, const T* __restrict__ gy, int64_t ldgy, const T* __restrict__ ys,
+                            int64_t ldys, T* __restrict__ gys, int64_t ldgys, float* __restrict__ gvals, int packs) {
+  __shared__ float part[kDotThreads / 32][kDotGroup];
+  const int64_t row = blockIdx.x;
+  zero_rest<Pack<T, N>>(r, reinterpret_cast<char*>(gys), ldgys * static_cast<int64_t>(sizeof(T)), packs, row, gridDim.x,
+                        threadIdx.x, kDotThreads);
+  int begin, end;
+  entry_range(r.rowptr, row, r.nnz, &begin, &end);
+  const T* g = gy + row * ldgy;
+  for (int e0 = begin; e0 < end; e0 += kDotGroup) {
+    int s[kDotGroup];
+    float w[kDotGroup], dot[kDotGroup];
+#pragma unroll
+    for (int j = 0; j < kDotGroup; ++j) {
+      s[j] = e0 + j < end ? slot_of(r, e0 + j) : -1;
+      w[j] = e0 + j < end ? r.vals[e0 + j] : 0.0f;
+      dot[j] = 0.0f;
+    }
+    for (int at = threadIdx.x; at < packs; at += kDotThreads) {
+      Pack<T, N> p[kDotGroup];
+#pragma unroll
+      for (int j = 0; j < kDotGroup; ++j)
+        if (s[j] >= 0) p[j] = *reinterpret_cast<const Pack<T, N>*>(ys + s[j] * ldys + at * N);
+      float a[N];
+      unpack<T, N>(*reinterpret_cast<const Pack<T, N>*>(g + at * N), a);
+#pragma unroll
+      for (int j = 0; j < kDotGroup; ++j) {
+        if (s[j] < 0) continue;
+        float f[N];
+        unpack<T, N>(p[j], f);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          dot[j] = fmaf(a[i], f[i], dot[j]);
+          f[i] = w[j] * a[i];
+        }
+        *reinterpret_cast<Pack<T, N>*>(gys + s[j] * ldgys + at * N) = pack<T, N>(f);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kDotGroup; ++j) dot[j] = warp_sum(dot[j]);
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+      for (int j = 0; j < kDotGroup; ++j) part[threadIdx.x >> 5][j] = dot[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < kDotGroup && e0 + static_cast<int>(threadIdx.x) < end) {
+      float sum = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kDotThreads / 32; ++i) sum += part[i][threadIdx.x];
+      gvals[e0 + threadIdx.x] = sum;
+    }
+    __syncthreads();
+  }
+}
+
+// Calls f with the widest pack (16, 8, 4 or 2 bytes) that every address and row length allows.
+template <typename F>
+void for_pack(uint64_t bits, F f) {
+  if (bits % 16 == 0) f(std::integral_constant<int, 16>());
+  else if (bits % 8 == 0) f(std::integral_constant<int, 8>());
+  else if (bits % 4 == 0) f(std::integral_constant<int, 4>());
+  else f(std::integral_constant<int, 2>());
+}
+template <int B>
+struct Bytes;
+template <>
+struct Bytes<16> { using type = uint4; };
+template <>
+struct Bytes<8> { using type = uint2; };
+template <>
+struct Bytes<4> { using type = uint32_t; };
+template <>
+struct Bytes<2> { using type = uint16_t; };
+
+template <typename F>
+void for_type(ws_dtype_t dt, F f) {
+  if (dt == WS_F32) f(float());
+  else if (dt == WS_BF16) f(__nv_bfloat16());
+  else f(__half());
+}
+
+int64_t value_size(ws_dtype_t dt) { return dt == WS_F32 ? 4 : 2; }
+uint64_t address_bits(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+
+unsigned warp_grid(int64_t units) { return static_cast<unsigned>((units + kMoveWarps - 1) / kMoveWarps); }
+
+}  // namespace
+
+// As many chunks as SMs at most, of whole tiles.
+int64_t routing_chunks(int64_t nrows, int num_sms) {
+  if (nrows <= kOneLaunchRows) return 1;
+  const int64_t tiles = (nrows + kTileRows - 1) / kTileRows;
+  const int64_t each = (tiles + num_sms - 1) / num_sms;
+  return (tiles + each - 1) / each;
+}
+
+void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cudaStream_t s) {
+  const int cols = static_cast<int>(r.ncols);
+  const size_t smem = build_smem(cols);
+  const int64_t chunks = routing_chunks(r.nrows, num_sms);
+  const auto allow = [&](const void* kernel) {
+    if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  };
+  if (chunks == 1) {
+    allow(reinterpret_cast<const void*>(routing_small_kernel));
+    routing_small_kernel<<<1, kTileRows, smem, s>>>(r, cols);
+    return;
+  }
+  const int64_t tiles = (r.nrows + kTileRows - 1) / kTileRows;
+  const int64_t chunk = (tiles + chunks - 1) / chunks * kTileRows;
+  allow(reinterpret_cast<const void*>(routing_count_kernel));
+  allow(reinterpret_cast<const void*>(routing_place_kernel));
+  routing_count_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
+  routing_place_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
+}
+
+void launch_dispatch(const ws_routing& r, const void* x, int64_t ldx, void* xs, int64_t ldxs, int64_t width,
+                     ws_dtype_t dt, cudaStream_t s) {
+  const int64_t z = value_size(dt);
+  for_pack(address_bits(x) | address_bits(xs) | (ldx * z) | (ldxs * z) | (width * z), [&](auto b) {
+    constexpr int B = decltype(b)::value;
+    using P = typename Bytes<B>::type;
+    const int packs = static_cast<int>(width * z / B);
+    const char* src = static_cast<const char*>(x);
+    char* dst = static_cast<char*>(xs);
+    // Four packs a lane where the warps still fill the GPU, else one: a short call lasts as long as its longest warp.
+    if (r.nrows * static_cast<int64_t>(packs) >= 32 * 4 * 8192) {
+      const int segs = (packs + 127) / 128;
+      dispatch_kernel<P, 4><<<warp_grid(r.nrows * segs), kMoveThreads, 0, s>>>(r, src, ldx * z, dst, ldxs * z, packs, segs);
+    } else {
+      const int segs = (packs + 31) / 32;
+      dispatch_kernel<P, 1><<<warp_grid(r.nrows * segs), kMoveThreads, 0, s>>>(r, src, ldx * z, dst, ldxs * z, packs, segs);
+    }
+  });
+}
+
+void launch_combine(const ws_routing& r, bool weighted, const void* ys, int64_t ldys, void* y, int64_t ldy,
+                    int64_t width, ws_dtype_t dt, cudaStream_t s) {
+  const int64_t z = value_size(dt);
+  for_type(dt, [&](auto t) {
+    using T = decltype(t);
+    for_pack(address_bits(ys) | address_bits(y) | (ldys * z) | (ldy * z) | (width * z), [&](auto b) {
+      constexpr int B = decltype(b)::value;
+      if constexpr (B >= static_cast<int>(sizeof(T))) {
+        constexpr int N = B / sizeof(T);
+        const int packs = static_cast<int>(width / N), segs = (packs + 31) / 32;
+        auto kernel = weighted ? combine_kernel<T, N, true> : combine_kernel<T, N, false>;
+        kernel<<<warp_grid(r.nrows * segs), kMoveThreads, 0, s>>>(r, static_cast<const T*>(ys), ldys, static_cast<T*>(y),
+                                                                  ldy, packs, segs);
+      }
+    });
+  });
+}
+
+void launch_combine_backward(const ws_routing& r, const void* gy, int64_t ldgy, const void* ys, int64_t ldys,
+                             void* gys, int64_t ldgys, float* gvals, int64_t width, ws_dtype_t dt, cudaStream_t s) {
+  const int64_t z = value_size(dt);
+  for_type(dt, [&](auto t) {
+    using T = decltype(t);
+    for_pack(address_bits(gy) | address_bits(ys) | address_bits(gys) | (ldgy * z) | (ldys * z) | (ldgys * z) | (width * z),
+             [&](auto b) {
+               constexpr int B = decltype(b)::value;
+               if constexpr (B >= static_cast<int>(sizeof(T))) {
+                 constexpr int N = B / sizeof(T);
+                 combine_backward_kernel<T, N><<<static_cast<unsigned>(r.nrows), kDotThreads, 0, s>>>(
+                     r, static_cast<const T*>(gy), ldgy, static_cast<const T*>(ys), ldys, static_cast<T*>(gys), ldgys,
+                     gvals, static_cast<int>(width / N));
+               }
+             });
+  });
+}
+
+}  // namespace wsk

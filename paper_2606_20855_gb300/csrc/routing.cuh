@@ -1,0 +1,86 @@
+// Declarations shared by the operators on sparse routing matrices: route.cu
+// (rows of R chosen from logits), routing.cu (R transposed; rows gathered and
+// summed), grouped.cu (products by column of R), adapters.cu, routing_api.cu.
+#pragma once
+
+#include <cstdint>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+
+#include "ws_spgemm.h"
+
+namespace wsk {
+
+constexpr int kRouteMaxCols = 1024;  // columns of a routing matrix: a warp of the choice holds a row, 32 logits a lane
+constexpr int kRouteMaxK = 32;       // entries chosen in a row: one a lane
+
+// Message of ws_last_error() on the calling thread (api.cu); never throws.
+ws_status_t routing_fail(ws_status_t st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
+template <typename T>
+__device__ __forceinline__ float to_f32(T v);
+template <>
+__device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <>
+__device__ __forceinline__ float to_f32<__half>(__half v) { return __half2float(v); }
+template <typename T>
+__device__ __forceinline__ T from_f32(float v);
+template <>
+__device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <>
+__device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <>
+__device__ __forceinline__ __half from_f32<__half>(float v) { return __float2half_rn(v); }
+
+// N consecutive values of T, moved as one access.
+template <typename T, int N>
+struct alignas(sizeof(T) * N) Pack {
+  T v[N];
+};
+
+template <typename T, int N>
+__device__ __forceinline__ void unpack(const Pack<T, N>& p, float (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) f[i] = to_f32<T>(p.v[i]);
+}
+template <typename T, int N>
+__device__ __forceinline__ Pack<T, N> pack(const float (&f)[N]) {
+  Pack<T, N> p;
+#pragma unroll
+  for (int i = 0; i < N; ++i) p.v[i] = from_f32<T>(f[i]);
+  return p;
+}
+
+// Stored entries of row i, whatever rowptr holds: a range inside [0, nnz].
+__device__ __forceinline__ void entry_range(const int64_t* rowptr, int64_t i, int64_t nnz, int* begin, int* end) {
+  const int64_t b = rowptr[i], e = rowptr[i + 1];
+  const int64_t bc = b < 0 ? 0 : b > nnz ? nnz : b;
+  *begin = static_cast<int>(bc);
+  *end = static_cast<int>(e < bc ? bc : e > nnz ? nnz : e);
+}
+
+__device__ __forceinline__ float warp_sum(float x) {
+#pragma unroll
+  for (int o = 16; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+  return x;
+}
+
+// Launchers.  They queue kernels on s and leave errors to cudaGetLastError.
+void launch_topk_route(const void* logits, int64_t rows, int cols, int64_t ld, ws_dtype_t dt, int k, bool normalize,
+                       int64_t* rowptr, int32_t* colidx, float* vals, cudaStream_t s);
+void launch_topk_route_backward(const void* logits, int64_t rows, int cols, int64_t ld, ws_dtype_t dt, int k,
+                                bool normalize, const int32_t* colidx, const float* vals, const float* gvals,
+                                void* glogits, int64_t ldg, cudaStream_t s);
+int64_t routing_chunks(int64_t nrows, int num_sms);  // chunks of rows counted apart (1: one launch does it all)
+void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cudaStream_t s);
+void launch_dispatch(const ws_routing& r, const void* x, int64_t ldx, void* xs, int64_t ldxs, int64_t width,
+                     ws_dtype_t dt, cudaStream_t s);
+void launch_combine(const ws_routing& r, bool weighted, const void* ys, int64_t ldys, void* y, int64_t ldy,
+                    int64_t width, ws_dtype_t dt, cudaStream_t s);
+void launch_combine_backward(const ws_routing& r, const void* gy, int64_t ldgy, const void* ys, int64_t ldys,
+                             void* gys, int64_t ldgys, float* gvals, int64_t width, ws_dtype_t dt, cudaStream_t s);
+
+}  // namespace wsk

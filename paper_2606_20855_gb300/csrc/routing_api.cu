@@ -1,0 +1,171 @@
+// C entry points of the operations on routing matrices (declared in
+// include/ws_spgemm.h): argument checks, then the launchers.  Nothing here
+// allocates, waits or throws.
+#include <climits>
+#include <initializer_list>
+
+#include "routing.cuh"
+
+using namespace wsk;
+
+namespace {
+
+constexpr int64_t kMaxWidth = 1 << 24;
+
+bool row_type(ws_dtype_t dt) { return dt == WS_F32 || dt == WS_BF16 || dt == WS_F16; }
+
+cudaStream_t cuda_stream(ws_stream_t s) { return reinterpret_cast<cudaStream_t>(s); }
+
+ws_status_t launched(const char* what) {
+  const cudaError_t e = cudaGetLastError();
+  return e == cudaSuccess ? WS_OK : routing_fail(WS_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+
+ws_status_t sm_count(int* n) {
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e == cudaSuccess) e = cudaDeviceGetAttribute(n, cudaDevAttrMultiProcessorCount, dev);
+  return e == cudaSuccess ? WS_OK : routing_fail(WS_ERR_CUDA, "device query: %s", cudaGetErrorString(e));
+}
+
+// Sizes and arrays of a routing matrix; `built`: its transpose is there too.
+ws_status_t check(const ws_routing* r) {
+  if (!r) return routing_fail(WS_ERR_INVALID_ARG, "NULL routing matrix");
+  if (r->nrows < 0 || r->ncols < 0 || r->nnz < 0) return routing_fail(WS_ERR_INVALID_ARG, "negative size");
+  if (r->nrows > INT32_MAX || r->nnz > INT32_MAX || r->ncols > kRouteMaxCols)
+    return routing_fail(WS_ERR_OVERFLOW, "routing matrix %lld x %lld with %lld entries: at most %d columns and %d rows and entries",
+                        static_cast<long long>(r->nrows), static_cast<long long>(r->ncols),
+                        static_cast<long long>(r->nnz), kRouteMaxCols, INT32_MAX);
+  if (r->nnz > 0 && (r->nrows == 0 || r->ncols == 0))
+    return routing_fail(WS_ERR_SHAPE, "entries in a routing matrix without rows or columns");
+  if (!r->rowptr || !r->offsets || (r->nnz > 0 && (!r->colidx || !r->rows || !r->entries || !r->slots)))
+    return routing_fail(WS_ERR_INVALID_ARG, "NULL array in a routing matrix");
+  return WS_OK;
+}
+
+struct Dense {
+  const void* p;
+  int64_t rows, ld;
+};
+
+// The dense operands of a call that moves rows of `width` values.
+ws_status_t check_rows(const ws_routing* r, int64_t width, ws_dtype_t dt, std::initializer_list<Dense> all) {
+  if (const ws_status_t st = check(r)) return st;
+  if (!row_type(dt)) return routing_fail(WS_ERR_DTYPE, "dense rows are float, bfloat16 or half");
+  if (width < 0) return routing_fail(WS_ERR_INVALID_ARG, "negative width");
+  if (width > kMaxWidth || r->nrows * ((width + 31) / 32) / 8 >= INT32_MAX)
+    return routing_fail(WS_ERR_OVERFLOW, "rows of %lld values", static_cast<long long>(width));
+  const uintptr_t size = dt == WS_F32 ? 4 : 2;
+  for (const Dense& d : all) {
+    if (d.rows > 0 && width > 0 && !d.p) return routing_fail(WS_ERR_INVALID_ARG, "NULL dense matrix");
+    if (d.ld < width && d.rows > 1) return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
+    if (reinterpret_cast<uintptr_t>(d.p) % size) return routing_fail(WS_ERR_INVALID_ARG, "misaligned dense matrix");
+  }
+  return WS_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ws_status_t ws_topk_route(const void* logits, int64_t rows, int64_t cols, int64_t ld, ws_dtype_t dtype, int k,
+                          int normalize, int64_t* rowptr, int32_t* colidx, float* vals, ws_stream_t stream) {
+  if (rows < 0 || cols < 1 || k < 1 || k > cols || k > kRouteMaxK)
+    return routing_fail(WS_ERR_INVALID_ARG, "k must be in 1..min(cols, %d)", kRouteMaxK);
+  if (!row_type(dtype)) return routing_fail(WS_ERR_DTYPE, "logits are float, bfloat16 or half");
+  if (cols > kRouteMaxCols || rows > INT32_MAX / k)
+    return routing_fail(WS_ERR_OVERFLOW, "at most %d columns and %d entries", kRouteMaxCols, INT32_MAX);
+  if (!rowptr || (rows > 0 && (!logits || !colidx || !vals)) || (rows > 1 && ld < cols) ||
+      reinterpret_cast<uintptr_t>(logits) % (dtype == WS_F32 ? 4 : 2))
+    return routing_fail(WS_ERR_INVALID_ARG, "NULL or misaligned pointer, or row stride smaller than the row");
+  if (rows == 0) {
+    cudaMemsetAsync(rowptr, 0, sizeof(int64_t), cuda_stream(stream));
+    return launched("ws_topk_route");
+  }
+  launch_topk_route(logits, rows, static_cast<int>(cols), ld, dtype, k, normalize != 0, rowptr, colidx, vals, cuda_stream(stream));
+  return launched("ws_topk_route");
+}
+
+ws_status_t ws_topk_route_backward(const void* logits, int64_t rows, int64_t cols, int64_t ld, ws_dtype_t dtype,
+                                   int k, int normalize, const int32_t* colidx, const float* vals,
+                                   const float* gvals, void* glogits, int64_t ldg, ws_stream_t stream) {
+  if (rows < 0 || cols < 1 || k < 1 || k > cols || k > kRouteMaxK)
+    return routing_fail(WS_ERR_INVALID_ARG, "k must be in 1..min(cols, %d)", kRouteMaxK);
+  if (!row_type(dtype)) return routing_fail(WS_ERR_DTYPE, "logits are float, bfloat16 or half");
+  if (cols > kRouteMaxCols || rows > INT32_MAX / k)
+    return routing_fail(WS_ERR_OVERFLOW, "at most %d columns and %d entries", kRouteMaxCols, INT32_MAX);
+  const uintptr_t size = dtype == WS_F32 ? 4 : 2;
+  if ((rows > 0 && (!colidx || !vals || !gvals || !glogits || (!normalize && !logits))) || (rows > 1 && ldg < cols) ||
+      (rows > 1 && !normalize && ld < cols) || reinterpret_cast<uintptr_t>(glogits) % size ||
+      (!normalize && reinterpret_cast<uintptr_t>(logits) % size))
+    return routing_fail(WS_ERR_INVALID_ARG, "NULL or misaligned pointer, or row stride smaller than the row");
+  if (rows == 0) return WS_OK;
+  launch_topk_route_backward(logits, rows, static_cast<int>(cols), ld, dtype, k, normalize != 0, colidx, vals, gvals,
+                             glogits, ldg, cuda_stream(stream));
+  return launched("ws_topk_route_backward");
+}
+
+int64_t ws_routing_scratch(int64_t nrows, int64_t ncols) {
+  int sms = 0;
+  if (nrows < 0 || ncols < 0 || sm_count(&sms) != WS_OK) return 0;
+  const int64_t chunks = routing_chunks(nrows, sms);
+  return chunks == 1 ? 0 : chunks * ncols * static_cast<int64_t>(sizeof(int32_t));
+}
+
+ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
+  if (const ws_status_t st = check(r)) return st;
+  if (r->nnz == 0) {
+    cudaMemsetAsync(r->offsets, 0, static_cast<size_t>(r->ncols + 1) * sizeof(int64_t), cuda_stream(stream));
+    return launched("ws_routing_build");
+  }
+  int sms = 0;
+  if (const ws_status_t st = sm_count(&sms)) return st;
+  const int64_t chunks = routing_chunks(r->nrows, sms);
+  if (chunks > 1 && (!scratch || scratch_bytes < chunks * r->ncols * static_cast<int64_t>(sizeof(int32_t))))
+    return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_routing_scratch");
+  launch_routing_build(*r, static_cast<int32_t*>(scratch), sms, cuda_stream(stream));
+  return launched("ws_routing_build");
+}
+
+ws_status_t ws_routing_dispatch(const ws_routing* r, const void* x, int64_t ldx, void* xs, int64_t ldxs,
+                                int64_t width, ws_dtype_t dtype, ws_stream_t stream) {
+  if (const ws_status_t st = check_rows(r, width, dtype, {{x, r ? r->nrows : 0, ldx}, {xs, r ? r->nnz : 0, ldxs}})) return st;
+  if (r->nnz == 0 || width == 0) return WS_OK;
+  launch_dispatch(*r, x, ldx, xs, ldxs, width, dtype, cuda_stream(stream));
+  return launched("ws_routing_dispatch");
+}
+
+ws_status_t ws_routing_dispatch_backward(const ws_routing* r, const void* gxs, int64_t ldgxs, void* gx, int64_t ldgx,
+                                         int64_t width, ws_dtype_t dtype, ws_stream_t stream) {
+  if (const ws_status_t st = check_rows(r, width, dtype, {{gxs, r ? r->nnz : 0, ldgxs}, {gx, r ? r->nrows : 0, ldgx}})) return st;
+  if (r->nrows == 0 || width == 0) return WS_OK;
+  launch_combine(*r, false, gxs, ldgxs, gx, ldgx, width, dtype, cuda_stream(stream));
+  return launched("ws_routing_dispatch_backward");
+}
+
+ws_status_t ws_routing_combine(const ws_routing* r, const void* ys, int64_t ldys, void* y, int64_t ldy,
+                               int64_t width, ws_dtype_t dtype, ws_stream_t stream) {
+  if (const ws_status_t st = check_rows(r, width, dtype, {{ys, r ? r->nnz : 0, ldys}, {y, r ? r->nrows : 0, ldy}})) return st;
+  if (r->nnz > 0 && !r->vals) return routing_fail(WS_ERR_INVALID_ARG, "NULL values");
+  if (r->nrows == 0 || width == 0) return WS_OK;
+  launch_combine(*r, true, ys, ldys, y, ldy, width, dtype, cuda_stream(stream));
+  return launched("ws_routing_combine");
+}
+
+ws_status_t ws_routing_combine_backward(const ws_routing* r, const void* gy, int64_t ldgy, const void* ys,
+                                        int64_t ldys, void* gys, int64_t ldgys, float* gvals, int64_t width,
+                                        ws_dtype_t dtype, ws_stream_t stream) {
+  if (const ws_status_t st = check_rows(r, width, dtype, {{gy, r ? r->nrows : 0, ldgy}, {ys, r ? r->nnz : 0, ldys},
+                                                          {gys, r ? r->nnz : 0, ldgys}}))
+    return st;
+  if (r->nnz > 0 && (!r->vals || !gvals)) return routing_fail(WS_ERR_INVALID_ARG, "NULL values");
+  if (r->nnz == 0) return WS_OK;
+  if (width == 0) {
+    cudaMemsetAsync(gvals, 0, static_cast<size_t>(r->nnz) * sizeof(float), cuda_stream(stream));
+    return launched("ws_routing_combine_backward");
+  }
+  launch_combine_backward(*r, gy, ldgy, ys, ldys, gys, ldgys, gvals, width, dtype, cuda_stream(stream));
+  return launched("ws_routing_combine_backward");
+}
+
+}  // extern "C"
