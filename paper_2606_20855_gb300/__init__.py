@@ -15,10 +15,11 @@ __all__ += _ROUTING
 
 
 def __getattr__(name):
-    if name in _ROUTING:
-        from . import routing as _r
-        return getattr(_r, name)
-    if name in __all__:
-        from . import spgemm as _m
-        return getattr(_m, name)
-    raise AttributeError(name)
+    if name not in __all__:
+        raise AttributeError(name)
+    import importlib
+    here = globals()
+    for module, names in (("spgemm", [n for n in __all__ if n not in _ROUTING]), ("routing", _ROUTING)):
+        m = importlib.import_module(f"{__name__}.{module}")
+        here.update({n: getattr(m, n) for n in names})  # the function spgemm over the submodule of that name
+    return here[name]

@@ -282,18 +282,42 @@ __global__ void __launch_bounds__(kMoveThreads)
 }
 
 // A CTA per row: gy's row is read once for each group of four entries, whose
-// products with it are summed by the CTA in a fixed order.
+// products with it are summed by the CTA in a fixed order.  A thread takes 16
+// bytes of a row at a time, in packs of M values as far as the addresses
+// allow, so the order does not depend on strides and alignment.
 constexpr int kDotThreads = 128;
 constexpr int kDotGroup = 4;
 
-template <typename T, int N>
+template <typename T, int M, int N>
+__device__ __forceinline__ void load_group(const T* p, int count, float (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += M) {
+    float part[M] = {};
+    if (M == N || i < count) unpack<T, M>(*reinterpret_cast<const Pack<T, M>*>(p + i), part);
+#pragma unroll
+    for (int j = 0; j < M; ++j) f[i + j] = part[j];
+  }
+}
+template <typename T, int M, int N>
+__device__ __forceinline__ void store_group(T* p, int count, const float (&f)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += M) {
+    float part[M];
+#pragma unroll
+    for (int j = 0; j < M; ++j) part[j] = f[i + j];
+    if (M == N || i < count) *reinterpret_cast<Pack<T, M>*>(p + i) = pack<T, M>(part);
+  }
+}
+
+template <typename T, int M>
 __global__ void __launch_bounds__(kDotThreads)
     combine_backward_kernel(ws_routing r, const T* __restrict__ gy, int64_t ldgy, const T* __restrict__ ys,
-                            int64_t ldys, T* __restrict__ gys, int64_t ldgys, float* __restrict__ gvals, int packs) {
+                            int64_t ldys, T* __restrict__ gys, int64_t ldgys, float* __restrict__ gvals, int width) {
+  constexpr int N = 16 / sizeof(T);
   __shared__ float part[kDotThreads / 32][kDotGroup];
   const int64_t row = blockIdx.x;
-  zero_rest<Pack<T, N>>(r, reinterpret_cast<char*>(gys), ldgys * static_cast<int64_t>(sizeof(T)), packs, row, gridDim.x,
-                        threadIdx.x, kDotThreads);
+  zero_rest<Pack<T, M>>(r, reinterpret_cast<char*>(gys), ldgys * static_cast<int64_t>(sizeof(T)), width / M, row,
+                        gridDim.x, threadIdx.x, kDotThreads);
   int begin, end;
   entry_range(r.rowptr, row, r.nnz, &begin, &end);
   const T* g = gy + row * ldgy;
@@ -306,24 +330,22 @@ __global__ void __launch_bounds__(kDotThreads)
       w[j] = e0 + j < end ? r.vals[e0 + j] : 0.0f;
       dot[j] = 0.0f;
     }
-    for (int at = threadIdx.x; at < packs; at += kDotThreads) {
-      Pack<T, N> p[kDotGroup];
+    for (int at = threadIdx.x * N; at < width; at += kDotThreads * N) {
+      const int count = width - at;
+      float a[N], f[kDotGroup][N];
 #pragma unroll
       for (int j = 0; j < kDotGroup; ++j)
-        if (s[j] >= 0) p[j] = *reinterpret_cast<const Pack<T, N>*>(ys + s[j] * ldys + at * N);
-      float a[N];
-      unpack<T, N>(*reinterpret_cast<const Pack<T, N>*>(g + at * N), a);
+        if (s[j] >= 0) load_group<T, M, N>(ys + s[j] * ldys + at, count, f[j]);
+      load_group<T, M, N>(g + at, count, a);
 #pragma unroll
       for (int j = 0; j < kDotGroup; ++j) {
         if (s[j] < 0) continue;
-        float f[N];
-        unpack<T, N>(p[j], f);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          dot[j] = fmaf(a[i], f[i], dot[j]);
-          f[i] = w[j] * a[i];
+          dot[j] = fmaf(a[i], f[j][i], dot[j]);
+          f[j][i] = w[j] * a[i];
         }
-        *reinterpret_cast<Pack<T, N>*>(gys + s[j] * ldgys + at * N) = pack<T, N>(f);
+        store_group<T, M, N>(gys + s[j] * ldgys + at, count, f[j]);
       }
     }
 #pragma unroll
@@ -454,7 +476,7 @@ void launch_combine_backward(const ws_routing& r, const void* gy, int64_t ldgy, 
                  constexpr int N = B / sizeof(T);
                  combine_backward_kernel<T, N><<<static_cast<unsigned>(r.nrows), kDotThreads, 0, s>>>(
                      r, static_cast<const T*>(gy), ldgy, static_cast<const T*>(ys), ldys, static_cast<T*>(gys), ldgys,
-                     gvals, static_cast<int>(width / N));
+                     gvals, static_cast<int>(width));
                }
              });
   });

@@ -177,7 +177,7 @@ def test_sorted_by_column(T, E, kind):
 @pytest.mark.parametrize("T,E", [(0, 4), (0, 0), (5, 0), (5, 7), (3000, 7)])
 def test_no_entries(T, E):
     from paper_2606_20855_gb300 import Routing
-    R = _matrix(T, E, [0] * T, 0) if T and E else _matrix(max(T, 1), max(E, 1), [0], 0)
+    R = _matrix(T, E, [0] * T, 0) if T and E else _matrix(max(T, 1), max(E, 1), [0] * max(T, 1), 0)
     R.nrows, R.ncols, R.rowptr = T, E, torch.zeros(T + 1, dtype=torch.int64, device="cuda")
     plan = Routing(R)
     assert torch.equal(plan.offsets, torch.zeros(E + 1, dtype=torch.int64, device="cuda"))
