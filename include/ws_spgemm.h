@@ -403,6 +403,7 @@ typedef struct ws_routing {
   int32_t* rows;         /* [nnz]: row of every slot (the columns of R^T, ascending within a column) */
   int32_t* entries;      /* [nnz]: entry of R in every slot */
   int32_t* slots;        /* [nnz]: slot of every entry of R */
+  int32_t* status;       /* [1]: cleared by ws_routing_build; nonzero after a product whose bounded waits ran out */
 } ws_routing;
 
 /*
@@ -431,6 +432,27 @@ ws_status_t ws_routing_combine(const ws_routing* r, const void* ys, int64_t ldys
 ws_status_t ws_routing_combine_backward(const ws_routing* r, const void* gy, int64_t ldgy, const void* ys,
                                         int64_t ldys, void* gys, int64_t ldgys, float* gvals, int64_t width,
                                         ws_dtype_t dtype, ws_stream_t stream);
+
+/*
+ * Products by column of R: column e has a matrix W[e], N x K, row-major (ldw
+ * values from row to row, `stride` from matrix to matrix), and the rows of its
+ * slots.  bfloat16 or half, sums in 32 bits, one rounding.
+ *   matmul           ys[s] = W[e] xs[s]                     xs: nnz x K, ys: nnz x N
+ *   matmul_rows      gxs[s] = W[e]^T gys[s]                 gys: nnz x N, gxs: nnz x K
+ *   matmul_weights   gW[e] = sum over s of gys[s] xs[s]^T   zero for columns without entries
+ * Rows behind the placed entries are not written (matmul, matmul_rows).  The inputs'
+ * addresses and strides are multiples of 16 bytes; outputs need no alignment
+ * beyond their type's.  N, K <= 2^24.
+ */
+ws_status_t ws_routing_matmul(const ws_routing* r, const void* xs, int64_t ldxs, const void* W, int64_t ldw,
+                              int64_t stride, int64_t N, int64_t K, void* ys, int64_t ldys, ws_dtype_t dtype,
+                              ws_stream_t stream);
+ws_status_t ws_routing_matmul_rows(const ws_routing* r, const void* gys, int64_t ldgys, const void* W, int64_t ldw,
+                                   int64_t stride, int64_t N, int64_t K, void* gxs, int64_t ldgxs, ws_dtype_t dtype,
+                                   ws_stream_t stream);
+ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int64_t ldgys, const void* xs,
+                                      int64_t ldxs, int64_t N, int64_t K, void* gW, int64_t ldgw, int64_t stride,
+                                      ws_dtype_t dtype, ws_stream_t stream);
 
 #ifdef __cplusplus
 }

@@ -60,13 +60,16 @@ SIGNATURES = [
     ("ws_routing_dispatch_backward", _i32, [_p, _p, _i64, _p, _i64, _i64, _i32, _p]),
     ("ws_routing_combine", _i32, [_p, _p, _i64, _p, _i64, _i64, _i32, _p]),
     ("ws_routing_combine_backward", _i32, [_p, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i32, _p]),
+    ("ws_routing_matmul", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p]),
+    ("ws_routing_matmul_rows", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p]),
+    ("ws_routing_matmul_weights", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _i64, _i32, _p]),
 ]
 
 
 class WsRouting(ctypes.Structure):
     """struct ws_routing (device pointers as integers)."""
     _fields_ = [("nrows", _i64), ("ncols", _i64), ("nnz", _i64), ("rowptr", _p), ("colidx", _p), ("vals", _p),
-                ("offsets", _p), ("rows", _p), ("entries", _p), ("slots", _p)]
+                ("offsets", _p), ("rows", _p), ("entries", _p), ("slots", _p), ("status", _p)]
 
 EWISE_OPS = {"add": 1, "mul": 2}  # ws_ewise_op_t
 
@@ -261,3 +264,20 @@ def ws_routing_combine_backward(r, gy: int, ldgy: int, ys: int, ldys: int, gys: 
                                 width: int, dtype: int, stream: int) -> None:
     _check("ws_routing_combine_backward", load().ws_routing_combine_backward(r, gy, ldgy, ys, ldys, gys, ldgys, gvals,
                                                                              width, dtype, stream))
+
+
+def ws_routing_matmul(r, xs: int, ldxs: int, W: int, ldw: int, stride: int, N: int, K: int, ys: int, ldys: int,
+                      dtype: int, stream: int) -> None:
+    _check("ws_routing_matmul", load().ws_routing_matmul(r, xs, ldxs, W, ldw, stride, N, K, ys, ldys, dtype, stream))
+
+
+def ws_routing_matmul_rows(r, gys: int, ldgys: int, W: int, ldw: int, stride: int, N: int, K: int, gxs: int,
+                           ldgxs: int, dtype: int, stream: int) -> None:
+    _check("ws_routing_matmul_rows", load().ws_routing_matmul_rows(r, gys, ldgys, W, ldw, stride, N, K, gxs, ldgxs,
+                                                                   dtype, stream))
+
+
+def ws_routing_matmul_weights(r, gys: int, ldgys: int, xs: int, ldxs: int, N: int, K: int, gW: int, ldgw: int,
+                              stride: int, dtype: int, stream: int) -> None:
+    _check("ws_routing_matmul_weights", load().ws_routing_matmul_weights(r, gys, ldgys, xs, ldxs, N, K, gW, ldgw,
+                                                                         stride, dtype, stream))

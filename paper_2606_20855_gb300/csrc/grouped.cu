@@ -1,0 +1,562 @@
+// Products by column of a routing matrix: every column (expert) e has a matrix
+// W[e] (N x K) and, in slot order, the rows offsets[e] .. offsets[e + 1].
+//   forward    ys[s]  = W[e] xs[s]                      contraction over K
+//   rows       gxs[s] = W[e]^T gys[s]                   contraction over N
+//   weights    gW[e]  = sum over s of gys[s] xs[s]^T    contraction over the rows of e
+// bfloat16 or half operands, products and sums in 32 bits on the tensor cores
+// (tcgen05, accumulators in tensor memory), one rounding when a result is stored.
+//
+// One persistent CTA per SM: one warp's lane fetches operand tiles with TMA
+// (128-byte swizzle, a ring of stages), one lane issues the matrix
+// instructions, four warps store finished tiles while the next one is
+// multiplied (two accumulators).  How many rows an expert has is known on the
+// device only, so every CTA counts the tiles of all experts itself and takes
+// every gridDim-th one.  Operands are read as they lie in memory: an operand
+// whose contraction index runs along its rows (W in `rows`, both in `weights`)
+// is given to the tensor cores as "MN-major", never transposed by a copy.
+//
+// A tile of rows may reach past its expert's last row: such rows are computed
+// and not stored.  In `weights` they would be summed, so the last stage's rows
+// past the end are cleared in shared memory (in both operands: 0 * inf is NaN).
+#include <cuda.h>
+#include <type_traits>
+
+#include "routing.cuh"
+#include "ws_internal.cuh"
+
+namespace wsk {
+namespace {
+
+constexpr int kTileM = 128;   // rows of the M side: lanes of tensor memory
+constexpr int kTileK = 64;    // 128 bytes: the swizzle's span
+constexpr int kThreads = 192; // TMA warp, MMA warp, 4 epilogue warps
+constexpr int kBytesA = kTileM * kTileK * 2;
+constexpr unsigned long long kWaitLimitNs = 2000000000ull;
+
+// Where the rows of the experts are in the product D (M x N tile).
+constexpr int kRowsM = 0;    // on the M side (lanes)
+constexpr int kRowsN = 1;    // on the N side (columns): few rows per expert, W fills the lanes
+constexpr int kRowsSum = 2;  // summed over
+
+struct GroupedParams {
+  const int64_t* offsets;
+  int groups;
+  int64_t nnz;
+  int features;  // kRowsM, kRowsN: columns of the result; kRowsSum: rows of gW[e] (M side)
+  int width;     // kRowsSum: columns of gW[e] (N side)
+  int depth;     // contraction length; kRowsSum: unused
+  void* out;
+  int64_t ldo;   // values between rows of the result
+  int64_t group_stride;  // kRowsSum: values between gW[e]
+  bool half;
+  bool vec;      // rows of the result start at multiples of 16 bytes
+  int* status;
+};
+
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+
+__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bar_arrive(uint32_t bar) {
+  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+// Waits for a phase; gives up after kWaitLimitNs or when another role gave up (*dead).
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+  if (bar_try(bar, parity)) return true;
+  const unsigned long long start = now_ns();
+  for (unsigned i = 1;; ++i) {
+    if (bar_try(bar, parity)) return true;
+    if ((i & 31) == 0) {
+      if (*dead) return false;
+      if (now_ns() - start > kWaitLimitNs) {
+        *dead = 1;
+        return false;
+      }
+    }
+  }
+}
+
+__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+
+// Shared-memory matrix descriptor, 128-byte swizzle.  K-major: 8-row groups of
+// 1024 bytes follow each other.  MN-major: blocks of 64 (M or N) x 64 (K), in
+// which 8 steps of K take 1024 bytes; blocks are 8192 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major) {
+  const uint64_t lbo = mn_major ? 8192 >> 4 : 1, sbo = 1024 >> 4;
+  return (static_cast<uint64_t>(addr >> 4) & 0x3fff) | lbo << 16 | sbo << 32 | 1ull << 46 | 2ull << 61;
+}
+
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+      : "memory");
+}
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// 16 consecutive 32-bit columns of the warp's 32 lanes.
+__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&f)[16]) {
+  uint32_t r[16];
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(r[i]);
+}
+
+__device__ __forceinline__ uint16_t round16(float f, bool half) {
+  return half ? __half_as_ushort(__float2half_rn(f)) : __bfloat16_as_ushort(__float2bfloat16_rn(f));
+}
+
+// One tile of the product.
+struct Tile {
+  int group;
+  int m0, n0;    // first lane and column, in features (or gW's rows and columns)
+  int row0;      // first row of the experts' rows
+  int rows;      // rows from row0 on that are the group's
+  int steps;     // stages of the contraction
+};
+
+// Rows of a group in a tile, unless they are summed over.
+template <int BN, int kRows>
+constexpr int kRowTileOf = kRows == kRowsM ? kTileM : BN;
+
+template <int BN, int kRows>
+struct Shape {
+  static constexpr int kBytesB = BN * kTileK * 2;
+  static constexpr int kStageBytes = kBytesA + kBytesB;
+  static constexpr int kStages = (196 * 1024) / kStageBytes > 10 ? 10 : (196 * 1024) / kStageBytes;
+  static constexpr int kAccCols = 2 * BN < 32 ? 32 : 2 * BN;  // a power of two
+  static constexpr size_t kSmem = static_cast<size_t>(kStages) * kStageBytes + 1024;
+};
+
+// Tile t of the sequence that all roles of all CTAs share.  first[e]: row tiles of the groups before e.
+template <int BN, int kRows>
+__device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first, int64_t t, Tile* out) {
+  if constexpr (kRows == kRowsSum) {
+    const int mt = (p.features + kTileM - 1) / kTileM, nt = (p.width + BN - 1) / BN;
+    const int64_t each = static_cast<int64_t>(mt) * nt;
+    if (t >= each * p.groups) return false;
+    const int e = static_cast<int>(t / each);
+    const int i = static_cast<int>(t - each * e);
+    out->group = e;
+    out->m0 = i % mt * kTileM;
+    out->n0 = i / mt * BN;
+    const int64_t b = p.offsets[e], n = p.offsets[e + 1] - b;
+    out->row0 = static_cast<int>(b);
+    out->rows = static_cast<int>(n);
+    out->steps = static_cast<int>((n + kTileK - 1) / kTileK);
+  } else {
+    constexpr int kFeat = kRows == kRowsM ? BN : kTileM;
+    constexpr int kRowTile = kRowTileOf<BN, kRows>;
+    const int ft = (p.features + kFeat - 1) / kFeat;
+    const int64_t q = t / ft;
+    if (q >= first[p.groups]) return false;
+    int lo = 0, hi = p.groups - 1;  // the last group with first[e] <= q; groups without rows have none of their own
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (first[mid] <= q) lo = mid;
+      else hi = mid - 1;
+    }
+    const int e = lo;
+    const int rt = first[e + 1] - first[e];
+    const int i = static_cast<int>(t - static_cast<int64_t>(first[e]) * ft);
+    // eight row tiles side by side, so that CTAs at work together share rows and features in L2
+    const int band = i / (8 * ft), in = i - band * 8 * ft;
+    const int high = min(8, rt - 8 * band);
+    const int r = 8 * band + in % high, f = in / high;
+    out->group = e;
+    const int64_t b = p.offsets[e];
+    out->row0 = static_cast<int>(b) + r * kRowTile;
+    out->rows = static_cast<int>(p.offsets[e + 1] - b) - r * kRowTile;
+    out->m0 = kRows == kRowsM ? 0 : f * kFeat;
+    out->n0 = kRows == kRowsM ? f * kFeat : 0;
+    out->steps = (p.depth + kTileK - 1) / kTileK;
+  }
+  return true;
+}
+
+// Stores 16 values of a row of the result, `count` of them inside it.
+__device__ __forceinline__ void store_row16(const GroupedParams& p, uint16_t* dst, const float (&f)[16], int count) {
+  if (p.vec && count >= 16) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = round16(f[2 * i], p.half) | static_cast<uint32_t>(round16(f[2 * i + 1], p.half)) << 16;
+    reinterpret_cast<uint4*>(dst)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    reinterpret_cast<uint4*>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i < count) dst[i] = round16(f[i], p.half);
+  }
+}
+
+// a: the M side's operand (kRowsM: the experts' rows, kRowsN: W, kRowsSum: gys), b: the N side's.
+// kWMN: W's contraction index runs along its rows (MN-major).
+template <int BN, int kRows, bool kWMN>
+__global__ void __launch_bounds__(kThreads, 1)
+    grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const GroupedParams p) {
+  using S = Shape<BN, kRows>;
+  constexpr bool kAMN = kRows == kRowsSum || (kRows == kRowsN && kWMN);
+  constexpr bool kBMN = kRows == kRowsSum || (kRows == kRowsM && kWMN);
+  extern __shared__ uint8_t raw[];
+  __shared__ int first[kRouteMaxCols + 1];
+  __shared__ int scratch[32];
+  __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages], acc_full[2], acc_empty[2], last_bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int dead;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < S::kStages; ++i) {
+      bar_init(smem_u32(&full_bar[i]), 1);
+      bar_init(smem_u32(&empty_bar[i]), 1);
+    }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(smem_u32(&acc_full[i]), 1);
+      bar_init(smem_u32(&acc_empty[i]), 4);
+    }
+    bar_init(smem_u32(&last_bar), 1);
+    dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
+                 "r"(static_cast<uint32_t>(S::kAccCols))
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
+  if constexpr (kRows != kRowsSum) {  // row tiles before every group
+    int sum = 0;
+    for (int e0 = 0; e0 < p.groups; e0 += kThreads) {
+      const int e = e0 + threadIdx.x;
+      const int n = e < p.groups ? static_cast<int>((p.offsets[e + 1] - p.offsets[e] + kRowTileOf<BN, kRows> - 1) / kRowTileOf<BN, kRows>) : 0;
+      int all = 0;
+      const int before = block_exclusive_scan(n, scratch, &all);
+      if (e < p.groups) first[e] = sum + before;
+      sum += all;
+    }
+    if (threadIdx.x == 0) first[p.groups] = sum;
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      int64_t filled = 0;  // stages whose copies were started
+      bool ok = true;
+      Tile t;
+      for (int64_t i = blockIdx.x; ok && tile_at<BN, kRows>(p, first, i, &t); i += gridDim.x) {
+        for (int k = 0; k < t.steps; ++k) {
+          if (!bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead)) {
+            ok = false;
+            break;
+          }
+          const uint32_t bar = smem_u32(&full_bar[stage]);
+          const uint32_t sa = base + stage * S::kStageBytes, sb = sa + kBytesA;
+          const int at = k * kTileK;
+          bar_expect(bar, S::kStageBytes);
+          if constexpr (kRows == kRowsM) {
+            tma_2d(sa, &map_a, at, t.row0, bar);
+            if constexpr (kBMN) {
+#pragma unroll
+              for (int j = 0; j < BN / 64; ++j) tma_3d(sb + j * 8192, &map_b, t.n0 + 64 * j, at, t.group, bar);
+            } else {
+              tma_3d(sb, &map_b, at, t.n0, t.group, bar);
+            }
+          } else if constexpr (kRows == kRowsN) {
+            if constexpr (kAMN) {
+#pragma unroll
+              for (int j = 0; j < kTileM / 64; ++j) tma_3d(sa + j * 8192, &map_a, t.m0 + 64 * j, at, t.group, bar);
+            } else {
+              tma_3d(sa, &map_a, at, t.m0, t.group, bar);
+            }
+            tma_2d(sb, &map_b, at, t.row0, bar);
+          } else {
+#pragma unroll
+            for (int j = 0; j < kTileM / 64; ++j) tma_2d(sa + j * 8192, &map_a, t.m0 + 64 * j, t.row0 + at, bar);
+#pragma unroll
+            for (int j = 0; j < BN / 64; ++j) tma_2d(sb + j * 8192, &map_b, t.n0 + 64 * j, t.row0 + at, bar);
+          }
+          ++filled;
+          if (++stage == S::kStages) stage = 0, phase ^= 1;
+        }
+      }
+      if (!ok) {  // no copy may be in flight when the CTA leaves
+        const int64_t begin = filled > S::kStages ? filled - S::kStages : 0;
+        for (int64_t f = begin; f < filled; ++f) {
+          const unsigned long long start = now_ns();
+          const uint32_t bar = smem_u32(&full_bar[f % S::kStages]);
+          while (!bar_try(bar, static_cast<uint32_t>(f / S::kStages) & 1) && now_ns() - start < kWaitLimitNs / 10) {
+          }
+        }
+      }
+    }
+  } else if (warp == 1) {
+    // D 32-bit; A and B half (0) or bfloat16 (1)
+    const uint32_t idesc = 1u << 4 | (p.half ? 0u : 1u << 7 | 1u << 10) | static_cast<uint32_t>(kAMN) << 15 |
+                           static_cast<uint32_t>(kBMN) << 16 | static_cast<uint32_t>(BN >> 3) << 17 |
+                           static_cast<uint32_t>(kTileM >> 4) << 24;
+    int stage = 0, acc = 0;
+    uint32_t phase = 0, acc_phase = 0;
+    bool ok = true;
+    Tile t;
+    for (int64_t i = blockIdx.x; ok && tile_at<BN, kRows>(p, first, i, &t); i += gridDim.x) {
+      if (t.steps == 0) continue;
+      bool got = lane != 0 || bar_wait(smem_u32(&acc_empty[acc]), acc_phase ^ 1, &dead);
+      ok = __shfl_sync(0xffffffffu, got, 0);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      for (int k = 0; ok && k < t.steps; ++k) {
+        got = lane != 0 || bar_wait(smem_u32(&full_bar[stage]), phase, &dead);
+        ok = __shfl_sync(0xffffffffu, got, 0);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t sa = base + stage * S::kStageBytes, sb = sa + kBytesA;
+        if constexpr (kRows == kRowsSum) {
+          const int rows = t.rows - k * kTileK;
+          if (rows < kTileK) {  // the rows behind the group's last
+            for (int b = 0; b < S::kStageBytes / 8192; ++b)
+              for (int c = rows * 8 + lane; c < kTileK * 8; c += 32)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + b * 8192 + c * 16), "r"(0) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+          }
+        }
+        if (lane == 0) {
+          const uint64_t da = smem_desc(sa, kAMN), db = smem_desc(sb, kBMN);
+#pragma unroll
+          for (int j = 0; j < kTileK / 16; ++j)
+            mma_f16(tmem + acc * BN, da + j * (kAMN ? 2048 >> 4 : 32 >> 4), db + j * (kBMN ? 2048 >> 4 : 32 >> 4), idesc,
+                    k > 0 || j > 0);
+          mma_commit(smem_u32(&empty_bar[stage]));
+          if (k == t.steps - 1) mma_commit(smem_u32(&acc_full[acc]));
+        }
+        __syncwarp();
+        if (++stage == S::kStages) stage = 0, phase ^= 1;
+      }
+      if (++acc == 2) acc = 0, acc_phase ^= 1;
+    }
+    if (!ok && lane == 0) {  // nor may a product
+      mma_commit(smem_u32(&last_bar));
+      const unsigned long long start = now_ns();
+      while (!bar_try(smem_u32(&last_bar), 0) && now_ns() - start < kWaitLimitNs / 10) {
+      }
+    }
+  } else {
+    const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
+    int acc = 0;
+    uint32_t acc_phase = 0;
+    bool ok = true;
+    Tile t;
+    uint16_t* const result = static_cast<uint16_t*>(p.out);
+    for (int64_t i = blockIdx.x; ok && tile_at<BN, kRows>(p, first, i, &t); i += gridDim.x) {
+      if (t.steps > 0) {
+        const bool got = lane != 0 || bar_wait(smem_u32(&acc_full[acc]), acc_phase, &dead);
+        ok = __shfl_sync(0xffffffffu, got, 0);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      }
+      const int m = quarter * 32 + lane;
+      const uint32_t addr = tmem + acc * BN + (static_cast<uint32_t>(quarter * 32) << 16);
+#pragma unroll 1
+      for (int c = 0; c < BN; c += 16) {
+        float f[16] = {};
+        if constexpr (kRows == kRowsM) {
+          const int left = p.features - t.n0 - c;
+          if (left <= 0) break;
+          if (t.steps > 0) tmem_load16(addr + c, f);
+          if (m < t.rows) store_row16(p, result + (static_cast<int64_t>(t.row0) + m) * p.ldo + t.n0 + c, f, left);
+        } else if constexpr (kRows == kRowsSum) {
+          const int left = p.width - t.n0 - c;
+          if (left <= 0) break;
+          if (t.steps > 0) tmem_load16(addr + c, f);
+          if (t.m0 + m < p.features)
+            store_row16(p, result + t.group * p.group_stride + (static_cast<int64_t>(t.m0) + m) * p.ldo + t.n0 + c, f, left);
+        } else {
+          const int left = t.rows - c;
+          if (left <= 0) break;
+          if (t.steps > 0) tmem_load16(addr + c, f);
+          if (t.m0 + m < p.features) {
+            uint16_t* dst = result + (static_cast<int64_t>(t.row0) + c) * p.ldo + t.m0 + m;
+#pragma unroll
+            for (int j = 0; j < 16; ++j)
+              if (j < left) dst[j * p.ldo] = round16(f[j], p.half);
+          }
+        }
+      }
+      if (t.steps > 0) {
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive(smem_u32(&acc_empty[acc]));
+        if (++acc == 2) acc = 0, acc_phase ^= 1;
+      }
+    }
+  }
+  __syncwarp();
+  __syncthreads();
+  if (threadIdx.x == 0 && dead) atomicOr(p.status, 1);
+  if (warp == 1)
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(static_cast<uint32_t>(S::kAccCols))
+                 : "memory");
+}
+
+// ---------------------------------------------------------------- host
+
+using EncodeFn = CUresult(CUDAAPI*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeFn encoder() {
+  static const EncodeFn fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
+        found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      f = nullptr;
+    }
+    return reinterpret_cast<EncodeFn>(f);
+  }();
+  return fn;
+}
+
+// Rows of 16-bit values; groups > 0: `groups` matrices of `rows` rows.  Boxes of 64 values x box_rows.
+bool encode(CUtensorMap* map, const void* p, bool half, int64_t width, int64_t rows, int64_t ld, int64_t groups,
+            int64_t group_stride, int box_rows) {
+  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(groups)};
+  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2,
+                                 static_cast<cuuint64_t>(groups > 1 ? group_stride : ld * rows) * 2};
+  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1}, step[3] = {1, 1, 1};
+  return encoder()(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, groups > 0 ? 3 : 2,
+                   const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int BN, int kRows, bool kWMN>
+cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const GroupedParams& p, int64_t tiles, int num_sms,
+                   cudaStream_t s) {
+  using S = Shape<BN, kRows>;
+  const auto kernel = grouped_kernel<BN, kRows, kWMN>;
+  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+                                             cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem));
+  if (e != cudaSuccess) return e;
+  kernel<<<static_cast<unsigned>(tiles < num_sms ? tiles : num_sms), kThreads, S::kSmem, s>>>(a, b, p);
+  return cudaGetLastError();
+}
+
+int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
+
+template <bool kWMN>
+cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool* encoded) {
+  const int64_t features = kWMN ? g.K : g.N, depth = kWMN ? g.N : g.K;
+  GroupedParams p{};
+  p.offsets = g.r->offsets;
+  p.groups = static_cast<int>(g.r->ncols);
+  p.nnz = g.r->nnz;
+  p.features = static_cast<int>(features);
+  p.depth = static_cast<int>(depth);
+  p.out = g.out;
+  p.ldo = g.ldo;
+  p.half = g.half;
+  p.vec = reinterpret_cast<uintptr_t>(g.out) % 16 == 0 && g.ldo % 8 == 0;
+  p.status = g.r->status;
+  CUtensorMap x, w;
+  const int64_t met = g.r->nnz < g.r->ncols ? g.r->nnz : g.r->ncols;  // groups that can have rows
+  const double mean = static_cast<double>(g.r->nnz) / static_cast<double>(g.r->ncols);
+  const auto run = [&](auto bn, auto side) {
+    constexpr int BN = decltype(bn)::value, kRows = decltype(side)::value;
+    constexpr int kRowTile = kRowTileOf<BN, kRows>;
+    constexpr int kFeat = kRows == kRowsM ? BN : kTileM;
+    *encoded = encode(&x, g.x, g.half, depth, g.r->nnz, g.ldx, 0, 0, kRowTile) &&
+               encode(&w, g.w, g.half, g.K, g.N, g.ldw, g.r->ncols, g.group_stride, kWMN ? 64 : kFeat);
+    if (!*encoded) return cudaSuccess;
+    const int64_t tiles = (g.r->nnz / kRowTile + met) * up(features, kFeat);
+    return launch<BN, kRows, kWMN>(kRows == kRowsM ? x : w, kRows == kRowsM ? w : x, p, tiles, num_sms, s);
+  };
+  using std::integral_constant;
+  // Few rows an expert: W's features fill the 128 lanes and the rows are the short side.
+  if (mean <= 12) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>());
+  if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>());
+  // Tiles of 256 features where they still give every SM one, else of 128.
+  if ((g.r->nnz / kTileM + met / 2) * up(features, 256) >= num_sms)
+    return run(integral_constant<int, 256>(), integral_constant<int, kRowsM>());
+  return run(integral_constant<int, 128>(), integral_constant<int, kRowsM>());
+}
+
+}  // namespace
+
+ws_status_t launch_grouped(const GroupedRows& g, bool transposed, int num_sms, cudaStream_t s) {
+  if (!encoder()) return routing_fail(WS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+  bool encoded = true;
+  const cudaError_t e = transposed ? launch_rows<true>(g, num_sms, s, &encoded) : launch_rows<false>(g, num_sms, s, &encoded);
+  if (!encoded) return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
+  return e == cudaSuccess ? WS_OK : routing_fail(WS_ERR_CUDA, "grouped product: %s", cudaGetErrorString(e));
+}
+
+ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_t ldgys, int num_sms, cudaStream_t s) {
+  if (!encoder()) return routing_fail(WS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+  GroupedParams p{};
+  p.offsets = g.r->offsets;
+  p.groups = static_cast<int>(g.r->ncols);
+  p.nnz = g.r->nnz;
+  p.features = static_cast<int>(g.N);
+  p.width = static_cast<int>(g.K);
+  p.out = g.out;
+  p.ldo = g.ldo;
+  p.group_stride = g.group_stride;
+  p.half = g.half;
+  p.vec = reinterpret_cast<uintptr_t>(g.out) % 16 == 0 && g.ldo % 8 == 0 && g.group_stride % 8 == 0;
+  p.status = g.r->status;
+  CUtensorMap a, b;
+  if (!encode(&a, gys, g.half, g.N, g.r->nnz, ldgys, 0, 0, 64) || !encode(&b, g.x, g.half, g.K, g.r->nnz, g.ldx, 0, 0, 64))
+    return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
+  const int64_t wide = g.r->ncols * up(g.N, kTileM) * up(g.K, 256);
+  const cudaError_t e = wide >= num_sms
+                            ? launch<256, kRowsSum, false>(a, b, p, wide, num_sms, s)
+                            : launch<128, kRowsSum, false>(a, b, p, g.r->ncols * up(g.N, kTileM) * up(g.K, 128), num_sms, s);
+  return e == cudaSuccess ? WS_OK : routing_fail(WS_ERR_CUDA, "grouped product: %s", cudaGetErrorString(e));
+}
+
+}  // namespace wsk

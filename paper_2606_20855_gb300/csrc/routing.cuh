@@ -83,4 +83,22 @@ void launch_combine(const ws_routing& r, bool weighted, const void* ys, int64_t 
 void launch_combine_backward(const ws_routing& r, const void* gy, int64_t ldgy, const void* ys, int64_t ldys,
                              void* gys, int64_t ldgys, float* gvals, int64_t width, ws_dtype_t dt, cudaStream_t s);
 
+// Products by column of R (grouped.cu).  x: nnz rows in slot order; w: ncols matrices N x K; 16-bit values, addresses
+// and strides multiples of 16 bytes.  out is not aligned further than its type.
+struct GroupedRows {
+  const ws_routing* r;
+  bool half;
+  const void* x;
+  int64_t ldx;
+  const void* w;
+  int64_t ldw, group_stride;
+  void* out;
+  int64_t ldo;
+  int64_t N, K;
+};
+// transposed: out = rows of x (N values) times W, else rows of x (K values) times W^T.
+ws_status_t launch_grouped(const GroupedRows& g, bool transposed, int num_sms, cudaStream_t s);
+// out[e] (N x K, ldo, group_stride) = sum over the rows of e of gys row (N) times x row (K).
+ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_t ldgys, int num_sms, cudaStream_t s);
+
 }  // namespace wsk

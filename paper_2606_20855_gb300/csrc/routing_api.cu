@@ -38,7 +38,7 @@ ws_status_t check(const ws_routing* r) {
                         static_cast<long long>(r->nnz), kRouteMaxCols, INT32_MAX);
   if (r->nnz > 0 && (r->nrows == 0 || r->ncols == 0))
     return routing_fail(WS_ERR_SHAPE, "entries in a routing matrix without rows or columns");
-  if (!r->rowptr || !r->offsets || (r->nnz > 0 && (!r->colidx || !r->rows || !r->entries || !r->slots)))
+  if (!r->rowptr || !r->offsets || !r->status || (r->nnz > 0 && (!r->colidx || !r->rows || !r->entries || !r->slots)))
     return routing_fail(WS_ERR_INVALID_ARG, "NULL array in a routing matrix");
   return WS_OK;
 }
@@ -61,6 +61,30 @@ ws_status_t check_rows(const ws_routing* r, int64_t width, ws_dtype_t dt, std::i
     if (d.ld < width && d.rows > 1) return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
     if (reinterpret_cast<uintptr_t>(d.p) % size) return routing_fail(WS_ERR_INVALID_ARG, "misaligned dense matrix");
   }
+  return WS_OK;
+}
+
+// A 16-bit matrix that the copy engine reads, or (read false) a result.
+struct Operand {
+  const void* p;
+  int64_t rows, width, ld;
+  bool read;
+};
+
+ws_status_t check_product(const ws_routing* r, int64_t N, int64_t K, ws_dtype_t dt, int64_t group_stride,
+                          std::initializer_list<Operand> all) {
+  if (const ws_status_t st = check(r)) return st;
+  if (dt != WS_BF16 && dt != WS_F16) return routing_fail(WS_ERR_DTYPE, "products are of bfloat16 or half matrices");
+  if (N < 0 || K < 0) return routing_fail(WS_ERR_INVALID_ARG, "negative size");
+  if (N > kMaxWidth || K > kMaxWidth) return routing_fail(WS_ERR_OVERFLOW, "rows of more than 2^24 values");
+  for (const Operand& d : all) {
+    if (d.rows == 0 || d.width == 0) continue;
+    if (!d.p || (d.rows > 1 && d.ld < d.width)) return routing_fail(WS_ERR_INVALID_ARG, "NULL matrix, or row stride smaller than the row");
+    if (reinterpret_cast<uintptr_t>(d.p) % (d.read ? 16 : 2) || (d.read && (d.ld % 8 || d.ld >= int64_t{1} << 36)))
+      return routing_fail(WS_ERR_INVALID_ARG, "operands of a product start and have row strides at multiples of 16 bytes");
+  }
+  if (r->ncols > 1 && (group_stride % 8 || group_stride < 0 || group_stride >= int64_t{1} << 36))
+    return routing_fail(WS_ERR_INVALID_ARG, "matrices of a product are a multiple of 16 bytes apart");
   return WS_OK;
 }
 
@@ -114,6 +138,7 @@ int64_t ws_routing_scratch(int64_t nrows, int64_t ncols) {
 
 ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
   if (const ws_status_t st = check(r)) return st;
+  cudaMemsetAsync(r->status, 0, sizeof(int32_t), cuda_stream(stream));
   if (r->nnz == 0) {
     cudaMemsetAsync(r->offsets, 0, static_cast<size_t>(r->ncols + 1) * sizeof(int64_t), cuda_stream(stream));
     return launched("ws_routing_build");
@@ -166,6 +191,49 @@ ws_status_t ws_routing_combine_backward(const ws_routing* r, const void* gy, int
   }
   launch_combine_backward(*r, gy, ldgy, ys, ldys, gys, ldgys, gvals, width, dtype, cuda_stream(stream));
   return launched("ws_routing_combine_backward");
+}
+
+ws_status_t ws_routing_matmul(const ws_routing* r, const void* xs, int64_t ldxs, const void* W, int64_t ldw,
+                              int64_t stride, int64_t N, int64_t K, void* ys, int64_t ldys, ws_dtype_t dtype,
+                              ws_stream_t stream) {
+  if (const ws_status_t st = check_product(r, N, K, dtype, stride, {{xs, r ? r->nnz : 0, K, ldxs, true}, {W, N, K, ldw, true},
+                                                                    {ys, r ? r->nnz : 0, N, ldys, false}}))
+    return st;
+  if (r->nnz == 0 || N == 0) return WS_OK;
+  if (K == 0) return routing_fail(WS_ERR_SHAPE, "a product over no values");
+  int sms = 0;
+  if (const ws_status_t st = sm_count(&sms)) return st;
+  return launch_grouped({r, dtype == WS_F16, xs, ldxs, W, ldw, stride, ys, ldys, N, K}, false, sms, cuda_stream(stream));
+}
+
+ws_status_t ws_routing_matmul_rows(const ws_routing* r, const void* gys, int64_t ldgys, const void* W, int64_t ldw,
+                                   int64_t stride, int64_t N, int64_t K, void* gxs, int64_t ldgxs, ws_dtype_t dtype,
+                                   ws_stream_t stream) {
+  if (const ws_status_t st = check_product(r, N, K, dtype, stride, {{gys, r ? r->nnz : 0, N, ldgys, true}, {W, N, K, ldw, true},
+                                                                    {gxs, r ? r->nnz : 0, K, ldgxs, false}}))
+    return st;
+  if (r->nnz == 0 || K == 0) return WS_OK;
+  if (N == 0) return routing_fail(WS_ERR_SHAPE, "a product over no values");
+  int sms = 0;
+  if (const ws_status_t st = sm_count(&sms)) return st;
+  return launch_grouped({r, dtype == WS_F16, gys, ldgys, W, ldw, stride, gxs, ldgxs, N, K}, true, sms, cuda_stream(stream));
+}
+
+ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int64_t ldgys, const void* xs,
+                                      int64_t ldxs, int64_t N, int64_t K, void* gW, int64_t ldgw, int64_t stride,
+                                      ws_dtype_t dtype, ws_stream_t stream) {
+  if (const ws_status_t st = check_product(r, N, K, dtype, 0, {{gys, r ? r->nnz : 0, N, ldgys, true}, {xs, r ? r->nnz : 0, K, ldxs, true},
+                                                               {gW, N, K, ldgw, false}}))
+    return st;
+  if (r->ncols == 0 || N == 0 || K == 0) return WS_OK;
+  if (r->nnz == 0) {
+    if (ldgw != K || stride != N * K) return routing_fail(WS_ERR_INVALID_ARG, "gradients without rows are written to contiguous matrices only");
+    cudaMemsetAsync(gW, 0, static_cast<size_t>(r->ncols) * N * K * 2, cuda_stream(stream));
+    return launched("ws_routing_matmul_weights");
+  }
+  int sms = 0;
+  if (const ws_status_t st = sm_count(&sms)) return st;
+  return launch_grouped_weights({r, dtype == WS_F16, xs, ldxs, nullptr, 0, stride, gW, ldgw, N, K}, gys, ldgys, sms, cuda_stream(stream));
 }
 
 }  // extern "C"

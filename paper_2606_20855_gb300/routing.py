@@ -8,7 +8,8 @@ expert.  A layer of experts is
     xs = plan.dispatch(x)              # their rows in that order
     y = plan.combine(f(xs))            # the experts' rows summed back with R's values
 
-and its gradients are ``combine_backward``, ``dispatch_backward`` and ``topk_route_backward``.  All calls queue work on
+where the experts' matrices may be ``plan.matmul(xs, W)``; the gradients are ``combine_backward``,
+``dispatch_backward``, ``matmul_backward`` and ``topk_route_backward``.  All calls queue work on
 the current stream, or on ``stream``, and return without waiting; none reads anything back.
 """
 from __future__ import annotations
@@ -59,6 +60,21 @@ def _matrix(t: torch.Tensor, name: str, rows: int | None, like: torch.Tensor | N
     if (n > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < n):
         return t.contiguous()
     return t
+
+
+def _operand(t: torch.Tensor) -> torch.Tensor:
+    """A matrix (or a stack of matrices) of 16-bit values whose rows start at multiples of 16 bytes: t itself, or a
+    copy with longer rows where t's do not."""
+    n = t.shape[-1]
+    if t.data_ptr() % 16 == 0 and (n <= 1 or t.stride(-1) == 1) and \
+            all(t.shape[i] == 1 or (t.stride(i) % 8 == 0 and t.stride(i) >= n) for i in range(t.dim() - 1)):
+        return t
+    out = torch.empty((*t.shape[:-1], (n + 7) // 8 * 8), dtype=t.dtype, device=t.device)[..., :n]
+    return out.copy_(t)
+
+
+def _ld8(t: torch.Tensor) -> int:
+    return t.stride(-2) if t.shape[-2] > 1 else (t.shape[-1] + 7) // 8 * 8
 
 
 def _ld(t: torch.Tensor) -> int:
@@ -126,13 +142,14 @@ class Routing:
             if validate:
                 _abi.ws_csr_destroy(R._handle(True, raw))
             scratch = _abi.ws_routing_scratch(R.nrows, E)
-            # offsets, then rows, entries and slots, then the scratch
-            words = 2 * (E + 1) + 3 * nnz
+            # offsets, then rows, entries and slots, the status word, the scratch
+            words = 2 * (E + 1) + 3 * nnz + 1
             self._buf = torch.empty(words + scratch // 4, dtype=torch.int32, device=self.device)
             at = self._buf.data_ptr()
             rows = at + 8 * (E + 1)
             self._c = _abi.WsRouting(R.nrows, E, nnz, R.rowptr.data_ptr(), R.colidx.data_ptr() or None,
-                                     R.vals.data_ptr() or None, at, rows, rows + 4 * nnz, rows + 8 * nnz)
+                                     R.vals.data_ptr() or None, at, rows, rows + 4 * nnz, rows + 8 * nnz,
+                                     rows + 12 * nnz)
             self._r = ctypes.byref(self._c)
             self._stream = raw
             _abi.ws_routing_build(self._r, at + 4 * words, scratch, raw)
@@ -210,3 +227,54 @@ class Routing:
             _abi.ws_routing_combine_backward(self._r, g.data_ptr(), _ld(g), ys.data_ptr(), _ld(ys), out.data_ptr(), H,
                                              gvals.data_ptr(), H, dt, self._queue())
         return out, gvals
+
+    def _experts(self, W: torch.Tensor, like: torch.Tensor):
+        if W.dim() != 3 or W.shape[0] != self.R.ncols:
+            raise ValueError(f"W must be {self.R.ncols} matrices, got {tuple(W.shape)}")
+        if W.dtype != like.dtype or W.device != like.device:
+            raise TypeError("W must have the rows' type and device")
+        W = _operand(W)
+        return W, W.stride(0) if W.shape[0] > 1 else W.shape[1] * _ld8(W)
+
+    def matmul(self, xs: torch.Tensor, W: torch.Tensor, stream=None) -> torch.Tensor:
+        """ys[s] = W[e] xs[s] for the rows s of every column e: xs nnz x K in slot order, W E x N x K, bfloat16 or
+        float16; products and sums in 32 bits, rounded once.  Rows behind the placed entries are left unwritten."""
+        dt = _dtype(xs, "xs")
+        with _on(stream, xs, W):
+            xs = _operand(_matrix(xs, "xs", self.nnz))
+            W, apart = self._experts(W, xs)
+            (_, N, K), Z = W.shape, self.nnz
+            if xs.shape[1] != K:
+                raise ValueError(f"rows of {xs.shape[1]} values do not fit matrices of {K} columns")
+            out = torch.empty((Z, N), dtype=xs.dtype, device=xs.device)
+            _abi.ws_routing_matmul(self._r, xs.data_ptr(), _ld8(xs), W.data_ptr(), _ld8(W), apart, N, K,
+                                   out.data_ptr(), N, dt, self._queue())
+        return out
+
+    def matmul_backward(self, grad_ys: torch.Tensor, xs: torch.Tensor, W: torch.Tensor, stream=None):
+        """Gradients of xs (W[e]^T grad_ys[s]) and of W (sum over the rows of e of grad_ys[s] xs[s]^T; zero for a
+        column without entries), in their types."""
+        dt = _dtype(xs, "xs")
+        with _on(stream, grad_ys, xs, W):
+            xs = _operand(_matrix(xs, "xs", self.nnz))
+            g = _operand(_matrix(grad_ys, "grad_ys", self.nnz, xs))
+            W, apart = self._experts(W, xs)
+            (E, N, K), Z, raw = W.shape, self.nnz, self._queue()
+            if xs.shape[1] != K or g.shape[1] != N:
+                raise ValueError(f"rows of {xs.shape[1]} and {g.shape[1]} values do not fit matrices {N} x {K}")
+            gxs = torch.empty((Z, K), dtype=xs.dtype, device=xs.device)
+            gW = torch.empty((E, N, K), dtype=xs.dtype, device=xs.device)
+            _abi.ws_routing_matmul_rows(self._r, g.data_ptr(), _ld8(g), W.data_ptr(), _ld8(W), apart, N, K,
+                                        gxs.data_ptr(), K, dt, raw)
+            _abi.ws_routing_matmul_weights(self._r, g.data_ptr(), _ld8(g), xs.data_ptr(), _ld8(xs), N, K,
+                                           gW.data_ptr(), K, N * K, dt, raw)
+        return gxs, gW
+
+    def wait(self, stream=None) -> None:
+        """Waits for the stream and raises if a product's kernel gave up a wait since the plan was built."""
+        with _on(stream):
+            self._queue()
+            torch.cuda.current_stream(self.device).synchronize()
+        at = 2 * (self.R.ncols + 1) + 3 * self.nnz
+        if int(self._buf[at]):
+            raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
