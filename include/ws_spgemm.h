@@ -454,6 +454,40 @@ ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int6
                                       int64_t ldxs, int64_t N, int64_t K, void* gW, int64_t ldgw, int64_t stride,
                                       ws_dtype_t dtype, ws_stream_t stream);
 
+/*
+ * ws_adapters -- low-rank adapters of many requests beside a projection they
+ * share: y[t] = base[t] + sum over row t of S of value * B[a] (A[a] x[t]).
+ * S is an nrows x ncols CSR matrix, tokens x adapters (columns strictly
+ * increasing within a row; rows may be empty; entries whose column is out of
+ * range take no part).  bfloat16 or half; inner products A[a] x[t] are summed in
+ * 32 bits and kept as pairs of 16-bit values (for half up to 65504), the result
+ * is summed in 32 bits and rounded once.  x and A start and have strides at
+ * multiples of 16 bytes.  base may be NULL (zero) and may be y itself.
+ * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned.  Queued on
+ * `stream`; nothing is allocated.
+ */
+typedef struct ws_adapters_call {
+  int64_t nrows, ncols, nnz;
+  const int64_t* rowptr;
+  const int32_t* colidx;
+  const float* vals;
+  int64_t K, r, N; /* A[a]: r x K, B[a]: N x r */
+  const void* x;
+  int64_t ldx;
+  const void* A;
+  int64_t lda, strideA;
+  const void* B;
+  int64_t ldb, strideB;
+  const void* base;
+  int64_t ldbase;
+  void* y;
+  int64_t ldy;
+  ws_dtype_t dtype;
+} ws_adapters_call;
+
+int64_t ws_adapters_scratch(int64_t nnz, int64_t r);
+ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scratch_bytes, ws_stream_t stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -10,7 +10,7 @@ this package loads nothing; the library is loaded on first use.
 """
 
 __all__ = ["DeviceCSR", "SpGEMM", "SpGEMMOuter", "spgemm", "spgemm_outer", "submatrix", "Ewise", "ewise", "SpMSpV", "spmspv"]
-_ROUTING = ["Routing", "topk_route", "topk_route_backward"]
+_ROUTING = ["Routing", "topk_route", "topk_route_backward", "adapters"]
 __all__ += _ROUTING
 
 

@@ -63,6 +63,8 @@ SIGNATURES = [
     ("ws_routing_matmul", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p]),
     ("ws_routing_matmul_rows", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p]),
     ("ws_routing_matmul_weights", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _i64, _i32, _p]),
+    ("ws_adapters_scratch", _i64, [_i64, _i64]),
+    ("ws_adapters", _i32, [_p, _p, _i64, _p]),
 ]
 
 
@@ -70,6 +72,14 @@ class WsRouting(ctypes.Structure):
     """struct ws_routing (device pointers as integers)."""
     _fields_ = [("nrows", _i64), ("ncols", _i64), ("nnz", _i64), ("rowptr", _p), ("colidx", _p), ("vals", _p),
                 ("offsets", _p), ("rows", _p), ("entries", _p), ("slots", _p), ("status", _p)]
+
+class WsAdaptersCall(ctypes.Structure):
+    """struct ws_adapters_call (device pointers as integers)."""
+    _fields_ = [("nrows", _i64), ("ncols", _i64), ("nnz", _i64), ("rowptr", _p), ("colidx", _p), ("vals", _p),
+                ("K", _i64), ("r", _i64), ("N", _i64), ("x", _p), ("ldx", _i64), ("A", _p), ("lda", _i64),
+                ("strideA", _i64), ("B", _p), ("ldb", _i64), ("strideB", _i64), ("base", _p), ("ldbase", _i64),
+                ("y", _p), ("ldy", _i64), ("dtype", _i32)]
+
 
 EWISE_OPS = {"add": 1, "mul": 2}  # ws_ewise_op_t
 
@@ -281,3 +291,11 @@ def ws_routing_matmul_weights(r, gys: int, ldgys: int, xs: int, ldxs: int, N: in
                               stride: int, dtype: int, stream: int) -> None:
     _check("ws_routing_matmul_weights", load().ws_routing_matmul_weights(r, gys, ldgys, xs, ldxs, N, K, gW, ldgw,
                                                                          stride, dtype, stream))
+
+
+def ws_adapters_scratch(nnz: int, r: int) -> int:
+    return load().ws_adapters_scratch(nnz, r)
+
+
+def ws_adapters(call: WsAdaptersCall, scratch: int, scratch_bytes: int, stream: int) -> None:
+    _check("ws_adapters", load().ws_adapters(ctypes.byref(call), scratch, scratch_bytes, stream))

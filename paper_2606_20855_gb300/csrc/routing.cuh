@@ -101,4 +101,8 @@ ws_status_t launch_grouped(const GroupedRows& g, bool transposed, int num_sms, c
 // out[e] (N x K, ldo, group_stride) = sum over the rows of e of gys row (N) times x row (K).
 ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_t ldgys, int num_sms, cudaStream_t s);
 
+// Ranks kept for an entry of S: h is padded with zeros.
+inline int adapters_rank(int64_t r) { return static_cast<int>((r + 15) / 16 * 16); }
+void launch_adapters(const ws_adapters_call& c, void* scratch, cudaStream_t s);
+
 }  // namespace wsk

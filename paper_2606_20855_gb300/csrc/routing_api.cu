@@ -236,4 +236,40 @@ ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int6
   return launch_grouped_weights({r, dtype == WS_F16, xs, ldxs, nullptr, 0, stride, gW, ldgw, N, K}, gys, ldgys, sms, cuda_stream(stream));
 }
 
+int64_t ws_adapters_scratch(int64_t nnz, int64_t r) {
+  return nnz <= 0 || r <= 0 ? 0 : nnz * adapters_rank(r) * static_cast<int64_t>(sizeof(float));
+}
+
+ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
+  if (!call) return routing_fail(WS_ERR_INVALID_ARG, "NULL arguments");
+  const ws_adapters_call& c = *call;
+  if (c.nrows < 0 || c.ncols < 0 || c.nnz < 0 || c.K < 0 || c.r < 0 || c.N < 0)
+    return routing_fail(WS_ERR_INVALID_ARG, "negative size");
+  if (c.dtype != WS_BF16 && c.dtype != WS_F16) return routing_fail(WS_ERR_DTYPE, "adapters are bfloat16 or half");
+  if (c.nrows > INT32_MAX || c.ncols > INT32_MAX || c.nnz > INT32_MAX || c.K > kMaxWidth || c.N > kMaxWidth || c.r > 4096)
+    return routing_fail(WS_ERR_OVERFLOW, "at most %d rows, columns and entries, rows of 2^24 values, rank 4096", INT32_MAX);
+  if (c.nnz > 0 && (c.nrows == 0 || c.ncols == 0)) return routing_fail(WS_ERR_SHAPE, "entries in a matrix without rows or columns");
+  const bool used = c.nrows > 0 && c.N > 0, inner = used && c.nnz > 0 && c.r > 0 && c.K > 0;
+  if (!c.rowptr || (c.nnz > 0 && (!c.colidx || !c.vals)) || (used && !c.y) || (inner && (!c.x || !c.A || !c.B || !scratch)))
+    return routing_fail(WS_ERR_INVALID_ARG, "NULL pointer");
+  if (used && c.nrows > 1 && (c.ldy < c.N || (c.base && c.ldbase < c.N)))
+    return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
+  if (inner) {
+    const auto off16 = [](const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 != 0 || ld % 8 != 0; };
+    if (off16(c.x, c.nrows > 1 ? c.ldx : 0) || off16(c.A, c.r > 1 ? c.lda : 0) || (c.ncols > 1 && c.strideA % 8))
+      return routing_fail(WS_ERR_INVALID_ARG, "x and A start and have strides at multiples of 16 bytes");
+    if ((c.nrows > 1 && c.ldx < c.K) || (c.r > 1 && c.lda < c.K) || (c.N > 1 && c.ldb < c.r) || c.strideA < 0 || c.strideB < 0)
+      return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
+    if (scratch_bytes < ws_adapters_scratch(c.nnz, c.r) || reinterpret_cast<uintptr_t>(scratch) % 16)
+      return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_adapters_scratch, or misaligned");
+  }
+  if ((reinterpret_cast<uintptr_t>(c.y) | reinterpret_cast<uintptr_t>(c.base) | reinterpret_cast<uintptr_t>(c.B)) % 2)
+    return routing_fail(WS_ERR_INVALID_ARG, "misaligned matrix");
+  if (!used) return WS_OK;
+  ws_adapters_call run = c;
+  if (!inner) run.nnz = 0;  // nothing to add: entry ranges are cut to [0, 0]
+  launch_adapters(run, scratch, cuda_stream(stream));
+  return launched("ws_adapters");
+}
+
 }  // extern "C"

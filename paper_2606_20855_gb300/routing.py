@@ -278,3 +278,60 @@ class Routing:
         at = 2 * (self.R.ncols + 1) + 3 * self.nnz
         if int(self._buf[at]):
             raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
+
+
+def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, base: torch.Tensor | None = None,
+             out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """y[t] = base[t] + sum over row t of S of value * B[a] (A[a] x[t]): low-rank adapters of many requests beside the
+    projection they share (``base``, its result; None for zero).
+
+    x: T x K, A: L x r x K, B: L x N x r, base: T x N, bfloat16 or float16; S: T x L in CSR, float32 values, rows empty
+    for tokens without an adapter.  ``out`` may be ``base``: the adapters' part is then added in place.
+    """
+    dt = _dtype(x, "x")
+    if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+        raise ValueError(f"A must be L x r x K and B L x N x r, got {tuple(A.shape)} and {tuple(B.shape)}")
+    (L, r, K), N, T = A.shape, B.shape[1], S.nrows
+    if A.dtype != x.dtype or B.dtype != x.dtype or A.device != x.device or B.device != x.device:
+        raise TypeError("x, A and B must have one type and device")
+    for t, d in ((S.rowptr, torch.int64), (S.colidx, torch.int32), (S.vals, torch.float32)):
+        if t.dtype != d or t.device != x.device or not t.is_contiguous():
+            raise TypeError("S must hold contiguous int64/int32/float32 tensors on x's device")
+    nnz = S.colidx.numel()
+    if S.ncols != L or S.rowptr.numel() != T + 1 or S.vals.numel() != nnz:
+        raise ValueError(f"S must be {x.shape[0]} x {L} in CSR")
+    with _on(stream, x, A, B, S.rowptr, S.colidx, S.vals, *(() if base is None else (base,))):
+        x = _operand(_matrix(x, "x", T))
+        if x.shape[1] != K:
+            raise ValueError(f"rows of {x.shape[1]} values do not fit adapters of {K}")
+        A = _operand(A)
+        if (r > 1 and B.stride(2) != 1) or (N > 1 and B.stride(1) < r):
+            B = B.contiguous()
+        if base is not None:
+            base = _matrix(base, "base", T, x)
+            if base.shape[1] != N:
+                raise ValueError(f"base must be {T} x {N}")
+        if out is None:
+            out = torch.empty((T, N), dtype=x.dtype, device=x.device)
+        elif _matrix(out, "out", T, x) is not out or out.shape[1] != N:
+            raise ValueError(f"out must be {T} x {N} with unit stride within its rows")
+        elif base is not None and _overlap(out, base) and (out.data_ptr(), _ld(out)) != (base.data_ptr(), _ld(base)):
+            raise ValueError("out must be base itself or lie apart from it")
+        need = _abi.ws_adapters_scratch(nnz, r)
+        scratch = torch.empty(need, dtype=torch.uint8, device=x.device)
+        call = _abi.WsAdaptersCall(T, L, nnz, S.rowptr.data_ptr(), S.colidx.data_ptr(), S.vals.data_ptr(), K, r, N,
+                                   x.data_ptr(), _ld8(x), A.data_ptr(), _ld8(A), A.stride(0), B.data_ptr(),
+                                   B.stride(1), B.stride(0), 0 if base is None else base.data_ptr(),
+                                   0 if base is None else _ld(base), out.data_ptr(), _ld(out), dt)
+        _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(x.device))
+    return out
+
+
+def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
+    """Whether the address ranges of two matrices meet."""
+    def span(t):
+        if t.numel() == 0:
+            return t.data_ptr(), t.data_ptr()
+        return t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size()
+    (a0, a1), (b0, b1) = span(a), span(b)
+    return a0 < b1 and b0 < a1
