@@ -34,16 +34,6 @@ constexpr int kAdThreads = 256;
 constexpr int kAdWarps = kAdThreads / 32;
 constexpr int kTileTok = 32;
 
-template <bool half>
-__device__ __forceinline__ float value16(uint16_t u) {
-  if constexpr (half) return __half2float(__ushort_as_half(u));
-  else return __uint_as_float(static_cast<uint32_t>(u) << 16);
-}
-template <bool half>
-__device__ __forceinline__ uint16_t bits16(float f) {
-  if constexpr (half) return __half_as_ushort(__float2half_rn(f));
-  else return __bfloat16_as_ushort(__float2bfloat16_rn(f));
-}
 // h as {roundings, remainders} of two neighbouring ranks.
 template <bool half>
 __device__ __forceinline__ uint2 split_pair(float a, float b) {
@@ -55,21 +45,6 @@ __device__ __forceinline__ uint2 split_pair(float a, float b) {
   return make_uint2(ha | static_cast<uint32_t>(hb) << 16, la | static_cast<uint32_t>(lb) << 16);
 }
 
-template <bool half>
-__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
-                                      uint32_t b1) {
-  if constexpr (half)
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-  else
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
 // d += (roundings + remainders of h, rows a and b) times v.
 template <bool half>
 __device__ __forceinline__ void mma_pair(float (&d)[4], const uint4& a, const uint4& b, const uint2& v) {
@@ -77,15 +52,6 @@ __device__ __forceinline__ void mma_pair(float (&d)[4], const uint4& a, const ui
   mma16<half>(d, a.y, b.y, a.w, b.w, v.x, v.y);
 }
 
-// Values k .. k + 7 of a row of K (16-byte aligned), zero past its end.
-__device__ __forceinline__ uint4 load8(const uint16_t* row, int k, int K) {
-  if (k + 8 <= K) return *reinterpret_cast<const uint4*>(row + k);
-  uint32_t w[4] = {};
-#pragma unroll
-  for (int i = 0; i < 8; ++i)
-    if (k + i < K) w[i >> 1] |= static_cast<uint32_t>(row[k + i]) << (16 * (i & 1));
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
 // Ranks k .. k + 3 of a row of B, zero past its end.
 __device__ __forceinline__ uint2 load4(const uint16_t* row, int k, int r, bool vec) {
   if (vec) return k < r ? *reinterpret_cast<const uint2*>(row + k) : make_uint2(0, 0);
@@ -128,8 +94,9 @@ struct Walk {
 // ---------------------------------------------------------------- many tokens
 
 // h of a tile of 32 tokens, 8 NR ranks from 8 NR blockIdx.y on; the warps take every eighth step of 32 values.
+// Rows that are not there (tokens past the last, ranks past r) repeat one that is; what comes of them is not used.
 template <bool half, int NR>
-__global__ void __launch_bounds__(kAdThreads) shrink_tile_kernel(const ws_adapters_call c, uint2* __restrict__ h, int rpad) {
+__global__ void __launch_bounds__(kAdThreads, NR <= 4 ? 2 : 1) shrink_tile_kernel(const ws_adapters_call c, uint2* __restrict__ h, int rpad) {
   extern __shared__ float red[];  // [warps][32][8 NR]
   __shared__ int entry[kTileTok];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
@@ -138,32 +105,21 @@ __global__ void __launch_bounds__(kAdThreads) shrink_tile_kernel(const ws_adapte
   const int K = static_cast<int>(c.K), r = static_cast<int>(c.r);
   Walk w;
   w.start(c, t0 + lane);
-  const uint16_t* x = static_cast<const uint16_t*>(c.x);
   const uint16_t* xrow[4];
-  bool xon[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t t = t0 + 8 * i + g;
-    xon[i] = t < c.nrows;
-    xrow[i] = x + (xon[i] ? t : 0) * c.ldx;
-  }
+  for (int i = 0; i < 4; ++i)
+    xrow[i] = static_cast<const uint16_t*>(c.x) + min(t0 + 8 * i + g, c.nrows - 1) * c.ldx;
   for (;;) {
     const int a = __reduce_min_sync(0xffffffffu, w.col);
     if (a == INT_MAX) break;
     const bool mine = w.col == a;
-    const uint32_t mask = __ballot_sync(0xffffffffu, mine);
     if (warp == 0) entry[lane] = mine ? w.at : -1;
     const uint16_t* A = static_cast<const uint16_t*>(c.A) + a * c.strideA;
+    const uint16_t* arow[NR];
+#pragma unroll
+    for (int j = 0; j < NR; ++j) arow[j] = A + min(r0 + 8 * j + g, r - 1) * c.lda;
     float acc[2][NR][4] = {};
-#pragma unroll 2
-    for (int k = 32 * warp + 8 * q; k - 8 * q < K; k += 32 * kAdWarps) {
-      uint4 xv[4], av[NR];
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        xv[i] = xon[i] && (mask >> (8 * i) & 0xffu) ? load8(xrow[i], k, K) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-      for (int j = 0; j < NR; ++j)
-        av[j] = r0 + 8 * j + g < r ? load8(A + (r0 + 8 * j + g) * c.lda, k, K) : make_uint4(0, 0, 0, 0);
+    const auto step = [&](const uint4(&xv)[4], const uint4(&av)[NR]) {
 #pragma unroll
       for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -171,6 +127,29 @@ __global__ void __launch_bounds__(kAdThreads) shrink_tile_kernel(const ws_adapte
           mma16<half>(acc[m][j], xv[2 * m].x, xv[2 * m + 1].x, xv[2 * m].y, xv[2 * m + 1].y, av[j].x, av[j].y);
           mma16<half>(acc[m][j], xv[2 * m].z, xv[2 * m + 1].z, xv[2 * m].w, xv[2 * m + 1].w, av[j].z, av[j].w);
         }
+    };
+    int k = 32 * warp + 8 * q;
+    constexpr int U = NR <= 4 ? 2 : 1;  // steps whose loads are in flight together
+    for (; k - 8 * q + 32 * kAdWarps * (U - 1) + 32 <= K; k += 32 * kAdWarps * U) {
+      uint4 xv[U][4], av[U][NR];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) xv[u][i] = *reinterpret_cast<const uint4*>(xrow[i] + k + 32 * kAdWarps * u);
+#pragma unroll
+        for (int j = 0; j < NR; ++j) av[u][j] = *reinterpret_cast<const uint4*>(arow[j] + k + 32 * kAdWarps * u);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) step(xv[u], av[u]);
+    }
+#pragma unroll 1
+    for (; k - 8 * q < K; k += 32 * kAdWarps) {
+      uint4 xv[4], av[NR];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) xv[i] = load8(xrow[i], k, K);
+#pragma unroll
+      for (int j = 0; j < NR; ++j) av[j] = load8(arow[j], k, K);
+      step(xv, av);
     }
 #pragma unroll
     for (int m = 0; m < 2; ++m)
@@ -192,7 +171,8 @@ __global__ void __launch_bounds__(kAdThreads) shrink_tile_kernel(const ws_adapte
         s1 += f.y;
       }
       const float v = c.vals[entry[tok]];
-      h[static_cast<int64_t>(entry[tok]) * (rpad / 2) + r0 / 2 + pair] = split_pair<half>(v * s0, v * s1);
+      h[static_cast<int64_t>(entry[tok]) * (rpad / 2) + r0 / 2 + pair] =
+          split_pair<half>(r0 + 2 * pair < r ? v * s0 : 0.0f, r0 + 2 * pair + 1 < r ? v * s1 : 0.0f);
     }
     __syncthreads();
     if (mine) w.next(c);
@@ -200,42 +180,47 @@ __global__ void __launch_bounds__(kAdThreads) shrink_tile_kernel(const ws_adapte
 }
 
 // y of 32 tokens: a warp takes 64 values of each; in tile j of eight, column g of the instruction is value
-// 16 (g / 2) + 2 j + g % 2, so that a lane ends up with 16 neighbouring values of its rows.
-template <bool half>
-__global__ void __launch_bounds__(kAdThreads)
-    expand_tile_kernel(const ws_adapters_call c, const uint2* __restrict__ h, int rpad, bool vecB, bool vecY) {
+// 32 (j / 4) + 8 (g / 2) + 2 (j % 4) + g % 2, so that a lane ends up with two times eight neighbouring values of a row.
+template <bool half, bool vec>
+__global__ void __launch_bounds__(kAdThreads, 2)
+    expand_tile_kernel(const ws_adapters_call c, const uint2* __restrict__ h, int rpad, bool vecB) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTileTok;
   const int N = static_cast<int>(c.N), r = static_cast<int>(c.r);
   const int n0 = (blockIdx.y * kAdWarps + warp) * 64;
   if (n0 >= N) return;
-  const int nq = n0 + 16 * q;  // the lane's values
-  float acc[2][8][4];
   const uint16_t* base = static_cast<const uint16_t*>(c.base);
+  uint4 bv16[4][2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {  // rows g, g + 8, g + 16, g + 24
     const int64_t t = t0 + 8 * i + g;
-    uint32_t v[8] = {};
-    if (base && t < c.nrows) {
-      const uint16_t* src = base + t * c.ldbase + nq;
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        if (vecY && nq + 8 * s + 8 <= N) {
-          const uint4 u = *reinterpret_cast<const uint4*>(src + 8 * s);
-          v[4 * s] = u.x, v[4 * s + 1] = u.y, v[4 * s + 2] = u.z, v[4 * s + 3] = u.w;
-        } else {
+    for (int s = 0; s < 2; ++s) {
+      const int n = n0 + 32 * s + 8 * q;
+      if (vec) {  // rows start at multiples of 16 bytes and N is a multiple of 8
+        bv16[i][s] = base && t < c.nrows && n < N ? *reinterpret_cast<const uint4*>(base + t * c.ldbase + n) : make_uint4(0, 0, 0, 0);
+      } else {
+        uint32_t v[4] = {};
+        if (base && t < c.nrows)
 #pragma unroll
           for (int e = 0; e < 8; ++e)
-            if (nq + 8 * s + e < N) v[4 * s + (e >> 1)] |= static_cast<uint32_t>(src[8 * s + e]) << (16 * (e & 1));
-        }
+            if (n + e < N) v[e >> 1] |= static_cast<uint32_t>(base[t * c.ldbase + n + e]) << (16 * (e & 1));
+        bv16[i][s] = make_uint4(v[0], v[1], v[2], v[3]);
       }
     }
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      acc[i >> 1][j][2 * (i & 1)] = value16<half>(static_cast<uint16_t>(v[j]));
-      acc[i >> 1][j][2 * (i & 1) + 1] = value16<half>(static_cast<uint16_t>(v[j] >> 16));
-    }
   }
+  float acc[2][8][4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      const uint32_t v[4] = {bv16[i][s].x, bv16[i][s].y, bv16[i][s].z, bv16[i][s].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        acc[i >> 1][4 * s + j][2 * (i & 1)] = value16<half>(static_cast<uint16_t>(v[j]));
+        acc[i >> 1][4 * s + j][2 * (i & 1) + 1] = value16<half>(static_cast<uint16_t>(v[j] >> 16));
+      }
+    }
   Walk w;
   w.start(c, t0 + lane);
   for (;;) {
@@ -253,9 +238,9 @@ __global__ void __launch_bounds__(kAdThreads)
         hv[i] = entry[i] >= 0 ? *reinterpret_cast<const uint4*>(h + static_cast<int64_t>(entry[i]) * (rpad / 2) + k / 2 + 2 * q)
                               : make_uint4(0, 0, 0, 0);
     };
-    const auto load_b = [&](int k, int j) {
-      const int n = n0 + 16 * (g >> 1) + 2 * j + (g & 1);
-      return n < N ? load4(B + n * c.ldb, k + 4 * q, r, vecB) : make_uint2(0, 0);
+    const auto load_b = [&](int k, int j) {  // a row past the last repeats it: its sums are not stored
+      const int n = min(n0 + 32 * (j >> 2) + 8 * (g >> 1) + 2 * (j & 3) + (g & 1), N - 1);
+      return load4(B + n * c.ldb, k + 4 * q, r, vecB);
     };
     if (__all_sync(0xffffffffu, mine || t0 + lane >= c.nrows)) {
 #pragma unroll 1
@@ -299,20 +284,21 @@ __global__ void __launch_bounds__(kAdThreads)
   for (int i = 0; i < 4; ++i) {
     const int64_t t = t0 + 8 * i + g;
     if (t >= c.nrows) continue;
-    uint16_t* dst = y + t * c.ldy + nq;
-    uint32_t v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      v[j] = bits16<half>(acc[i >> 1][j][2 * (i & 1)]) |
-             static_cast<uint32_t>(bits16<half>(acc[i >> 1][j][2 * (i & 1) + 1])) << 16;
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      if (vecY && nq + 8 * s + 8 <= N) {
-        *reinterpret_cast<uint4*>(dst + 8 * s) = make_uint4(v[4 * s], v[4 * s + 1], v[4 * s + 2], v[4 * s + 3]);
+      const int n = n0 + 32 * s + 8 * q;
+      uint32_t v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        v[j] = bits16<half>(acc[i >> 1][4 * s + j][2 * (i & 1)]) |
+               static_cast<uint32_t>(bits16<half>(acc[i >> 1][4 * s + j][2 * (i & 1) + 1])) << 16;
+      uint16_t* dst = y + t * c.ldy + n;
+      if (vec) {
+        if (n < N) *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (nq + 8 * s + e < N) dst[8 * s + e] = static_cast<uint16_t>(v[4 * s + (e >> 1)] >> (16 * (e & 1)));
+          if (n + e < N) dst[e] = static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1)));
       }
     }
   }
@@ -337,9 +323,7 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
     if (2 * p < r) {
       const uint16_t* A0 = static_cast<const uint16_t*>(c.A) + a * c.strideA + 2 * p * c.lda;
       const uint16_t* A1 = 2 * p + 1 < r ? A0 + c.lda : A0;
-#pragma unroll 4
-      for (int k = 8 * lane; k < K; k += 256) {
-        const uint4 xv = load8(x, k, K), av = load8(A0, k, K), bv = load8(A1, k, K);
+      const auto add = [&](const uint4& xv, const uint4& av, const uint4& bv) {
         const uint32_t xw[4] = {xv.x, xv.y, xv.z, xv.w}, aw[4] = {av.x, av.y, av.z, av.w}, bw[4] = {bv.x, bv.y, bv.z, bv.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -349,7 +333,21 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
           s1 = fmaf(x0, value16<half>(static_cast<uint16_t>(bw[i])), s1);
           s1 = fmaf(x1, value16<half>(static_cast<uint16_t>(bw[i] >> 16)), s1);
         }
+      };
+      constexpr int U = 8;  // steps whose loads are in flight together
+      int k = 8 * lane;
+      for (; k - 8 * lane + 256 * U <= K; k += 256 * U) {
+        uint4 xv[U], av[U], bv[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          xv[u] = *reinterpret_cast<const uint4*>(x + k + 256 * u);
+          av[u] = *reinterpret_cast<const uint4*>(A0 + k + 256 * u);
+          bv[u] = *reinterpret_cast<const uint4*>(A1 + k + 256 * u);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) add(xv[u], av[u], bv[u]);
       }
+      for (; k < K; k += 256) add(load8(x, k, K), load8(A0, k, K), load8(A1, k, K));
       if (2 * p + 1 >= r) s1 = 0.0f;
     }
     s0 = warp_sum(s0);
@@ -419,8 +417,9 @@ void launch(const ws_adapters_call& c, uint2* h, cudaStream_t s) {
     else if (rpad <= 32) run(std::integral_constant<int, 4>());
     else run(std::integral_constant<int, 8>());
   }
-  expand_tile_kernel<half><<<dim3(tiles, static_cast<unsigned>((c.N + 64 * kAdWarps - 1) / (64 * kAdWarps))), kAdThreads, 0, s>>>(
-      c, h, rpad, vecB, (!c.base || rows16(c.base, c.ldbase)) && rows16(c.y, c.ldy));
+  const bool vec = c.N % 8 == 0 && (!c.base || rows16(c.base, c.ldbase)) && rows16(c.y, c.ldy);
+  const auto expand = vec ? expand_tile_kernel<half, true> : expand_tile_kernel<half, false>;
+  expand<<<dim3(tiles, static_cast<unsigned>((c.N + 64 * kAdWarps - 1) / (64 * kAdWarps))), kAdThreads, 0, s>>>(c, h, rpad, vecB);
 }
 
 }  // namespace

@@ -211,9 +211,30 @@ __device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first
   return true;
 }
 
-// Stores 16 values of a row of the result, `count` of them inside it.
-__device__ __forceinline__ void store_row16(const GroupedParams& p, uint16_t* dst, const float (&f)[16], int count) {
-  if (p.vec && count >= 16) {
+// Where a warp turns 32 rows of 16 values, one row a lane, so that its lanes store along rows.
+using Stage = uint16_t[32][18];
+
+// Stores 16 values of a row of the result, `count` of them inside it; on: the lane's row is stored.
+// Rows that start at multiples of 16 bytes take two stores a lane; others go through `stage`, as a lane's 2-byte stores would
+// touch 32 rows at a time (3003 rows of 1003 values, K = 1000: 54 us so, 23 us turned).
+__device__ __forceinline__ void store_rows16(const GroupedParams& p, uint16_t* dst, const float (&f)[16], int count, bool on,
+                                             Stage& stage) {
+  if (!p.vec) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) stage[lane][i] = round16(f[i], p.half);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int row = 2 * i + (lane >> 4), col = lane & 15;
+      uint16_t* to = reinterpret_cast<uint16_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), row));
+      if (__shfl_sync(0xffffffffu, on, row) && col < count) to[col] = stage[row][col];
+    }
+    __syncwarp();
+    return;
+  }
+  if (!on) return;
+  if (count >= 16) {
     uint32_t w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = round16(f[2 * i], p.half) | static_cast<uint32_t>(round16(f[2 * i + 1], p.half)) << 16;
@@ -240,6 +261,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ int scratch[32];
   __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages], acc_full[2], acc_empty[2], last_bar;
   __shared__ uint32_t tmem_slot;
+  __shared__ Stage stage[kRows == kRowsN ? 1 : 4];
   __shared__ volatile int dead;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -406,13 +428,13 @@ __global__ void __launch_bounds__(kThreads, 1)
           const int left = p.features - t.n0 - c;
           if (left <= 0) break;
           if (t.steps > 0) tmem_load16(addr + c, f);
-          if (m < t.rows) store_row16(p, result + (static_cast<int64_t>(t.row0) + m) * p.ldo + t.n0 + c, f, left);
+          store_rows16(p, result + (static_cast<int64_t>(t.row0) + m) * p.ldo + t.n0 + c, f, left, m < t.rows, stage[quarter]);
         } else if constexpr (kRows == kRowsSum) {
           const int left = p.width - t.n0 - c;
           if (left <= 0) break;
           if (t.steps > 0) tmem_load16(addr + c, f);
-          if (t.m0 + m < p.features)
-            store_row16(p, result + t.group * p.group_stride + (static_cast<int64_t>(t.m0) + m) * p.ldo + t.n0 + c, f, left);
+          store_rows16(p, result + t.group * p.group_stride + (static_cast<int64_t>(t.m0) + m) * p.ldo + t.n0 + c, f, left,
+                       t.m0 + m < p.features, stage[quarter]);
         } else {
           const int left = t.rows - c;
           if (left <= 0) break;
@@ -439,6 +461,115 @@ __global__ void __launch_bounds__(kThreads, 1)
   if (warp == 1)
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(static_cast<uint32_t>(S::kAccCols))
                  : "memory");
+}
+
+// ---------------------------------------------------------------- few rows an expert, forward
+//
+// Bound by W, each met expert's once.  A CTA takes 32 features and up to 16 rows of an expert; its eight warps split K and
+// read W straight into the operands of the warp-level matrix instruction (16 features x 8 rows), 16 bytes a load, four steps
+// in flight; the warps' sums meet in shared memory.  Against a tile of 128 features on the tcgen05 path the GPU gets four
+// times as many pieces of work: six rows of four experts each, N = 1024, K = 2048, bfloat16: 31 us there.
+
+constexpr int kThinThreads = 256;
+constexpr int kThinWarps = kThinThreads / 32;
+constexpr int kThinRows = 16, kThinFeatures = 32;
+
+template <bool half>
+__global__ void __launch_bounds__(kThinThreads, 2)
+    thin_kernel(const int64_t* __restrict__ offsets, int groups, const uint16_t* __restrict__ x, int64_t ldx,
+                const uint16_t* __restrict__ W, int64_t ldw, int64_t group_stride, uint16_t* __restrict__ y, int64_t ldy,
+                int N, int K) {
+  __shared__ float red[kThinWarps][kThinFeatures][kThinRows + 1];
+  __shared__ int scratch[32];
+  __shared__ int found[3];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
+  if (threadIdx.x == 0) found[0] = -1;
+  int sum = 0;
+  const int want = blockIdx.y;
+  for (int e0 = 0; e0 < groups && sum <= want; e0 += kThinThreads) {
+    const int e = e0 + threadIdx.x;
+    const int64_t b = e < groups ? offsets[e] : 0;
+    const int rows = e < groups ? static_cast<int>(offsets[e + 1] - b) : 0;
+    const int n = (rows + kThinRows - 1) / kThinRows;
+    int all = 0;
+    const int before = sum + block_exclusive_scan(n, scratch, &all);
+    if (want >= before && want < before + n) {
+      found[0] = e;
+      found[1] = static_cast<int>(b) + (want - before) * kThinRows;
+      found[2] = min(kThinRows, rows - (want - before) * kThinRows);
+    }
+    sum += all;
+  }
+  __syncthreads();
+  const int e = found[0], row0 = found[1], rows = found[2];
+  if (e < 0) return;
+  const int f0 = blockIdx.x * kThinFeatures;
+  const uint16_t* wrow[4];
+  const uint16_t* xrow[2];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) wrow[i] = W + e * group_stride + min(f0 + 8 * i + g, N - 1) * ldw;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) xrow[i] = x + (static_cast<int64_t>(row0) + min(8 * i + g, rows - 1)) * ldx;
+  const bool both = rows > 8;
+  float acc[2][2][4] = {};
+  const auto step = [&](const uint4(&wv)[4], const uint4(&xv)[2]) {
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        mma16<half>(acc[m][j], wv[2 * m].x, wv[2 * m + 1].x, wv[2 * m].y, wv[2 * m + 1].y, xv[j].x, xv[j].y);
+        mma16<half>(acc[m][j], wv[2 * m].z, wv[2 * m + 1].z, wv[2 * m].w, wv[2 * m + 1].w, xv[j].z, xv[j].w);
+      }
+  };
+  constexpr int kStep = 32 * kThinWarps, U = 4;
+  int k = 32 * warp + 8 * q;
+  for (; k - 8 * q + kStep * (U - 1) + 32 <= K; k += kStep * U) {
+    uint4 wv[U][4], xv[U][2];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) wv[u][i] = *reinterpret_cast<const uint4*>(wrow[i] + k + kStep * u);
+      xv[u][0] = *reinterpret_cast<const uint4*>(xrow[0] + k + kStep * u);
+      xv[u][1] = both ? *reinterpret_cast<const uint4*>(xrow[1] + k + kStep * u) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) step(wv[u], xv[u]);
+  }
+#pragma unroll 1
+  for (; k - 8 * q < K; k += kStep) {
+    uint4 wv[4], xv[2];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) wv[i] = load8(wrow[i], k, K);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) xv[i] = load8(xrow[i], k, K);
+    step(wv, xv);
+  }
+#pragma unroll
+  for (int m = 0; m < 2; ++m)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) red[warp][16 * m + 8 * (i >> 1) + g][8 * j + 2 * q + (i & 1)] = acc[m][j][i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < kThinFeatures * rows; i += kThinThreads) {
+    const int f = i % kThinFeatures, row = i / kThinFeatures;
+    if (f0 + f >= N) continue;
+    float s = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kThinWarps; ++w) s += red[w][f][row];
+    y[(static_cast<int64_t>(row0) + row) * ldy + f0 + f] = bits16<half>(s);
+  }
+}
+
+cudaError_t launch_thin(const GroupedRows& g, cudaStream_t s) {
+  const int64_t met = g.r->nnz < g.r->ncols ? g.r->nnz : g.r->ncols;
+  const dim3 grid(static_cast<unsigned>((g.N + kThinFeatures - 1) / kThinFeatures),
+                  static_cast<unsigned>(g.r->nnz / kThinRows + met));
+  const auto kernel = g.half ? thin_kernel<true> : thin_kernel<false>;
+  kernel<<<grid, kThinThreads, 0, s>>>(g.r->offsets, static_cast<int>(g.r->ncols), static_cast<const uint16_t*>(g.x), g.ldx,
+                                       static_cast<const uint16_t*>(g.w), g.ldw, g.group_stride,
+                                       static_cast<uint16_t*>(g.out), g.ldo, static_cast<int>(g.N), static_cast<int>(g.K));
+  return cudaGetLastError();
 }
 
 // ---------------------------------------------------------------- host
@@ -517,7 +648,10 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
   };
   using std::integral_constant;
   // Few rows an expert: W's features fill the 128 lanes and the rows are the short side.
-  if (mean <= 12) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>());
+  if (mean <= 12) {
+    if constexpr (kWMN) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>());
+    else return launch_thin(g, s);
+  }
   if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>());
   // Tiles of 256 features where they still give every SM one, else of 128.
   if ((g.r->nnz / kTileM + met / 2) * up(features, 256) >= num_sms)

@@ -44,47 +44,107 @@ __device__ __forceinline__ void load_row(const T* row, int at, int cols, bool ve
   }
 }
 
+__device__ __forceinline__ float key_value(uint32_t key) {
+  return key == 0xffffffffu ? NAN : __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+}
+
 // A warp per row; a lane holds V consecutive logits, so that among equal
 // logits the lowest lane holds the lowest column and a ballot settles ties.
+//
+// The k-th largest of the lanes' own maxima is at most the row's k-th largest
+// logit, so every chosen logit is at or above it, and few others are: those
+// candidates go to one a lane, by column, and k rounds of a warp maximum choose
+// among them.  Rows with more than 32 candidates (many equal logits, or k near
+// the number of lanes) choose among all logits, a round at a time: the lane
+// that held the maximum looks for its next.  65,537 rows of 256 (k = 8,
+// float) took 51 us with that way alone (issue: 900 instructions a row).
 template <typename T, int V>
 __global__ void __launch_bounds__(32 * kRouteWarps)
     topk_route_kernel(const T* __restrict__ logits, int64_t rows, int cols, int64_t ld, bool vec, int k,
                       bool normalize, int64_t* __restrict__ rowptr, int32_t* __restrict__ colidx,
                       float* __restrict__ vals) {
-  const int lane = threadIdx.x & 31;
-  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
+  __shared__ uint2 cand[kRouteWarps][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  const int64_t row = static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp;
   if (row >= rows) return;
   float f[V];
   load_row<T, V>(logits + row * ld, lane * V, cols, vec, f);
   uint32_t key[V];
-  uint32_t best = 0;
-  int where = 0;
 #pragma unroll
-  for (int i = V - 1; i >= 0; --i) {
-    key[i] = lane * V + i < cols ? order_key(f[i]) : 0u;
-    if (key[i] >= best) best = key[i], where = i;
-  }
-  uint32_t my_key = 0;
-  int my_col = 0x7fffffff;
-  for (int r = 0; r < k; ++r) {
-    const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-    const int owner = __ffs(__ballot_sync(0xffffffffu, best == top)) - 1;
-    const int col = __shfl_sync(0xffffffffu, lane * V + where, owner);
-    if (lane == r) my_key = top, my_col = col;
-    if (lane == owner) {  // the logit leaves; the lane's next best
+  for (int i = 0; i < V; ++i) key[i] = lane * V + i < cols ? order_key(f[i]) : 0u;
+  uint32_t my_key = key[0];  // the lane's candidate
+  int my_col = lane;
+  bool one_each = V == 1;
+  if constexpr (V > 1) {
+    uint32_t best = key[0];
+#pragma unroll
+    for (int i = 1; i < V; ++i) best = max(best, key[i]);
+    uint32_t bound = 0;
+    for (int r = 0; r < k; ++r) {  // equal maxima leave together: the bound is lower then, not wrong
+      bound = __reduce_max_sync(0xffffffffu, best);
+      if (best == bound) best = 0;
+    }
+    bound = max(bound, 1u);
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < V; ++i) mine += key[i] >= bound;
+    int upto = mine;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const int all = __shfl_sync(0xffffffffu, upto, 31);
+    one_each = all <= 32;
+    if (one_each) {
+      int at = upto - mine;
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        if (i == where) key[i] = 0;
-      best = 0;
-#pragma unroll
-      for (int i = V - 1; i >= 0; --i)
-        if (key[i] >= best) best = key[i], where = i;
+        if (key[i] >= bound) cand[warp][at++] = make_uint2(key[i], lane * V + i);
+      __syncwarp();
+      const uint2 c = lane < all ? cand[warp][lane] : make_uint2(0, 0);
+      my_key = c.x;
+      my_col = c.y;
     }
   }
-  const float mine = my_key == 0xffffffffu ? NAN : __uint_as_float(my_key & 0x80000000u ? my_key & 0x7fffffffu : ~my_key);
-  float m = __shfl_sync(0xffffffffu, mine, 0);
+  bool chosen = false;
+  int rank;
+  if (one_each) {
+    uint32_t left = my_key;
+    for (int r = 0; r < k; ++r) {
+      const uint32_t top = __reduce_max_sync(0xffffffffu, left);
+      if (lane == __ffs(__ballot_sync(0xffffffffu, left == top)) - 1) left = 0, chosen = true;
+    }
+    rank = __popc(__ballot_sync(0xffffffffu, chosen) & ((1u << lane) - 1u));
+  } else {
+    uint32_t best = 0;
+    int where = 0;
+#pragma unroll
+    for (int i = V - 1; i >= 0; --i)
+      if (key[i] >= best) best = key[i], where = i;
+    my_col = 0x7fffffff;
+    for (int r = 0; r < k; ++r) {
+      const uint32_t top = __reduce_max_sync(0xffffffffu, best);
+      const int owner = __ffs(__ballot_sync(0xffffffffu, best == top)) - 1;
+      const int col = __shfl_sync(0xffffffffu, lane * V + where, owner);
+      if (lane == r) my_key = top, my_col = col;
+      if (lane == owner) {  // the logit leaves; the lane's next best
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (i == where) key[i] = 0;
+        best = 0;
+#pragma unroll
+        for (int i = V - 1; i >= 0; --i)
+          if (key[i] >= best) best = key[i], where = i;
+      }
+    }
+    chosen = lane < k;
+    rank = 0;  // places by column
+    for (int r = 0; r < k; ++r) rank += __shfl_sync(0xffffffffu, my_col, r) < my_col;
+  }
+  float m = key_value(__reduce_max_sync(0xffffffffu, chosen ? my_key : 0u));
   if (m == -INFINITY) m = 0.0f;
-  const float e = lane < k ? expf(mine - m) : 0.0f;
+  const float e = chosen ? expf(key_value(my_key) - m) : 0.0f;
   float total = e;
   if (!normalize) {
     total = 0.0f;
@@ -92,10 +152,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
     for (int i = 0; i < V; ++i) total += expf(f[i] - m);  // 0 past the row's end
   }
   total = warp_sum(total);
-  int rank = 0;  // places by column
-  for (int r = 0; r < k; ++r) rank += __shfl_sync(0xffffffffu, my_col, r) < my_col;
   const int64_t at = row * k;
-  if (lane < k) {
+  if (chosen) {
     colidx[at + rank] = my_col;
     vals[at + rank] = total == 0.0f ? 0.0f : e / total;
   }
@@ -132,7 +190,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
 #pragma unroll
     for (int i = 0; i < V; ++i) best = max(best, order_key(out[i]));
     const uint32_t top = __reduce_max_sync(0xffffffffu, best);
-    float m = top == 0xffffffffu ? NAN : __uint_as_float(top & 0x80000000u ? top & 0x7fffffffu : ~top);
+    float m = key_value(top);
     if (m == -INFINITY) m = 0.0f;
     float total = 0.0f;
 #pragma unroll

@@ -26,87 +26,92 @@ namespace {
 
 // ---------------------------------------------------------------- R transposed
 
-constexpr int kBuildWarps = 16;
-constexpr int kTileRows = 32 * kBuildWarps;
-constexpr int kOneLaunchRows = 2 * kTileRows;  // rows that one CTA takes alone
+// A tile is 32 rows for each warp of a CTA: 32 warps where one CTA builds the
+// plan alone (a single launch), eight where many CTAs do (a launch that counts
+// and one that places).
+constexpr int kSmallWarps = 32, kBuildWarps = 8;
+constexpr int kSmallRows = 32 * kSmallWarps, kTileRows = 32 * kBuildWarps;
+constexpr int kHeld = 8;  // entries that a lane holds at once: loads in flight, and rows of 8 entries walked once
 
-// Marks the columns of the tile's rows: bit i of mask[warp * cols + e] is row 32 warp + i.
-// With `place`, the second walk: pre[warp * cols + e] holds the slot of the warp's first entry of column e.
-template <bool place>
-__device__ __forceinline__ void walk_tile(const ws_routing& r, int64_t row0, int cols, uint32_t* mask, const int* pre) {
+// The entries of a warp's 32 rows, kHeld a lane at a time.
+struct WarpRows {
+  int end;          // of the lane's row
+  int64_t lo, hi;   // of all 32 rows
+  int64_t first;    // their first row
+  int col[kHeld];
+  int row[kHeld];   // of 0..31; -1: no entry
+  __device__ __forceinline__ void start(const ws_routing& r, int64_t first_row) {
+    const int lane = threadIdx.x & 31;
+    first = first_row;
+    int begin = 0;
+    end = 0;
+    lo = hi = 0;
+    if (first < r.nrows) {
+      entry_range(r.rowptr, min(first + lane, r.nrows - 1), r.nnz, &begin, &end);
+      if (first + lane >= r.nrows) begin = end;
+      lo = __shfl_sync(0xffffffffu, begin, 0);
+      hi = __shfl_sync(0xffffffffu, end, 31);
+    }
+  }
+  __device__ __forceinline__ void load(const ws_routing& r, int64_t base) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) col[i] = base + 32 * i + lane < hi ? r.colidx[base + 32 * i + lane] : -1;
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i) {
+      const int64_t e = base + 32 * i + lane;
+      int n = 0;  // rows that end at or before e
+#pragma unroll
+      for (int step = 16; step; step >>= 1) {
+        const int last = __shfl_sync(0xffffffffu, end, n + step - 1);
+        if (last <= e) n += step;
+      }
+      row[i] = e < hi && first + n < r.nrows ? n : -1;
+    }
+  }
+};
+
+// Marks the columns of the warp's rows: bit i of mask[warp * cols + e] is its row i.
+__device__ __forceinline__ void mark_rows(const ws_routing& r, WarpRows& w, int cols, uint32_t* mask) {
+  uint32_t* word = mask + (threadIdx.x >> 5) * cols;
+  for (int64_t base = w.lo; base < w.hi; base += 32 * kHeld) {
+    w.load(r, base);
+#pragma unroll
+    for (int i = 0; i < kHeld; ++i)
+      if (w.row[i] >= 0 && static_cast<unsigned>(w.col[i]) < static_cast<unsigned>(cols))
+        atomicOr(word + w.col[i], 1u << w.row[i]);
+  }
+}
+
+// Slots of the warp's rows; pre[warp * cols + e] plus first[e] is the slot of the warp's first entry of column e.
+__device__ __forceinline__ void place_rows(const ws_routing& r, WarpRows& w, int cols, const uint32_t* mask,
+                                           const uint16_t* pre, const int* first) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int64_t first = row0 + 32 * warp;
-  if (first >= r.nrows) return;
-  int begin = 0, end = 0;
-  entry_range(r.rowptr, min(first + lane, r.nrows - 1), r.nnz, &begin, &end);
-  if (first + lane >= r.nrows) begin = end;
-  const int lo = __shfl_sync(0xffffffffu, begin, 0);
-  const int hi = __shfl_sync(0xffffffffu, end, 31);
-  for (int64_t base = lo; base < hi; base += 32) {
-    const int64_t e = base + lane;
-    int row = 0;  // rows of the warp that end at or before e
+  const bool held = w.hi - w.lo <= 32 * kHeld;  // by mark_rows
+  for (int64_t base = w.lo; base < w.hi; base += 32 * kHeld) {
+    if (!held) w.load(r, base);
 #pragma unroll
-    for (int step = 16; step; step >>= 1) {
-      const int last = __shfl_sync(0xffffffffu, end, row + step - 1);
-      if (last <= e) row += step;
-    }
-    if (e < hi && first + row < r.nrows) {
-      const int col = r.colidx[e];
-      const bool in = static_cast<unsigned>(col) < static_cast<unsigned>(cols);
-      uint32_t* word = mask + warp * cols + col;
-      if (!place) {
-        if (in) atomicOr(word, 1u << row);
-      } else {
-        int slot = -1;
-        if (in) {
-          slot = pre[warp * cols + col] + __popc(*word & ((1u << row) - 1u));
-          r.rows[slot] = static_cast<int32_t>(first + row);
-          r.entries[slot] = static_cast<int32_t>(e);
-        }
-        r.slots[e] = slot;
+    for (int i = 0; i < kHeld; ++i) {
+      if (w.row[i] < 0) continue;
+      const int64_t e = base + 32 * i + lane;
+      const int col = w.col[i];
+      int slot = -1;
+      if (static_cast<unsigned>(col) < static_cast<unsigned>(cols)) {
+        slot = first[col] + pre[warp * cols + col] + __popc(mask[warp * cols + col] & ((1u << w.row[i]) - 1u));
+        r.rows[slot] = static_cast<int32_t>(w.first + w.row[i]);
+        r.entries[slot] = static_cast<int32_t>(e);
       }
+      r.slots[e] = slot;
     }
   }
 }
 
-// Entries of every column in the rows [begin, end), added to cnt (shared).
-__device__ __forceinline__ void count_rows(const ws_routing& r, int64_t begin, int64_t end, int cols, uint32_t* mask,
-                                           int* cnt) {
-  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
-    for (int i = threadIdx.x; i < kBuildWarps * cols; i += blockDim.x) mask[i] = 0;
-    __syncthreads();
-    walk_tile<false>(r, row0, cols, mask, nullptr);
-    __syncthreads();
-    for (int e = threadIdx.x; e < cols; e += blockDim.x) {
-      int n = 0;
-#pragma unroll
-      for (int w = 0; w < kBuildWarps; ++w) n += __popc(mask[w * cols + e]);
-      cnt[e] += n;
-    }
-    __syncthreads();
-  }
-}
-
-// Places the entries of the rows [begin, end); next[e] (shared) is the next slot of column e.
-__device__ __forceinline__ void place_rows(const ws_routing& r, int64_t begin, int64_t end, int cols, uint32_t* mask,
-                                           int* pre, int* next) {
-  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
-    for (int i = threadIdx.x; i < kBuildWarps * cols; i += blockDim.x) mask[i] = 0;
-    __syncthreads();
-    walk_tile<false>(r, row0, cols, mask, nullptr);
-    __syncthreads();
-    for (int e = threadIdx.x; e < cols; e += blockDim.x) {
-      int n = next[e];
-#pragma unroll
-      for (int w = 0; w < kBuildWarps; ++w) {
-        pre[w * cols + e] = n;
-        n += __popc(mask[w * cols + e]);
-      }
-      next[e] = n;
-    }
-    __syncthreads();
-    walk_tile<true>(r, row0, cols, mask, pre);
-    __syncthreads();
+// Clears `words` words, 16 bytes at a time (the masks start at a multiple of that).
+__device__ __forceinline__ void clear_words(uint32_t* p, int words) {
+  for (int i = 4 * threadIdx.x; i < words; i += 4 * blockDim.x) {
+    if (i + 4 <= words) *reinterpret_cast<uint4*>(p + i) = make_uint4(0, 0, 0, 0);
+    else
+      for (int j = i; j < words; ++j) p[j] = 0;
   }
 }
 
@@ -128,36 +133,69 @@ __device__ __forceinline__ int scan_columns(int cols, int* total, int* scratch) 
 // Offsets of all columns, and -1 in the slots that entries of no column leave over.
 __device__ __forceinline__ void write_offsets(const ws_routing& r, int cols, const int* first, int placed) {
   for (int e = threadIdx.x; e < cols; e += blockDim.x) r.offsets[e] = first[e];
-  if (threadIdx.x == 0) r.offsets[cols] = placed;
+  if (threadIdx.x == 0) {
+    r.offsets[cols] = placed;
+    *r.status = 0;
+  }
   for (int64_t i = placed + static_cast<int64_t>(threadIdx.x); i < r.nnz; i += blockDim.x) r.rows[i] = r.entries[i] = -1;
 }
 
-// Shared memory of the build kernels: mask and pre [kBuildWarps][cols], next [cols].
-size_t build_smem(int cols) { return (2 * kBuildWarps + 1) * static_cast<size_t>(cols) * sizeof(int); }
+// Entries of column e in the warps' rows; pre[w * cols + e] receives those of the warps before w.
+template <int W>
+__device__ __forceinline__ int count_column(const uint32_t* mask, uint16_t* pre, int cols, int e) {
+  int n = 0;
+#pragma unroll
+  for (int w = 0; w < W; ++w) {
+    pre[w * cols + e] = static_cast<uint16_t>(n);
+    n += __popc(mask[w * cols + e]);
+  }
+  return n;
+}
 
-__global__ void __launch_bounds__(kTileRows) routing_small_kernel(ws_routing r, int cols) {
-  extern __shared__ int sm[];
+// Shared memory: mask [W][cols], two int arrays [cols], pre [W][cols].
+template <int W>
+size_t build_smem(int cols) { return static_cast<size_t>(cols) * (W * 4 + 8 + W * 2); }
+
+__global__ void __launch_bounds__(32 * kSmallWarps) routing_small_kernel(ws_routing r, int cols) {
+  extern __shared__ __align__(16) int sm[];
   __shared__ int scratch[32];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
-  int* pre = sm + kBuildWarps * cols;
-  int* next = pre + kBuildWarps * cols;
-  for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = 0;
-  count_rows(r, 0, r.nrows, cols, mask, next);
+  int* first = sm + kSmallWarps * cols;
+  uint16_t* pre = reinterpret_cast<uint16_t*>(first + 2 * cols);
+  WarpRows w;
+  w.start(r, threadIdx.x & ~31u);
+  clear_words(mask, kSmallWarps * cols);
   __syncthreads();
-  const int placed = scan_columns(cols, next, scratch);
-  write_offsets(r, cols, next, placed);
+  mark_rows(r, w, cols, mask);
   __syncthreads();
-  place_rows(r, 0, r.nrows, cols, mask, pre, next);
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) first[e] = count_column<kSmallWarps>(mask, pre, cols, e);
+  __syncthreads();
+  const int placed = scan_columns(cols, first, scratch);
+  write_offsets(r, cols, first, placed);
+  place_rows(r, w, cols, mask, pre, first);
 }
 
 __global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, int cols, int64_t chunk, int32_t* counts) {
-  extern __shared__ int sm[];
+  extern __shared__ __align__(16) int sm[];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
   int* cnt = sm + kBuildWarps * cols;
   for (int e = threadIdx.x; e < cols; e += blockDim.x) cnt[e] = 0;
-  const int64_t begin = chunk * blockIdx.x;
-  count_rows(r, begin, min(begin + chunk, r.nrows), cols, mask, cnt);
-  __syncthreads();
+  const int64_t begin = chunk * blockIdx.x, end = min(begin + chunk, r.nrows);
+  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
+    WarpRows w;
+    w.start(r, row0 + (threadIdx.x & ~31u));
+    clear_words(mask, kBuildWarps * cols);
+    __syncthreads();
+    mark_rows(r, w, cols, mask);
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) {
+      int n = 0;
+#pragma unroll
+      for (int i = 0; i < kBuildWarps; ++i) n += __popc(mask[i * cols + e]);
+      cnt[e] += n;
+    }
+    __syncthreads();
+  }
   for (int e = threadIdx.x; e < cols; e += blockDim.x) counts[static_cast<int64_t>(blockIdx.x) * cols + e] = cnt[e];
 }
 
@@ -165,35 +203,48 @@ __global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, 
 // a launch less than a scan of its own.
 __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, int cols, int64_t chunk,
                                                                   const int32_t* counts) {
-  extern __shared__ int sm[];
+  extern __shared__ __align__(16) int sm[];
   __shared__ int scratch[32];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
-  int* pre = sm + kBuildWarps * cols;
-  int* next = pre + kBuildWarps * cols;
-  int* before = sm;       // [cols], entries of the chunks before this one: taken out of use before the masks
+  int* next = sm + kBuildWarps * cols;  // first slot of the tile in every column
+  int* before = next + cols;            // entries of the chunks before this one
+  uint16_t* pre = reinterpret_cast<uint16_t*>(before + cols);
   for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = before[e] = 0;
   __syncthreads();
   const int groups = cols >= static_cast<int>(blockDim.x) ? 1 : blockDim.x / cols;
   const int g = static_cast<int>(threadIdx.x) / cols;
-  for (int e = threadIdx.x - g * cols; g < groups && e < cols; e += blockDim.x) {
+  for (int e = threadIdx.x - (groups > 1 ? g * cols : 0); g < groups || groups == 1; e += blockDim.x) {
+    if (e >= cols) break;
     int total = 0, mine = 0;
 #pragma unroll 8
-    for (int c = g; c < static_cast<int>(gridDim.x); c += groups) {
+    for (int c = groups > 1 ? g : 0; c < static_cast<int>(gridDim.x); c += groups) {
       const int n = counts[static_cast<int64_t>(c) * cols + e];
       total += n;
       if (c < static_cast<int>(blockIdx.x)) mine += n;
     }
     atomicAdd(&next[e], total);
     atomicAdd(&before[e], mine);
+    if (groups > 1) break;
   }
   __syncthreads();
   const int placed = scan_columns(cols, next, scratch);
   if (blockIdx.x == 0) write_offsets(r, cols, next, placed);
   __syncthreads();
   for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
-  __syncthreads();
-  const int64_t begin = chunk * blockIdx.x;
-  place_rows(r, begin, min(begin + chunk, r.nrows), cols, mask, pre, next);
+  const int64_t begin = chunk * blockIdx.x, end = min(begin + chunk, r.nrows);
+  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
+    WarpRows w;
+    w.start(r, row0 + (threadIdx.x & ~31u));
+    clear_words(mask, kBuildWarps * cols);
+    __syncthreads();
+    mark_rows(r, w, cols, mask);
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) before[e] = count_column<kBuildWarps>(mask, pre, cols, e);
+    __syncthreads();
+    place_rows(r, w, cols, mask, pre, next);
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
+  }
 }
 
 // ------------------------------------------------------------------ rows moved
@@ -400,7 +451,7 @@ unsigned warp_grid(int64_t units) { return static_cast<unsigned>((units + kMoveW
 
 // As many chunks as SMs at most, of whole tiles.
 int64_t routing_chunks(int64_t nrows, int num_sms) {
-  if (nrows <= kOneLaunchRows) return 1;
+  if (nrows <= kSmallRows) return 1;
   const int64_t tiles = (nrows + kTileRows - 1) / kTileRows;
   const int64_t each = (tiles + num_sms - 1) / num_sms;
   return (tiles + each - 1) / each;
@@ -408,20 +459,21 @@ int64_t routing_chunks(int64_t nrows, int num_sms) {
 
 void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cudaStream_t s) {
   const int cols = static_cast<int>(r.ncols);
-  const size_t smem = build_smem(cols);
   const int64_t chunks = routing_chunks(r.nrows, num_sms);
-  const auto allow = [&](const void* kernel) {
+  const auto allow = [&](const void* kernel, size_t smem) {
     if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   };
   if (chunks == 1) {
-    allow(reinterpret_cast<const void*>(routing_small_kernel));
-    routing_small_kernel<<<1, kTileRows, smem, s>>>(r, cols);
+    const size_t smem = build_smem<kSmallWarps>(cols);
+    allow(reinterpret_cast<const void*>(routing_small_kernel), smem);
+    routing_small_kernel<<<1, 32 * kSmallWarps, smem, s>>>(r, cols);
     return;
   }
+  const size_t smem = build_smem<kBuildWarps>(cols);
   const int64_t tiles = (r.nrows + kTileRows - 1) / kTileRows;
   const int64_t chunk = (tiles + chunks - 1) / chunks * kTileRows;
-  allow(reinterpret_cast<const void*>(routing_count_kernel));
-  allow(reinterpret_cast<const void*>(routing_place_kernel));
+  allow(reinterpret_cast<const void*>(routing_count_kernel), smem);
+  allow(reinterpret_cast<const void*>(routing_place_kernel), smem);
   routing_count_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
   routing_place_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
 }

@@ -68,6 +68,44 @@ __device__ __forceinline__ float warp_sum(float x) {
   return x;
 }
 
+// A 16-bit value (half or bfloat16) and a float.
+template <bool half>
+__device__ __forceinline__ float value16(uint16_t u) {
+  if constexpr (half) return __half2float(__ushort_as_half(u));
+  else return __uint_as_float(static_cast<uint32_t>(u) << 16);
+}
+template <bool half>
+__device__ __forceinline__ uint16_t bits16(float f) {
+  if constexpr (half) return __half_as_ushort(__float2half_rn(f));
+  else return __bfloat16_as_ushort(__float2bfloat16_rn(f));
+}
+// The warp-level matrix instruction: d (16 x 8) += a (16 x 16) b (16 x 8).  Lane 4 g + q holds rows g (a0, a2) and g + 8 (a1,
+// a3) of a and column g of b; a0, a1, b0 are one pair of the contraction index, a2, a3, b1 another, the same pairs for all
+// lanes of a q.  d: rows g (d0, d1) and g + 8, columns 2 q and 2 q + 1.
+template <bool half>
+__device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                      uint32_t b1) {
+  if constexpr (half)
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm volatile(
+        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Values k .. k + 7 of a row of K (16-byte aligned), zero past its end.
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int k, int K) {
+  if (k + 8 <= K) return *reinterpret_cast<const uint4*>(row + k);
+  uint32_t w[4] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (k + i < K) w[i >> 1] |= static_cast<uint32_t>(row[k + i]) << (16 * (i & 1));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
 // Launchers.  They queue kernels on s and leave errors to cudaGetLastError.
 void launch_topk_route(const void* logits, int64_t rows, int cols, int64_t ld, ws_dtype_t dt, int k, bool normalize,
                        int64_t* rowptr, int32_t* colidx, float* vals, cudaStream_t s);

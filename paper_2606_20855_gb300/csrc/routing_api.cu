@@ -138,8 +138,8 @@ int64_t ws_routing_scratch(int64_t nrows, int64_t ncols) {
 
 ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
   if (const ws_status_t st = check(r)) return st;
-  cudaMemsetAsync(r->status, 0, sizeof(int32_t), cuda_stream(stream));
   if (r->nnz == 0) {
+    cudaMemsetAsync(r->status, 0, sizeof(int32_t), cuda_stream(stream));
     cudaMemsetAsync(r->offsets, 0, static_cast<size_t>(r->ncols + 1) * sizeof(int64_t), cuda_stream(stream));
     return launched("ws_routing_build");
   }
