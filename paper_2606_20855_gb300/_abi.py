@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libws_spgemm.so")
 
@@ -64,7 +65,7 @@ SIGNATURES = [
     ("ws_routing_matmul_rows", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p]),
     ("ws_routing_matmul_weights", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _i64, _i32, _p]),
     ("ws_adapters_scratch", _i64, [_i64, _i64]),
-    ("ws_adapters", _i32, [_p, _p, _i64, _p]),
+    ("ws_adapters", _i32, [ctypes.c_char_p, _p, _i64, _p]),
 ]
 
 
@@ -73,12 +74,8 @@ class WsRouting(ctypes.Structure):
     _fields_ = [("nrows", _i64), ("ncols", _i64), ("nnz", _i64), ("rowptr", _p), ("colidx", _p), ("vals", _p),
                 ("offsets", _p), ("rows", _p), ("entries", _p), ("slots", _p), ("status", _p)]
 
-class WsAdaptersCall(ctypes.Structure):
-    """struct ws_adapters_call (device pointers as integers)."""
-    _fields_ = [("nrows", _i64), ("ncols", _i64), ("nnz", _i64), ("rowptr", _p), ("colidx", _p), ("vals", _p),
-                ("K", _i64), ("r", _i64), ("N", _i64), ("x", _p), ("ldx", _i64), ("A", _p), ("lda", _i64),
-                ("strideA", _i64), ("B", _p), ("ldb", _i64), ("strideB", _i64), ("base", _p), ("ldbase", _i64),
-                ("y", _p), ("ldy", _i64), ("dtype", _i32)]
+# struct ws_adapters_call: 21 64-bit fields (sizes, device pointers as integers, strides), then the type
+ADAPTERS_CALL = struct.Struct("<21qi4x")
 
 
 EWISE_OPS = {"add": 1, "mul": 2}  # ws_ewise_op_t
@@ -297,5 +294,6 @@ def ws_adapters_scratch(nnz: int, r: int) -> int:
     return load().ws_adapters_scratch(nnz, r)
 
 
-def ws_adapters(call: WsAdaptersCall, scratch: int, scratch_bytes: int, stream: int) -> None:
-    _check("ws_adapters", load().ws_adapters(ctypes.byref(call), scratch, scratch_bytes, stream))
+def ws_adapters(call: bytes, scratch: int, scratch_bytes: int, stream: int) -> None:
+    """``call``: the fields of struct ws_adapters_call packed by ADAPTERS_CALL."""
+    _check("ws_adapters", load().ws_adapters(call, scratch, scratch_bytes, stream))

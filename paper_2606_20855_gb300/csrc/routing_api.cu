@@ -88,6 +88,15 @@ ws_status_t check_product(const ws_routing* r, int64_t N, int64_t K, ws_dtype_t 
   return WS_OK;
 }
 
+// Rows of 16-bit zeros: a sum over nothing.
+ws_status_t zero_rows(void* p, int64_t rows, int64_t width, int64_t ld, ws_stream_t stream) {
+  const cudaError_t e = ld == width || rows == 1
+                            ? cudaMemsetAsync(p, 0, static_cast<size_t>(rows) * width * 2, cuda_stream(stream))
+                            : cudaMemset2DAsync(p, static_cast<size_t>(ld) * 2, 0, static_cast<size_t>(width) * 2,
+                                                static_cast<size_t>(rows), cuda_stream(stream));
+  return e == cudaSuccess ? WS_OK : routing_fail(WS_ERR_CUDA, "memset: %s", cudaGetErrorString(e));
+}
+
 }  // namespace
 
 extern "C" {
@@ -200,7 +209,7 @@ ws_status_t ws_routing_matmul(const ws_routing* r, const void* xs, int64_t ldxs,
                                                                     {ys, r ? r->nnz : 0, N, ldys, false}}))
     return st;
   if (r->nnz == 0 || N == 0) return WS_OK;
-  if (K == 0) return routing_fail(WS_ERR_SHAPE, "a product over no values");
+  if (K == 0) return zero_rows(ys, r->nnz, N, ldys, stream);
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;
   return launch_grouped({r, dtype == WS_F16, xs, ldxs, W, ldw, stride, ys, ldys, N, K}, false, sms, cuda_stream(stream));
@@ -213,7 +222,7 @@ ws_status_t ws_routing_matmul_rows(const ws_routing* r, const void* gys, int64_t
                                                                     {gxs, r ? r->nnz : 0, K, ldgxs, false}}))
     return st;
   if (r->nnz == 0 || K == 0) return WS_OK;
-  if (N == 0) return routing_fail(WS_ERR_SHAPE, "a product over no values");
+  if (N == 0) return zero_rows(gxs, r->nnz, K, ldgxs, stream);
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;
   return launch_grouped({r, dtype == WS_F16, gys, ldgys, W, ldw, stride, gxs, ldgxs, N, K}, true, sms, cuda_stream(stream));
@@ -227,9 +236,9 @@ ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int6
     return st;
   if (r->ncols == 0 || N == 0 || K == 0) return WS_OK;
   if (r->nnz == 0) {
-    if (ldgw != K || stride != N * K) return routing_fail(WS_ERR_INVALID_ARG, "gradients without rows are written to contiguous matrices only");
-    cudaMemsetAsync(gW, 0, static_cast<size_t>(r->ncols) * N * K * 2, cuda_stream(stream));
-    return launched("ws_routing_matmul_weights");
+    for (int64_t e = 0; e < r->ncols; ++e)
+      if (const ws_status_t st = zero_rows(static_cast<char*>(gW) + 2 * e * stride, N, K, ldgw, stream)) return st;
+    return WS_OK;
   }
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;

@@ -10,12 +10,13 @@ expert.  A layer of experts is
 
 where the experts' matrices may be ``plan.matmul(xs, W)``; the gradients are ``combine_backward``,
 ``dispatch_backward``, ``matmul_backward`` and ``topk_route_backward``.  All calls queue work on
-the current stream, or on ``stream``, and return without waiting; none reads anything back.
+the current stream, or on ``stream``, and return without waiting; none reads anything back.  Tensors are on the current
+device.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
+import functools
 
 import torch
 
@@ -23,99 +24,109 @@ from . import _abi
 from .spgemm import DeviceCSR
 
 _ROW_DTYPES = {torch.float32: _abi.WS_F32, torch.bfloat16: _abi.WS_BF16, torch.float16: _abi.WS_F16}
-_HERE = contextlib.nullcontext()
+_raw_stream = torch._C._cuda_getCurrentRawStream  # of a device, without building the object
 
 
-def _on(stream, *tensors):
-    """Context in which results are allocated and work is queued on ``stream`` (None: the current one).  Inputs that
-    came from another stream stay allocated until it is done with them."""
-    if stream is None:
-        return _HERE
-    for t in tensors:
-        t.record_stream(stream)
-    return torch.cuda.stream(stream)
-
-
-def _raw_stream(device) -> int:
-    return torch._C._cuda_getCurrentRawStream(device.index)
+def _elsewhere(f, stream, *args, **kwargs):
+    """f on ``stream``: results are allocated and work is queued there; inputs that came from another stream stay
+    allocated until it is done with them."""
+    for t in args:
+        for u in (t.rowptr, t.colidx, t.vals) if isinstance(t, DeviceCSR) else (t,):
+            if isinstance(u, torch.Tensor):
+                u.record_stream(stream)
+    with torch.cuda.stream(stream):
+        return f(*args, **kwargs)
 
 
 def _dtype(t: torch.Tensor, name: str) -> int:
     dt = _ROW_DTYPES.get(t.dtype)
     if dt is None:
         raise TypeError(f"{name} must be float32, bfloat16 or float16, got {t.dtype}")
+    if not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA tensor")
     return dt
 
 
-def _matrix(t: torch.Tensor, name: str, rows: int | None, like: torch.Tensor | None = None) -> torch.Tensor:
-    """A 2-D CUDA tensor whose rows have unit stride (copied if they have not)."""
-    if not t.is_cuda:
-        raise TypeError(f"{name} must be a CUDA tensor")
+def _same(t: torch.Tensor, like: torch.Tensor, name: str) -> None:
+    if t.dtype != like.dtype or t.device != like.device:
+        raise TypeError(f"{name} must have the other matrix's type and device")
+
+
+def _matrix(t: torch.Tensor, name: str, rows: int | None):
+    """(t, its row stride): a 2-D tensor whose rows have unit stride (copied if they have not)."""
     if t.dim() != 2 or (rows is not None and t.shape[0] != rows):
         raise ValueError(f"{name} must be 2-D" + (f" with {rows} rows" if rows is not None else "") +
                          f", got {tuple(t.shape)}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        raise TypeError(f"{name} must have the other matrix's type and device")
     n = t.shape[1]
+    if t.is_contiguous():
+        return t, n
     if (n > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < n):
-        return t.contiguous()
-    return t
+        return t.contiguous(), n
+    return t, t.stride(0) if t.shape[0] > 1 else n
 
 
-def _operand(t: torch.Tensor) -> torch.Tensor:
-    """A matrix (or a stack of matrices) of 16-bit values whose rows start at multiples of 16 bytes: t itself, or a
-    copy with longer rows where t's do not."""
+def _operand(t: torch.Tensor):
+    """(t, its row stride, that of the matrices of a stack): a matrix or a stack of matrices of 16-bit values whose rows
+    start at multiples of 16 bytes; t itself, or a copy with longer rows where t's do not."""
     n = t.shape[-1]
-    if t.data_ptr() % 16 == 0 and (n <= 1 or t.stride(-1) == 1) and \
-            all(t.shape[i] == 1 or (t.stride(i) % 8 == 0 and t.stride(i) >= n) for i in range(t.dim() - 1)):
-        return t
-    out = torch.empty((*t.shape[:-1], (n + 7) // 8 * 8), dtype=t.dtype, device=t.device)[..., :n]
-    return out.copy_(t)
-
-
-def _ld8(t: torch.Tensor) -> int:
-    return t.stride(-2) if t.shape[-2] > 1 else (t.shape[-1] + 7) // 8 * 8
-
-
-def _ld(t: torch.Tensor) -> int:
-    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+    if t.data_ptr() % 16 == 0:
+        if n % 8 == 0 and t.is_contiguous():
+            return t, n, n * t.shape[-2]
+        if (n <= 1 or t.stride(-1) == 1) and \
+                all(t.shape[i] == 1 or (t.stride(i) % 8 == 0 and t.stride(i) >= n) for i in range(t.dim() - 1)):
+            ld = t.stride(-2) if t.shape[-2] > 1 else (n + 7) // 8 * 8
+            return t, ld, t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else ld * t.shape[-2]
+    ld = (n + 7) // 8 * 8
+    out = torch.empty((*t.shape[:-1], ld), dtype=t.dtype, device=t.device)[..., :n]
+    return out.copy_(t), ld, ld * t.shape[-2]
 
 
 def topk_route(logits: torch.Tensor, k: int, normalize: bool = True, stream=None) -> DeviceCSR:
     """The routing matrix of a T x E tensor of logits: row i holds the k largest logits of row i (ties to the lowest
     column), by ascending column, with softmax weights over the chosen (``normalize``) or over all columns.  A logit
     of -inf has weight 0 and is chosen last; a row of nothing else has weights 0."""
+    if stream is not None:
+        return _elsewhere(topk_route, stream, logits, k, normalize)
     dt = _dtype(logits, "logits")
-    with _on(stream, logits):
-        x = _matrix(logits, "logits", None)
-        (T, E), k, dev = x.shape, int(k), x.device
-        if not 1 <= k <= min(E, 32):
-            raise ValueError(f"k must be in 1..min(columns, 32), got {k} of {E}")
-        rowptr = torch.empty(T + 1, dtype=torch.int64, device=dev)
-        colidx = torch.empty(T * k, dtype=torch.int32, device=dev)
-        vals = torch.empty(T * k, dtype=torch.float32, device=dev)
-        _abi.ws_topk_route(x.data_ptr(), T, E, _ld(x), dt, k, normalize, rowptr.data_ptr(), colidx.data_ptr(),
-                           vals.data_ptr(), _raw_stream(dev))
+    x, ld = _matrix(logits, "logits", None)
+    (T, E), k, dev = x.shape, int(k), x.device
+    if not 1 <= k <= min(E, 32):
+        raise ValueError(f"k must be in 1..min(columns, 32), got {k} of {E}")
+    rowptr = torch.empty(T + 1, dtype=torch.int64, device=dev)
+    colidx = torch.empty(T * k, dtype=torch.int32, device=dev)
+    vals = torch.empty(T * k, dtype=torch.float32, device=dev)
+    _abi.ws_topk_route(x.data_ptr(), T, E, ld, dt, k, normalize, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(),
+                       _raw_stream(dev.index))
     return DeviceCSR(T, E, rowptr, colidx, vals)
 
 
 def topk_route_backward(logits: torch.Tensor, R: DeviceCSR, grad_vals: torch.Tensor, normalize: bool = True,
                         stream=None) -> torch.Tensor:
     """Gradient of the logits from that of R's values, for ``R = topk_route(logits, k, normalize)``."""
+    if stream is not None:
+        return _elsewhere(topk_route_backward, stream, logits, R, grad_vals, normalize)
     dt = _dtype(logits, "logits")
-    with _on(stream, logits, R.colidx, R.vals, grad_vals):
-        x = _matrix(logits, "logits", R.nrows)
-        T, E = x.shape
-        k = R.nnz // T if T else 1
-        if E != R.ncols or k * T != R.nnz:
-            raise ValueError("R is not the routing matrix of these logits")
-        if grad_vals.dtype != torch.float32 or grad_vals.numel() != R.nnz or R.vals.dtype != torch.float32:
-            raise TypeError("grad_vals must be float32, one for every value of R")
-        g, vals = grad_vals.contiguous(), R.vals.contiguous()
-        out = torch.empty((T, E), dtype=x.dtype, device=x.device)
-        _abi.ws_topk_route_backward(x.data_ptr(), T, E, _ld(x), dt, k, normalize, R.colidx.data_ptr(),
-                                    vals.data_ptr(), g.data_ptr(), out.data_ptr(), E, _raw_stream(x.device))
+    x, ld = _matrix(logits, "logits", R.nrows)
+    T, E = x.shape
+    nnz = R.colidx.numel()
+    k = nnz // T if T else 1
+    if E != R.ncols or k * T != nnz:
+        raise ValueError("R is not the routing matrix of these logits")
+    vals = R.vals
+    if grad_vals.dtype != torch.float32 or grad_vals.numel() != nnz or vals.dtype != torch.float32:
+        raise TypeError("grad_vals must be float32, one for every value of R")
+    if grad_vals.device != x.device or R.colidx.dtype != torch.int32 or R.colidx.device != x.device:
+        raise TypeError("R and grad_vals must be on the logits' device")
+    g, vals, cols = grad_vals.contiguous(), vals.contiguous(), R.colidx.contiguous()
+    out = torch.empty((T, E), dtype=x.dtype, device=x.device)
+    _abi.ws_topk_route_backward(x.data_ptr(), T, E, ld, dt, k, normalize, cols.data_ptr(), vals.data_ptr(),
+                                g.data_ptr(), out.data_ptr(), E, _raw_stream(x.device.index))
     return out
+
+
+@functools.lru_cache(maxsize=256)
+def _scratch(nrows: int, ncols: int, device: int) -> int:
+    return _abi.ws_routing_scratch(nrows, ncols)
 
 
 class Routing:
@@ -128,31 +139,34 @@ class Routing:
     """
 
     def __init__(self, R: DeviceCSR, validate: bool = False, stream=None):
-        if R.vals.dtype != torch.float32:
-            raise TypeError(f"a routing matrix has float32 values, got {R.vals.dtype}")
-        for t, dt in ((R.rowptr, torch.int64), (R.colidx, torch.int32), (R.vals, torch.float32)):
-            if t.dtype != dt or not t.is_cuda or not t.is_contiguous():
-                raise TypeError("rowptr/colidx/vals must be contiguous CUDA int64/int32/float32 tensors")
-        nnz, E = R.colidx.numel(), R.ncols
-        if R.rowptr.numel() != R.nrows + 1 or R.vals.numel() != nnz:
+        if stream is not None:
+            _elsewhere(self.__init__, stream, R, validate)
+            return
+        rowptr, colidx, vals = R.rowptr, R.colidx, R.vals
+        if vals.dtype != torch.float32:
+            raise TypeError(f"a routing matrix has float32 values, got {vals.dtype}")
+        if rowptr.dtype != torch.int64 or colidx.dtype != torch.int32 or \
+                not (rowptr.is_cuda and colidx.is_cuda and vals.is_cuda) or \
+                not (rowptr.is_contiguous() and colidx.is_contiguous() and vals.is_contiguous()):
+            raise TypeError("rowptr/colidx/vals must be contiguous CUDA int64/int32/float32 tensors")
+        nnz, T, E = colidx.numel(), R.nrows, R.ncols
+        if rowptr.numel() != T + 1 or vals.numel() != nnz:
             raise ValueError("rowptr must have nrows + 1 entries, and every column index a value")
-        self.R, self.nnz, self.device = R, nnz, R.rowptr.device
-        with _on(stream, R.rowptr, R.colidx, R.vals):
-            raw = _raw_stream(self.device)
-            if validate:
-                _abi.ws_csr_destroy(R._handle(True, raw))
-            scratch = _abi.ws_routing_scratch(R.nrows, E)
-            # offsets, then rows, entries and slots, the status word, the scratch
-            words = 2 * (E + 1) + 3 * nnz + 1
-            self._buf = torch.empty(words + scratch // 4, dtype=torch.int32, device=self.device)
-            at = self._buf.data_ptr()
-            rows = at + 8 * (E + 1)
-            self._c = _abi.WsRouting(R.nrows, E, nnz, R.rowptr.data_ptr(), R.colidx.data_ptr() or None,
-                                     R.vals.data_ptr() or None, at, rows, rows + 4 * nnz, rows + 8 * nnz,
-                                     rows + 12 * nnz)
-            self._r = ctypes.byref(self._c)
-            self._stream = raw
-            _abi.ws_routing_build(self._r, at + 4 * words, scratch, raw)
+        self.R, self.nnz, self.device = R, nnz, rowptr.device
+        self._index = self.device.index
+        self._stream = raw = _raw_stream(self._index)
+        if validate:
+            _abi.ws_csr_destroy(R._handle(True, raw))
+        scratch = _scratch(T, E, self._index)
+        # offsets, then rows, entries and slots, the status word, the scratch
+        words = 2 * (E + 1) + 3 * nnz + 1
+        self._buf = torch.empty(words + scratch // 4, dtype=torch.int32, device=self.device)
+        at = self._buf.data_ptr()
+        rows = at + 8 * (E + 1)
+        self._c = _abi.WsRouting(T, E, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), at, rows,
+                                 rows + 4 * nnz, rows + 8 * nnz, rows + 12 * nnz)
+        self._r = ctypes.byref(self._c)
+        _abi.ws_routing_build(self._r, at + 4 * words, scratch, raw)
 
     def _ints(self, i: int) -> torch.Tensor:
         at = 2 * (self.R.ncols + 1) + i * self.nnz
@@ -174,109 +188,117 @@ class Routing:
     def slots(self) -> torch.Tensor:
         return self._ints(2)
 
-    def _queue(self) -> int:
-        """The current stream; the plan's arrays stay allocated until it is done with them."""
-        raw = _raw_stream(self.device)
+    def _queue(self, t: torch.Tensor) -> int:
+        """The current stream, for a call with t; the plan's arrays stay allocated until it is done with them."""
+        if t.device.index != self._index:
+            raise TypeError("the rows and the routing matrix must be on one device")
+        raw = _raw_stream(self._index)
         if raw != self._stream:
             s = torch.cuda.current_stream(self.device)
-            for t in (self._buf, self.R.rowptr, self.R.colidx, self.R.vals):
-                t.record_stream(s)
+            for u in (self._buf, self.R.rowptr, self.R.colidx, self.R.vals):
+                u.record_stream(s)
         return raw
 
     def dispatch(self, x: torch.Tensor, stream=None) -> torch.Tensor:
         """xs[slot] = x[row]: the rows of x (T x H) in slot order (nnz x H)."""
+        if stream is not None:
+            return _elsewhere(self.dispatch, stream, x)
         dt = _dtype(x, "x")
-        with _on(stream, x):
-            x = _matrix(x, "x", self.R.nrows)
-            H = x.shape[1]
-            out = torch.empty((self.nnz, H), dtype=x.dtype, device=x.device)
-            _abi.ws_routing_dispatch(self._r, x.data_ptr(), _ld(x), out.data_ptr(), H, H, dt, self._queue())
+        x, ld = _matrix(x, "x", self.R.nrows)
+        H = x.shape[1]
+        out = torch.empty((self.nnz, H), dtype=x.dtype, device=self.device)
+        _abi.ws_routing_dispatch(self._r, x.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue(x))
         return out
 
     def dispatch_backward(self, grad_xs: torch.Tensor, stream=None) -> torch.Tensor:
         """Gradient of x: gx[i] = sum of grad_xs over the slots of row i."""
+        if stream is not None:
+            return _elsewhere(self.dispatch_backward, stream, grad_xs)
         dt = _dtype(grad_xs, "grad_xs")
-        with _on(stream, grad_xs):
-            g = _matrix(grad_xs, "grad_xs", self.nnz)
-            H = g.shape[1]
-            out = torch.empty((self.R.nrows, H), dtype=g.dtype, device=g.device)
-            _abi.ws_routing_dispatch_backward(self._r, g.data_ptr(), _ld(g), out.data_ptr(), H, H, dt, self._queue())
+        g, ld = _matrix(grad_xs, "grad_xs", self.nnz)
+        H = g.shape[1]
+        out = torch.empty((self.R.nrows, H), dtype=g.dtype, device=self.device)
+        _abi.ws_routing_dispatch_backward(self._r, g.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue(g))
         return out
 
     def combine(self, ys: torch.Tensor, stream=None) -> torch.Tensor:
         """y[i] = sum over row i of R's value times ys[slot]."""
+        if stream is not None:
+            return _elsewhere(self.combine, stream, ys)
         dt = _dtype(ys, "ys")
-        with _on(stream, ys):
-            ys = _matrix(ys, "ys", self.nnz)
-            H = ys.shape[1]
-            out = torch.empty((self.R.nrows, H), dtype=ys.dtype, device=ys.device)
-            _abi.ws_routing_combine(self._r, ys.data_ptr(), _ld(ys), out.data_ptr(), H, H, dt, self._queue())
+        ys, ld = _matrix(ys, "ys", self.nnz)
+        H = ys.shape[1]
+        out = torch.empty((self.R.nrows, H), dtype=ys.dtype, device=self.device)
+        _abi.ws_routing_combine(self._r, ys.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue(ys))
         return out
 
     def combine_backward(self, grad_y: torch.Tensor, ys: torch.Tensor, stream=None):
         """Gradients of ys (value times grad_y's row) and of R's values (the products of grad_y's and ys's rows)."""
+        if stream is not None:
+            return _elsewhere(self.combine_backward, stream, grad_y, ys)
         dt = _dtype(ys, "ys")
-        with _on(stream, ys, grad_y):
-            ys = _matrix(ys, "ys", self.nnz)
-            g = _matrix(grad_y, "grad_y", self.R.nrows, ys)
-            H = ys.shape[1]
-            if g.shape[1] != H:
-                raise ValueError("grad_y and ys differ in the length of their rows")
-            out = torch.empty((self.nnz, H), dtype=ys.dtype, device=ys.device)
-            gvals = torch.empty(self.nnz, dtype=torch.float32, device=ys.device)
-            _abi.ws_routing_combine_backward(self._r, g.data_ptr(), _ld(g), ys.data_ptr(), _ld(ys), out.data_ptr(), H,
-                                             gvals.data_ptr(), H, dt, self._queue())
+        _same(grad_y, ys, "grad_y")
+        ys, ld = _matrix(ys, "ys", self.nnz)
+        g, ldg = _matrix(grad_y, "grad_y", self.R.nrows)
+        H = ys.shape[1]
+        if g.shape[1] != H:
+            raise ValueError("grad_y and ys differ in the length of their rows")
+        out = torch.empty((self.nnz, H), dtype=ys.dtype, device=self.device)
+        gvals = torch.empty(self.nnz, dtype=torch.float32, device=self.device)
+        _abi.ws_routing_combine_backward(self._r, g.data_ptr(), ldg, ys.data_ptr(), ld, out.data_ptr(), H,
+                                         gvals.data_ptr(), H, dt, self._queue(ys))
         return out, gvals
 
     def _experts(self, W: torch.Tensor, like: torch.Tensor):
         if W.dim() != 3 or W.shape[0] != self.R.ncols:
             raise ValueError(f"W must be {self.R.ncols} matrices, got {tuple(W.shape)}")
-        if W.dtype != like.dtype or W.device != like.device:
-            raise TypeError("W must have the rows' type and device")
-        W = _operand(W)
-        return W, W.stride(0) if W.shape[0] > 1 else W.shape[1] * _ld8(W)
+        _same(W, like, "W")
+        return _operand(W)
 
     def matmul(self, xs: torch.Tensor, W: torch.Tensor, stream=None) -> torch.Tensor:
         """ys[s] = W[e] xs[s] for the rows s of every column e: xs nnz x K in slot order, W E x N x K, bfloat16 or
         float16; products and sums in 32 bits, rounded once.  Rows behind the placed entries are left unwritten."""
+        if stream is not None:
+            return _elsewhere(self.matmul, stream, xs, W)
         dt = _dtype(xs, "xs")
-        with _on(stream, xs, W):
-            xs = _operand(_matrix(xs, "xs", self.nnz))
-            W, apart = self._experts(W, xs)
-            (_, N, K), Z = W.shape, self.nnz
-            if xs.shape[1] != K:
-                raise ValueError(f"rows of {xs.shape[1]} values do not fit matrices of {K} columns")
-            out = torch.empty((Z, N), dtype=xs.dtype, device=xs.device)
-            _abi.ws_routing_matmul(self._r, xs.data_ptr(), _ld8(xs), W.data_ptr(), _ld8(W), apart, N, K,
-                                   out.data_ptr(), N, dt, self._queue())
+        xs, ldx, _ = _operand(_matrix(xs, "xs", self.nnz)[0])
+        W, ldw, apart = self._experts(W, xs)
+        (_, N, K), Z = W.shape, self.nnz
+        if xs.shape[1] != K:
+            raise ValueError(f"rows of {xs.shape[1]} values do not fit matrices of {K} columns")
+        out = torch.empty((Z, N), dtype=xs.dtype, device=self.device)
+        _abi.ws_routing_matmul(self._r, xs.data_ptr(), ldx, W.data_ptr(), ldw, apart, N, K, out.data_ptr(), N, dt,
+                               self._queue(xs))
         return out
 
     def matmul_backward(self, grad_ys: torch.Tensor, xs: torch.Tensor, W: torch.Tensor, stream=None):
         """Gradients of xs (W[e]^T grad_ys[s]) and of W (sum over the rows of e of grad_ys[s] xs[s]^T; zero for a
         column without entries), in their types."""
+        if stream is not None:
+            return _elsewhere(self.matmul_backward, stream, grad_ys, xs, W)
         dt = _dtype(xs, "xs")
-        with _on(stream, grad_ys, xs, W):
-            xs = _operand(_matrix(xs, "xs", self.nnz))
-            g = _operand(_matrix(grad_ys, "grad_ys", self.nnz, xs))
-            W, apart = self._experts(W, xs)
-            (E, N, K), Z, raw = W.shape, self.nnz, self._queue()
-            if xs.shape[1] != K or g.shape[1] != N:
-                raise ValueError(f"rows of {xs.shape[1]} and {g.shape[1]} values do not fit matrices {N} x {K}")
-            gxs = torch.empty((Z, K), dtype=xs.dtype, device=xs.device)
-            gW = torch.empty((E, N, K), dtype=xs.dtype, device=xs.device)
-            _abi.ws_routing_matmul_rows(self._r, g.data_ptr(), _ld8(g), W.data_ptr(), _ld8(W), apart, N, K,
-                                        gxs.data_ptr(), K, dt, raw)
-            _abi.ws_routing_matmul_weights(self._r, g.data_ptr(), _ld8(g), xs.data_ptr(), _ld8(xs), N, K,
-                                           gW.data_ptr(), K, N * K, dt, raw)
+        _same(grad_ys, xs, "grad_ys")
+        xs, ldx, _ = _operand(_matrix(xs, "xs", self.nnz)[0])
+        g, ldg, _ = _operand(_matrix(grad_ys, "grad_ys", self.nnz)[0])
+        W, ldw, apart = self._experts(W, xs)
+        (E, N, K), Z, raw = W.shape, self.nnz, self._queue(xs)
+        if xs.shape[1] != K or g.shape[1] != N:
+            raise ValueError(f"rows of {xs.shape[1]} and {g.shape[1]} values do not fit matrices {N} x {K}")
+        gxs = torch.empty((Z, K), dtype=xs.dtype, device=self.device)
+        gW = torch.empty((E, N, K), dtype=xs.dtype, device=self.device)
+        _abi.ws_routing_matmul_rows(self._r, g.data_ptr(), ldg, W.data_ptr(), ldw, apart, N, K, gxs.data_ptr(), K, dt,
+                                    raw)
+        _abi.ws_routing_matmul_weights(self._r, g.data_ptr(), ldg, xs.data_ptr(), ldx, N, K, gW.data_ptr(), K, N * K,
+                                       dt, raw)
         return gxs, gW
 
     def wait(self, stream=None) -> None:
         """Waits for the stream and raises if a product's kernel gave up a wait since the plan was built."""
-        with _on(stream):
-            self._queue()
-            torch.cuda.current_stream(self.device).synchronize()
-        at = 2 * (self.R.ncols + 1) + 3 * self.nnz
-        if int(self._buf[at]):
+        if stream is not None:
+            return _elsewhere(self.wait, stream)
+        self._queue(self._buf)
+        torch.cuda.current_stream(self.device).synchronize()
+        if int(self._buf[2 * (self.R.ncols + 1) + 3 * self.nnz]):
             raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
 
 
@@ -288,42 +310,49 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     x: T x K, A: L x r x K, B: L x N x r, base: T x N, bfloat16 or float16; S: T x L in CSR, float32 values, rows empty
     for tokens without an adapter.  ``out`` may be ``base``: the adapters' part is then added in place.
     """
+    if stream is not None:
+        return _elsewhere(adapters, stream, x, A, B, S, base, out)
     dt = _dtype(x, "x")
-    if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+    (La, r, K), (L, N, rb) = A.shape, B.shape
+    if La != L or r != rb:
         raise ValueError(f"A must be L x r x K and B L x N x r, got {tuple(A.shape)} and {tuple(B.shape)}")
-    (L, r, K), N, T = A.shape, B.shape[1], S.nrows
-    if A.dtype != x.dtype or B.dtype != x.dtype or A.device != x.device or B.device != x.device:
-        raise TypeError("x, A and B must have one type and device")
-    for t, d in ((S.rowptr, torch.int64), (S.colidx, torch.int32), (S.vals, torch.float32)):
-        if t.dtype != d or t.device != x.device or not t.is_contiguous():
-            raise TypeError("S must hold contiguous int64/int32/float32 tensors on x's device")
-    nnz = S.colidx.numel()
-    if S.ncols != L or S.rowptr.numel() != T + 1 or S.vals.numel() != nnz:
+    _same(A, x, "A")
+    _same(B, x, "B")
+    rowptr, colidx, vals, dev, T = S.rowptr, S.colidx, S.vals, x.device, S.nrows
+    if rowptr.dtype != torch.int64 or colidx.dtype != torch.int32 or vals.dtype != torch.float32 or \
+            not (rowptr.is_contiguous() and colidx.is_contiguous() and vals.is_contiguous()) or \
+            not rowptr.device == colidx.device == vals.device == dev:
+        raise TypeError("S must hold contiguous int64/int32/float32 tensors on x's device")
+    nnz = colidx.numel()
+    if S.ncols != L or rowptr.numel() != T + 1 or vals.numel() != nnz:
         raise ValueError(f"S must be {x.shape[0]} x {L} in CSR")
-    with _on(stream, x, A, B, S.rowptr, S.colidx, S.vals, *(() if base is None else (base,))):
-        x = _operand(_matrix(x, "x", T))
-        if x.shape[1] != K:
-            raise ValueError(f"rows of {x.shape[1]} values do not fit adapters of {K}")
-        A = _operand(A)
-        if (r > 1 and B.stride(2) != 1) or (N > 1 and B.stride(1) < r):
-            B = B.contiguous()
-        if base is not None:
-            base = _matrix(base, "base", T, x)
-            if base.shape[1] != N:
-                raise ValueError(f"base must be {T} x {N}")
-        if out is None:
-            out = torch.empty((T, N), dtype=x.dtype, device=x.device)
-        elif _matrix(out, "out", T, x) is not out or out.shape[1] != N:
+    x, ldx, _ = _operand(_matrix(x, "x", T)[0])
+    if x.shape[1] != K:
+        raise ValueError(f"rows of {x.shape[1]} values do not fit adapters of {K}")
+    A, lda, apart = _operand(A)
+    if not B.is_contiguous() and ((r > 1 and B.stride(2) != 1) or (N > 1 and B.stride(1) < r)):
+        B = B.contiguous()
+    ldbase = ldy = N
+    if base is not None:
+        _same(base, x, "base")
+        base, ldbase = _matrix(base, "base", T)
+        if base.shape[1] != N:
+            raise ValueError(f"base must be {T} x {N}")
+    if out is None:
+        out = torch.empty((T, N), dtype=x.dtype, device=dev)
+    else:
+        _same(out, x, "out")
+        same, ldy = _matrix(out, "out", T)
+        if same is not out or out.shape[1] != N:
             raise ValueError(f"out must be {T} x {N} with unit stride within its rows")
-        elif base is not None and _overlap(out, base) and (out.data_ptr(), _ld(out)) != (base.data_ptr(), _ld(base)):
+        if base is not None and (out.data_ptr(), ldy) != (base.data_ptr(), ldbase) and _overlap(out, base):
             raise ValueError("out must be base itself or lie apart from it")
-        need = _abi.ws_adapters_scratch(nnz, r)
-        scratch = torch.empty(need, dtype=torch.uint8, device=x.device)
-        call = _abi.WsAdaptersCall(T, L, nnz, S.rowptr.data_ptr(), S.colidx.data_ptr(), S.vals.data_ptr(), K, r, N,
-                                   x.data_ptr(), _ld8(x), A.data_ptr(), _ld8(A), A.stride(0), B.data_ptr(),
-                                   B.stride(1), B.stride(0), 0 if base is None else base.data_ptr(),
-                                   0 if base is None else _ld(base), out.data_ptr(), _ld(out), dt)
-        _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(x.device))
+    need = nnz * ((r + 15) // 16 * 64)  # ws_adapters_scratch
+    scratch = torch.empty(need, dtype=torch.uint8, device=dev)
+    call = _abi.ADAPTERS_CALL.pack(T, L, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), K, r, N,
+                                   x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), B.stride(1), B.stride(0),
+                                   0 if base is None else base.data_ptr(), ldbase, out.data_ptr(), ldy, dt)
+    _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(dev.index))
     return out
 
 

@@ -162,6 +162,12 @@ def test_no_rows():
     assert plan.matmul(x, W).shape == (0, 24)
     gxs, gW = plan.matmul_backward(torch.empty((0, 24), dtype=torch.bfloat16, device="cuda"), x, W)
     assert gxs.shape == (0, 16) and bool((gW == 0).all())
+    plan = _plan([2, 0, 3])
+    for N, K in ((8, 0), (0, 8), (0, 0)):
+        x, W = torch.ones((5, K), dtype=torch.bfloat16, device="cuda"), torch.ones((3, N, K), dtype=torch.bfloat16, device="cuda")
+        assert torch.equal(plan.matmul(x, W), torch.zeros((5, N), dtype=torch.bfloat16, device="cuda"))
+        gxs, gW = plan.matmul_backward(torch.ones((5, N), dtype=torch.bfloat16, device="cuda"), x, W)
+        assert torch.equal(gxs, torch.zeros((5, K), dtype=torch.bfloat16, device="cuda")) and gW.shape == (3, N, K)
 
 
 def test_equal_inputs_give_equal_bits():
