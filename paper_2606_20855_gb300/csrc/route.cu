@@ -21,9 +21,10 @@ namespace {
 constexpr int kRouteWarps = 8;
 
 // Order of floats as unsigned numbers: NaN last of all, -0 as +0; 0 is below -inf and marks "no logit".
+// Adding zero makes -0 positive and any NaN the canonical one, 0x7fffffff.
 __device__ __forceinline__ uint32_t order_key(float f) {
-  const uint32_t u = __float_as_uint(f + 0.0f);
-  return f != f ? 0xffffffffu : u & 0x80000000u ? ~u : u | 0x80000000u;
+  const uint32_t u = __float_as_uint(__fadd_rn(f, 0.0f));
+  return u ^ (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u);
 }
 
 // V consecutive logits of a row from column `at` on; -inf and key 0 past the row's end.
@@ -45,7 +46,7 @@ __device__ __forceinline__ void load_row(const T* row, int at, int cols, bool ve
 }
 
 __device__ __forceinline__ float key_value(uint32_t key) {
-  return key == 0xffffffffu ? NAN : __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
+  return __uint_as_float(key ^ (static_cast<uint32_t>(static_cast<int>(~key) >> 31) | 0x80000000u));
 }
 
 // A warp per row; a lane holds V consecutive logits, so that among equal
@@ -75,6 +76,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
   uint32_t my_key = key[0];  // the lane's candidate
   int my_col = lane;
   bool one_each = V == 1;
+  int all = 32;  // candidates
   if constexpr (V > 1) {
     uint32_t best = key[0];
 #pragma unroll
@@ -94,7 +96,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
       const int y = __shfl_up_sync(0xffffffffu, upto, o);
       if (lane >= o) upto += y;
     }
-    const int all = __shfl_sync(0xffffffffu, upto, 31);
+    all = __shfl_sync(0xffffffffu, upto, 31);
     one_each = all <= 32;
     if (one_each) {
       int at = upto - mine;
@@ -110,10 +112,14 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
   bool chosen = false;
   int rank;
   if (one_each) {
-    uint32_t left = my_key;
-    for (int r = 0; r < k; ++r) {
-      const uint32_t top = __reduce_max_sync(0xffffffffu, left);
-      if (lane == __ffs(__ballot_sync(0xffffffffu, left == top)) - 1) left = 0, chosen = true;
+    if (all == k) {
+      chosen = lane < k;
+    } else {
+      uint32_t left = my_key;
+      for (int r = 0; r < k; ++r) {
+        const uint32_t top = __reduce_max_sync(0xffffffffu, left);
+        if (lane == __ffs(__ballot_sync(0xffffffffu, left == top)) - 1) left = 0, chosen = true;
+      }
     }
     rank = __popc(__ballot_sync(0xffffffffu, chosen) & ((1u << lane) - 1u));
   } else {

@@ -117,7 +117,7 @@ void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cud
 void launch_dispatch(const ws_routing& r, const void* x, int64_t ldx, void* xs, int64_t ldxs, int64_t width,
                      ws_dtype_t dt, cudaStream_t s);
 void launch_combine(const ws_routing& r, bool weighted, const void* ys, int64_t ldys, void* y, int64_t ldy,
-                    int64_t width, ws_dtype_t dt, cudaStream_t s);
+                    int64_t width, ws_dtype_t dt, int num_sms, cudaStream_t s);
 void launch_combine_backward(const ws_routing& r, const void* gy, int64_t ldgy, const void* ys, int64_t ldys,
                              void* gys, int64_t ldgys, float* gvals, int64_t width, ws_dtype_t dt, cudaStream_t s);
 

@@ -173,7 +173,9 @@ ws_status_t ws_routing_dispatch_backward(const ws_routing* r, const void* gxs, i
                                          int64_t width, ws_dtype_t dtype, ws_stream_t stream) {
   if (const ws_status_t st = check_rows(r, width, dtype, {{gxs, r ? r->nnz : 0, ldgxs}, {gx, r ? r->nrows : 0, ldgx}})) return st;
   if (r->nrows == 0 || width == 0) return WS_OK;
-  launch_combine(*r, false, gxs, ldgxs, gx, ldgx, width, dtype, cuda_stream(stream));
+  int sms = 0;
+  if (const ws_status_t st = sm_count(&sms)) return st;
+  launch_combine(*r, false, gxs, ldgxs, gx, ldgx, width, dtype, sms, cuda_stream(stream));
   return launched("ws_routing_dispatch_backward");
 }
 
@@ -182,7 +184,9 @@ ws_status_t ws_routing_combine(const ws_routing* r, const void* ys, int64_t ldys
   if (const ws_status_t st = check_rows(r, width, dtype, {{ys, r ? r->nnz : 0, ldys}, {y, r ? r->nrows : 0, ldy}})) return st;
   if (r->nnz > 0 && !r->vals) return routing_fail(WS_ERR_INVALID_ARG, "NULL values");
   if (r->nrows == 0 || width == 0) return WS_OK;
-  launch_combine(*r, true, ys, ldys, y, ldy, width, dtype, cuda_stream(stream));
+  int sms = 0;
+  if (const ws_status_t st = sm_count(&sms)) return st;
+  launch_combine(*r, true, ys, ldys, y, ldy, width, dtype, sms, cuda_stream(stream));
   return launched("ws_routing_combine");
 }
 

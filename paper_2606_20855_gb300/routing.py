@@ -158,35 +158,30 @@ class Routing:
         if validate:
             _abi.ws_csr_destroy(R._handle(True, raw))
         scratch = _scratch(T, E, self._index)
-        # offsets, then rows, entries and slots, the status word, the scratch
-        words = 2 * (E + 1) + 3 * nnz + 1
-        self._buf = torch.empty(words + scratch // 4, dtype=torch.int32, device=self.device)
-        at = self._buf.data_ptr()
-        rows = at + 8 * (E + 1)
-        self._c = _abi.WsRouting(T, E, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), at, rows,
-                                 rows + 4 * nnz, rows + 8 * nnz, rows + 12 * nnz)
+        # offsets, the status word, the scratch; rows, entries and slots
+        self._buf = torch.empty(E + 2 + (scratch + 7) // 8, dtype=torch.int64, device=self.device)
+        self._ints = torch.empty((3, nnz), dtype=torch.int32, device=self.device)
+        at, ints = self._buf.data_ptr(), self._ints.data_ptr()
+        self._c = _abi.WsRouting(T, E, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), at, ints,
+                                 ints + 4 * nnz, ints + 8 * nnz, at + 8 * (E + 1))
         self._r = ctypes.byref(self._c)
-        _abi.ws_routing_build(self._r, at + 4 * words, scratch, raw)
-
-    def _ints(self, i: int) -> torch.Tensor:
-        at = 2 * (self.R.ncols + 1) + i * self.nnz
-        return self._buf[at:at + self.nnz]
+        _abi.ws_routing_build(self._r, at + 8 * (E + 2), scratch, raw)
 
     @property
     def offsets(self) -> torch.Tensor:
-        return self._buf[:2 * (self.R.ncols + 1)].view(torch.int64)
+        return self._buf[:self.R.ncols + 1]
 
     @property
     def rows(self) -> torch.Tensor:
-        return self._ints(0)
+        return self._ints[0]
 
     @property
     def entries(self) -> torch.Tensor:
-        return self._ints(1)
+        return self._ints[1]
 
     @property
     def slots(self) -> torch.Tensor:
-        return self._ints(2)
+        return self._ints[2]
 
     def _queue(self, t: torch.Tensor) -> int:
         """The current stream, for a call with t; the plan's arrays stay allocated until it is done with them."""
@@ -195,7 +190,7 @@ class Routing:
         raw = _raw_stream(self._index)
         if raw != self._stream:
             s = torch.cuda.current_stream(self.device)
-            for u in (self._buf, self.R.rowptr, self.R.colidx, self.R.vals):
+            for u in (self._buf, self._ints, self.R.rowptr, self.R.colidx, self.R.vals):
                 u.record_stream(s)
         return raw
 
@@ -298,7 +293,7 @@ class Routing:
             return _elsewhere(self.wait, stream)
         self._queue(self._buf)
         torch.cuda.current_stream(self.device).synchronize()
-        if int(self._buf[2 * (self.R.ncols + 1) + 3 * self.nnz]):
+        if int(self._buf[self.R.ncols + 1]) & 0xFFFFFFFF:
             raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
 
 
