@@ -409,7 +409,7 @@ typedef struct ws_routing {
 /*
  * ws_routing_build -- fills offsets, rows, entries and slots: the entries of R
  * sorted by column, rows in order within a column.  `scratch` holds
- * ws_routing_scratch(nrows, ncols) bytes (0 for few rows: NULL then).
+ * ws_routing_scratch(nrows, ncols) bytes, 16-byte aligned (0 for few rows: NULL then).
  */
 int64_t ws_routing_scratch(int64_t nrows, int64_t ncols);
 ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch_bytes, ws_stream_t stream);
@@ -460,11 +460,14 @@ ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int6
  * S is an nrows x ncols CSR matrix, tokens x adapters (columns strictly
  * increasing within a row; rows may be empty; entries whose column is out of
  * range take no part).  bfloat16 or half; inner products A[a] x[t] are summed in
- * 32 bits and kept as pairs of 16-bit values (for half up to 65504), the result
- * is summed in 32 bits and rounded once.  x and A start and have strides at
- * multiples of 16 bytes.  base may be NULL (zero) and may be y itself.
- * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned.  Queued on
- * `stream`; nothing is allocated.
+ * 32 bits and, times the value, kept as pairs of 16-bit values (for half up to
+ * 65504), the result is summed in 32 bits and rounded once.  "Many tokens":
+ * nrows times r, rounded up to a multiple of 16, is above 8192.  x and A, and
+ * for many tokens B, start and have strides at multiples of 16 bytes.  base may
+ * be NULL (zero) and may be y itself.
+ * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned; for
+ * many tokens and nnz > 0 its first int is 0 after the call, or nonzero if a
+ * kernel's bounded waits ran out.  Queued on `stream`; nothing is allocated.
  */
 typedef struct ws_adapters_call {
   int64_t nrows, ncols, nnz;

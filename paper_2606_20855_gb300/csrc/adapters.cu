@@ -4,35 +4,31 @@
 // for most), A: adapters x rank x K, B: adapters x N x rank, 16-bit; base is the
 // shared projection's result.
 //
-// Two kernels: inner products h = v A[a] x[t] for every entry of S, then
-// y = base + B[a] h.  Both are bound by memory (x, base and y, and the met
+// Two kernels: inner products h = A[a] x[t] for every entry of S, then
+// y = base + B[a] (v h).  Both are bound by memory (x, base and y, and the met
 // adapters, once each; 2 rank multiply-adds per value), so h stays small: sums
-// are 32-bit, and h is kept as a pair of 16-bit values, its rounding and the
+// are 32-bit, and where v h meets B on the tensor cores it is a pair of 16-bit values, its rounding and the
 // rounding of what that left over, 16 (bfloat16) or 22 (half) significant bits.
 // One 16-bit value would add an error as large as the result's own rounding.
-// A half pair holds |h| up to 65504.
+// A half pair holds |v h| up to 65504.
 //
-// Few tokens ("step"): every token is on its own; a warp per entry and pair of
-// ranks, then a thread per value of y: everything in flight at once, no
-// reuse.  Many tokens ("prompt"): tiles of 32 tokens on the warp-level matrix
-// instruction.  The tokens of a tile mostly share an adapter, and the tile goes
-// through the adapters it meets in ascending order: every lane stands at its
-// token's first entry, the smallest column among the lanes is next, and the
-// lanes that have it move on (columns ascend within a row).  The matrix
-// instruction's operands go from global memory to registers in 16-byte loads:
-// the order of the contraction index is free as long as both operands agree, so
-// a lane's eight neighbouring values serve as the pairs of two instructions.
+// Few tokens ("step"): every token is on its own, its inner products split over warps, then
+// a thread per value of y: everything in flight at once, no
+// reuse.  Many tokens ("prompt"): tiles of 128 tokens on the tcgen05 tensor cores, x, A, B, base and y moved by the copy engine.
+// The tokens of a tile mostly share an adapter, and the tile goes
+// through the adapters it meets in ascending order: every thread stands at its
+// token's first entry, the smallest column among the threads is next, and the
+// threads that have it move on (columns ascend within a row).
 #include <climits>
-#include <type_traits>
 
 #include "routing.cuh"
+#include "tensor.cuh"
 
 namespace wsk {
 namespace {
 
 constexpr int kAdThreads = 256;
 constexpr int kAdWarps = kAdThreads / 32;
-constexpr int kTileTok = 32;
 
 // h as {roundings, remainders} of two neighbouring ranks.
 template <bool half>
@@ -43,13 +39,6 @@ __device__ __forceinline__ uint2 split_pair(float a, float b) {
   const uint16_t la = bits16<half>(ra == ra && fabsf(ra) <= 3.4e38f ? ra : 0.0f);
   const uint16_t lb = bits16<half>(rb == rb && fabsf(rb) <= 3.4e38f ? rb : 0.0f);
   return make_uint2(ha | static_cast<uint32_t>(hb) << 16, la | static_cast<uint32_t>(lb) << 16);
-}
-
-// d += (roundings + remainders of h, rows a and b) times v.
-template <bool half>
-__device__ __forceinline__ void mma_pair(float (&d)[4], const uint4& a, const uint4& b, const uint2& v) {
-  mma16<half>(d, a.x, b.x, a.z, b.z, v.x, v.y);
-  mma16<half>(d, a.y, b.y, a.w, b.w, v.x, v.y);
 }
 
 // Ranks k .. k + 3 of a row of B, zero past its end.
@@ -93,215 +82,354 @@ struct Walk {
 
 // ---------------------------------------------------------------- many tokens
 
-// h of a tile of 32 tokens, 8 NR ranks from 8 NR blockIdx.y on; the warps take every eighth step of 32 values.
-// Rows that are not there (tokens past the last, ranks past r) repeat one that is; what comes of them is not used.
-template <bool half, int NR>
-__global__ void __launch_bounds__(kAdThreads, NR <= 4 ? 2 : 1) shrink_tile_kernel(const ws_adapters_call c, uint2* __restrict__ h, int rpad) {
-  extern __shared__ float red[];  // [warps][32][8 NR]
-  __shared__ int entry[kTileTok];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTileTok;
-  const int r0 = blockIdx.y * 8 * NR;
-  const int K = static_cast<int>(c.K), r = static_cast<int>(c.r);
-  Walk w;
-  w.start(c, t0 + lane);
-  const uint16_t* xrow[4];
+constexpr int kTok = 128;           // tokens of a tile: lanes of tensor memory
+constexpr int kRankBlock = 64;      // ranks, of one adapter or of several, that a pass over x takes
+constexpr int kShrinkStages = 8;
+constexpr int kShrinkStage = kTok * 128 + kRankBlock * 128;  // 64 values of x's and of A's rows
+constexpr int kShrinkThreads = 192;
+constexpr size_t kShrinkSmem = kShrinkStages * kShrinkStage + 1024;
+constexpr int kList = 64;           // adapters that a tile collects at once
+constexpr int kMaxSplit = 4;        // parts of K
+
+// The smallest column at which the CTA's tokens stand (INT_MAX: none).  All threads call it; those without a token with INT_MAX.
+template <int kWarps>
+__device__ __forceinline__ int next_adapter(int col, int* mins) {
+  const int m = __reduce_min_sync(0xffffffffu, col);
+  if ((threadIdx.x & 31) == 0) mins[threadIdx.x >> 5] = m;
+  __syncthreads();
+  int a = mins[0];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    xrow[i] = static_cast<const uint16_t*>(c.x) + min(t0 + 8 * i + g, c.nrows - 1) * c.ldx;
-  for (;;) {
-    const int a = __reduce_min_sync(0xffffffffu, w.col);
-    if (a == INT_MAX) break;
-    const bool mine = w.col == a;
-    if (warp == 0) entry[lane] = mine ? w.at : -1;
-    const uint16_t* A = static_cast<const uint16_t*>(c.A) + a * c.strideA;
-    const uint16_t* arow[NR];
-#pragma unroll
-    for (int j = 0; j < NR; ++j) arow[j] = A + min(r0 + 8 * j + g, r - 1) * c.lda;
-    float acc[2][NR][4] = {};
-    const auto step = [&](const uint4(&xv)[4], const uint4(&av)[NR]) {
-#pragma unroll
-      for (int m = 0; m < 2; ++m)
-#pragma unroll
-        for (int j = 0; j < NR; ++j) {
-          mma16<half>(acc[m][j], xv[2 * m].x, xv[2 * m + 1].x, xv[2 * m].y, xv[2 * m + 1].y, av[j].x, av[j].y);
-          mma16<half>(acc[m][j], xv[2 * m].z, xv[2 * m + 1].z, xv[2 * m].w, xv[2 * m + 1].w, av[j].z, av[j].w);
-        }
-    };
-    int k = 32 * warp + 8 * q;
-    constexpr int U = NR <= 4 ? 2 : 1;  // steps whose loads are in flight together
-    for (; k - 8 * q + 32 * kAdWarps * (U - 1) + 32 <= K; k += 32 * kAdWarps * U) {
-      uint4 xv[U][4], av[U][NR];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) xv[u][i] = *reinterpret_cast<const uint4*>(xrow[i] + k + 32 * kAdWarps * u);
-#pragma unroll
-        for (int j = 0; j < NR; ++j) av[u][j] = *reinterpret_cast<const uint4*>(arow[j] + k + 32 * kAdWarps * u);
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) step(xv[u], av[u]);
-    }
-#pragma unroll 1
-    for (; k - 8 * q < K; k += 32 * kAdWarps) {
-      uint4 xv[4], av[NR];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) xv[i] = load8(xrow[i], k, K);
-#pragma unroll
-      for (int j = 0; j < NR; ++j) av[j] = load8(arow[j], k, K);
-      step(xv, av);
-    }
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int j = 0; j < NR; ++j)
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          *reinterpret_cast<float2*>(red + ((warp * kTileTok) + 16 * m + 8 * i + g) * (8 * NR) + 8 * j + 2 * q) =
-              make_float2(acc[m][j][2 * i], acc[m][j][2 * i + 1]);
-    __syncthreads();
-    for (int i = threadIdx.x; i < kTileTok * 4 * NR; i += kAdThreads) {
-      const int tok = i / (4 * NR), pair = i - tok * (4 * NR);
-      if (entry[tok] < 0 || r0 + 2 * pair >= rpad) continue;
-      float s0 = 0.0f, s1 = 0.0f;
-#pragma unroll
-      for (int k = 0; k < kAdWarps; ++k) {
-        const float2 f = *reinterpret_cast<const float2*>(red + (k * kTileTok + tok) * (8 * NR) + 2 * pair);
-        s0 += f.x;
-        s1 += f.y;
-      }
-      const float v = c.vals[entry[tok]];
-      h[static_cast<int64_t>(entry[tok]) * (rpad / 2) + r0 / 2 + pair] =
-          split_pair<half>(r0 + 2 * pair < r ? v * s0 : 0.0f, r0 + 2 * pair + 1 < r ? v * s1 : 0.0f);
-    }
-    __syncthreads();
-    if (mine) w.next(c);
-  }
+  for (int i = 1; i < kWarps; ++i) a = min(a, mins[i]);
+  __syncthreads();
+  return a;
 }
 
-// y of 32 tokens: a warp takes 64 values of each; in tile j of eight, column g of the instruction is value
-// 32 (j / 4) + 8 (g / 2) + 2 (j % 4) + g % 2, so that a lane ends up with two times eight neighbouring values of a row.
-template <bool half, bool vec>
-__global__ void __launch_bounds__(kAdThreads, 2)
-    expand_tile_kernel(const ws_adapters_call c, const uint2* __restrict__ h, int rpad, bool vecB) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
-  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTileTok;
-  const int N = static_cast<int>(c.N), r = static_cast<int>(c.r);
-  const int n0 = (blockIdx.y * kAdWarps + warp) * 64;
-  if (n0 >= N) return;
-  const uint16_t* base = static_cast<const uint16_t*>(c.base);
-  uint4 bv16[4][2];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {  // rows g, g + 8, g + 16, g + 24
-    const int64_t t = t0 + 8 * i + g;
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int n = n0 + 32 * s + 8 * q;
-      if (vec) {  // rows start at multiples of 16 bytes and N is a multiple of 8
-        bv16[i][s] = base && t < c.nrows && n < N ? *reinterpret_cast<const uint4*>(base + t * c.ldbase + n) : make_uint4(0, 0, 0, 0);
-      } else {
-        uint32_t v[4] = {};
-        if (base && t < c.nrows)
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (n + e < N) v[e >> 1] |= static_cast<uint32_t>(base[t * c.ldbase + n + e]) << (16 * (e & 1));
-        bv16[i][s] = make_uint4(v[0], v[1], v[2], v[3]);
-      }
+// h of 128 tokens over one part of K: one lane fetches x's and A's values through a ring of stages, one multiplies (D: tokens x
+// ranks, two accumulators), a thread per token stores.  Adapters of up to 32 or 16 ranks go two or four to a pass: a tile at
+// the border of two requests then reads x once, like the others.  (8191 tokens of 4096 halves, rank 32: 24 us with
+// tiles of 32 tokens on the warp-level instruction, 29 us with a pass for each adapter, 19 us so.)
+__global__ void __launch_bounds__(kShrinkThreads, 1)
+    shrink_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
+                       const ws_adapters_call c, float* __restrict__ h, int rpad, int* status) {
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t full_bar[kShrinkStages], empty_bar[kShrinkStages], acc_full[2], acc_empty[2], last_bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int dead;
+  __shared__ int list[kList], mins[kShrinkThreads / 32];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTok;
+  const int r0 = blockIdx.z * kRankBlock, n = min(kRankBlock, rpad - r0);  // of one adapter
+  const int group = kRankBlock / min(kRankBlock, rpad);                      // adapters of a pass
+  const int all = static_cast<int>((c.K + 63) / 64);
+  const int k0 = static_cast<int>(static_cast<int64_t>(all) * blockIdx.y / gridDim.y);
+  const int k1 = static_cast<int>(static_cast<int64_t>(all) * (blockIdx.y + 1) / gridDim.y);
+  h += static_cast<int64_t>(blockIdx.y) * c.nnz * rpad;
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < kShrinkStages; ++i) {
+      bar_init(smem_u32(&full_bar[i]), 1);
+      bar_init(smem_u32(&empty_bar[i]), 1);
     }
+    for (int i = 0; i < 2; ++i) {
+      bar_init(smem_u32(&acc_full[i]), 1);
+      bar_init(smem_u32(&acc_empty[i]), 4);
+    }
+    bar_init(smem_u32(&last_bar), 1);
+    dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  float acc[2][8][4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const uint32_t v[4] = {bv16[i][s].x, bv16[i][s].y, bv16[i][s].z, bv16[i][s].w};
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        acc[i >> 1][4 * s + j][2 * (i & 1)] = value16<half>(static_cast<uint16_t>(v[j]));
-        acc[i >> 1][4 * s + j][2 * (i & 1) + 1] = value16<half>(static_cast<uint16_t>(v[j] >> 16));
-      }
-    }
-  Walk w;
-  w.start(c, t0 + lane);
+  if (warp == 1) tmem_alloc<2 * kRankBlock>(smem_u32(&tmem_slot));
+  // warps 2 .. 5: a token a thread, in the lanes of tensor memory that the warp may read
+  const int quarter = warp & 3, m = quarter * 32 + lane;
+  Walk ahead, behind;  // the list is made ahead of what the stores have come to
+  ahead.at = ahead.end = 0;
+  ahead.col = INT_MAX;
+  if (warp >= 2) ahead.start(c, t0 + m);
+  behind = ahead;
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+
+  int stage = 0, acc = 0;
+  uint32_t phase = 0, acc_phase = 0;
+  int filled = 0;
+  bool ok = true;
   for (;;) {
-    const int a = __reduce_min_sync(0xffffffffu, w.col);
-    if (a == INT_MAX) break;
-    const bool mine = w.col == a;
-    int entry[4];
+    int items = 0;
+    while (items < kList) {
+      const int a = next_adapter<kShrinkThreads / 32>(ahead.col, mins);
+      if (a == INT_MAX) break;
+      if (threadIdx.x == 0) list[items] = a;
+      if (ahead.col == a) ahead.next(c);
+      ++items;
+    }
+    __syncthreads();
+    if (items == 0) break;
+    if (warp == 0) {
+      if (lane == 0) {
+        for (int i = 0; ok && i < items; i += group) {
+          const int these = min(group, items - i);
+          for (int k = k0; k < k1; ++k) {
+            if (!bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead)) {
+              ok = false;
+              break;
+            }
+            const uint32_t bar = smem_u32(&full_bar[stage]), at = base + stage * kShrinkStage;
+            const int rows = min(kRankBlock, rpad);  // of the copy; past r they are zero
+            bar_expect(bar, kTok * 128 + these * rows * 128);
+            tma_2d(at, &map_x, 64 * k, static_cast<int>(t0), bar);
+            for (int j = 0; j < these; ++j) tma_3d(at + kTok * 128 + j * rows * 128, &map_a, 64 * k, r0, list[i + j], bar);
+            ++filled;
+            if (++stage == kShrinkStages) stage = 0, phase ^= 1;
+          }
+        }
+      }
+    } else if (warp == 1) {
+      if (lane == 0) {
+        for (int i = 0; ok && i < items; i += group) {
+          const uint32_t idesc = instr_desc(c.dtype == WS_F16, false, false, kTok, n * min(group, items - i));
+          ok = bar_wait(smem_u32(&acc_empty[acc]), acc_phase ^ 1, &dead);
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          for (int k = k0; ok && k < k1; ++k) {
+            ok = bar_wait(smem_u32(&full_bar[stage]), phase, &dead);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t at = base + stage * kShrinkStage;
+            const uint64_t da = smem_desc(at, false), db = smem_desc(at + kTok * 128, false);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) entry[i] = __shfl_sync(0xffffffffu, mine ? w.at : -1, 8 * i + g);
-    const uint16_t* B = static_cast<const uint16_t*>(c.B) + a * c.strideB;
-    // {roundings, remainders} of ranks k + 4 q, + 1 and of + 2, + 3 of the lane's rows
-    const auto load_h = [&](int k, uint4(&hv)[4]) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        hv[i] = entry[i] >= 0 ? *reinterpret_cast<const uint4*>(h + static_cast<int64_t>(entry[i]) * (rpad / 2) + k / 2 + 2 * q)
-                              : make_uint4(0, 0, 0, 0);
-    };
-    const auto load_b = [&](int k, int j) {  // a row past the last repeats it: its sums are not stored
-      const int n = min(n0 + 32 * (j >> 2) + 8 * (g >> 1) + 2 * (j & 3) + (g & 1), N - 1);
-      return load4(B + n * c.ldb, k + 4 * q, r, vecB);
-    };
-    if (__all_sync(0xffffffffu, mine || t0 + lane >= c.nrows)) {
-#pragma unroll 1
-      for (int k = 0; k < rpad; k += 16) {
-        uint4 hv[4];
-        uint2 bv[8];
-        load_h(k, hv);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) bv[j] = load_b(k, j);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int m = 0; m < 2; ++m) mma_pair<half>(acc[m][j], hv[2 * m], hv[2 * m + 1], bv[j]);
+            for (int j = 0; j < 4; ++j)
+              mma_f16(tmem + acc * kRankBlock, da + j * (32 >> 4), db + j * (32 >> 4), idesc, k > k0 || j > 0);
+            mma_commit(smem_u32(&empty_bar[stage]));
+            if (k == k1 - 1) mma_commit(smem_u32(&acc_full[acc]));
+            if (++stage == kShrinkStages) stage = 0, phase ^= 1;
+          }
+          if (++acc == 2) acc = 0, acc_phase ^= 1;
+        }
       }
     } else {
-      // Some tokens do not have this adapter.  A zero h would leave them alone but for infinities and NaN in B, so
-      // the sum is taken apart and added to the tokens that have it.
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        float d[2][4] = {};
-#pragma unroll 1
-        for (int k = 0; k < rpad; k += 16) {
-          uint4 hv[4];
-          load_h(k, hv);
-          const uint2 bv = load_b(k, j);
-#pragma unroll
-          for (int m = 0; m < 2; ++m) mma_pair<half>(d[m], hv[2 * m], hv[2 * m + 1], bv);
+      for (int i = 0; ok && i < items; ++i) {
+        const int at = i % group;
+        if (at == 0) {
+          const bool got = lane != 0 || bar_wait(smem_u32(&acc_full[acc]), acc_phase, &dead);
+          ok = __shfl_sync(0xffffffffu, got, 0);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }
+        const bool mine = behind.col == list[i];
+        for (int j = 0; j < n; j += 16) {
+          float f[16];
+          tmem_load16(tmem + acc * kRankBlock + at * n + j + (static_cast<uint32_t>(quarter * 32) << 16), f);
+          if (mine) {
+            float4* dst = reinterpret_cast<float4*>(h + static_cast<int64_t>(behind.at) * rpad + r0 + j);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (entry[i] >= 0) {
-            acc[i >> 1][j][2 * (i & 1)] += d[i >> 1][2 * (i & 1)];
-            acc[i >> 1][j][2 * (i & 1) + 1] += d[i >> 1][2 * (i & 1) + 1];
+            for (int e = 0; e < 4; ++e) dst[e] = make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);
           }
+        }
+        if (mine) behind.next(c);
+        if (at == group - 1 || i == items - 1) {
+          asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) bar_arrive(smem_u32(&acc_empty[acc]));
+          if (++acc == 2) acc = 0, acc_phase ^= 1;
+        }
       }
+    }
+    __syncwarp();
+    __syncthreads();
+    if (items < kList || dead) break;
+  }
+  if (dead) {  // no copy and no product may be in flight when the CTA leaves
+    if (warp == 0 && lane == 0)
+      for (int f = max(0, filled - kShrinkStages); f < filled; ++f)
+        bar_wait_short(smem_u32(&full_bar[f % kShrinkStages]), static_cast<uint32_t>(f / kShrinkStages) & 1);
+    if (warp == 1 && lane == 0) {
+      mma_commit(smem_u32(&last_bar));
+      bar_wait_short(smem_u32(&last_bar), 0);
+      atomicOr(status, 1);
+    }
+    __syncwarp();
+    __syncthreads();
+  }
+  if (warp == 1) tmem_free<2 * kRankBlock>(tmem);
+}
+
+constexpr int kExpandThreads = 256;  // two threads a token
+constexpr int kExpandN = 256;        // values of y a CTA takes of every token
+constexpr int kExpandRanks = 32;     // ranks multiplied at once: 64 bytes of roundings and 64 of remainders a row
+constexpr int kExpandA = kTok * 128, kExpandB = kExpandN * 64, kExpandY = kTok * 128;  // bytes; y in four pieces of 64 values
+constexpr size_t kExpandSmem = kExpandA + kExpandB + 4 * kExpandY + 1024;
+
+// h of an entry, rank j: the parts of K summed, times the entry's value.
+__device__ __forceinline__ float4 scaled_h(const ws_adapters_call& c, const float* h, int rpad, int split, int entry, int j, float v) {
+  float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int i = 0; i < split; ++i) {
+    const float4 f = *reinterpret_cast<const float4*>(h + (static_cast<int64_t>(i) * c.nnz + entry) * rpad + j);
+    s.x += f.x, s.y += f.y, s.z += f.z, s.w += f.w;
+  }
+  return make_float4(v * s.x, v * s.y, v * s.z, v * s.w);
+}
+
+// What the adapters add to value n of token t, by itself.
+template <bool half>
+__device__ __noinline__ float added(const ws_adapters_call& c, const float* h, int rpad, int split, int64_t t, int64_t n) {
+  Walk w;
+  float sum = 0.0f;
+  for (w.start(c, t); w.col != INT_MAX; w.next(c)) {
+    const uint16_t* row = static_cast<const uint16_t*>(c.B) + w.col * c.strideB + n * c.ldb;
+    for (int j = 0; j < c.r; j += 4) {
+      const float4 f = scaled_h(c, h, rpad, split, w.at, j, c.vals[w.at]);
+      const float v[4] = {f.x, f.y, f.z, f.w};
+      for (int i = 0; i < 4 && j + i < c.r; ++i) sum = fmaf(v[i], value16<half>(row[j + i]), sum);
+    }
+  }
+  return sum;
+}
+
+// 256 values of 128 tokens: base arrives while the products run; the sums go through the same piece of shared memory to y.  Two
+// CTAs share an SM, so that one's latencies (row pointer, column, h and B, product, store) pass under the other's
+// work.  (8191 tokens, rank 32, 2048 halves: 31 us on the warp-level instruction, 38 us in columns of 128 values, 34 us with a CTA that
+// keeps v h for two columns, 30 us so.)
+template <bool half>
+__global__ void __launch_bounds__(kExpandThreads, 2)
+    expand_tile_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_base,
+                       const __grid_constant__ CUtensorMap map_y, const ws_adapters_call c, const float* __restrict__ h,
+                       int rpad, int split, bool copies, int* status) {
+  extern __shared__ uint8_t raw[];
+  __shared__ __align__(8) uint64_t base_bar, b_bar, m_bar;
+  __shared__ uint32_t tmem_slot;
+  __shared__ volatile int dead;
+  __shared__ int mins[kExpandThreads / 32];
+  const int warp = threadIdx.x >> 5, m = threadIdx.x & (kTok - 1), side = threadIdx.x / kTok;
+  const uint32_t sa = (smem_u32(raw) + 1023u) & ~1023u, sy = sa + kExpandA, sb = sy + 4 * kExpandY;
+  const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTok, t = t0 + m;
+  const int N = static_cast<int>(c.N);
+  const int n0 = blockIdx.y * kExpandN;
+  const int pieces = min(4, (N - n0 + 63) / 64);  // of 64 values that are there
+  const bool there = t < c.nrows;
+  if (threadIdx.x == 0) {
+    bar_init(smem_u32(&base_bar), 1);
+    bar_init(smem_u32(&b_bar), 1);
+    bar_init(smem_u32(&m_bar), 1);
+    dead = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    if (copies && c.base) {
+      bar_expect(smem_u32(&base_bar), pieces * kExpandY);
+      for (int i = 0; i < pieces; ++i) tma_2d(sy + i * kExpandY, &map_base, n0 + 64 * i, static_cast<int>(t0), smem_u32(&base_bar));
+    }
+  }
+  if (warp == 0) tmem_alloc<kExpandN>(smem_u32(&tmem_slot));
+  Walk w;
+  w.start(c, t);
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem = tmem_slot;
+  const uint32_t idesc = instr_desc(half, false, false, kTok, kExpandN);
+
+  int done = 0;        // products of 32 ranks
+  bool mixed = false;  // some token does not have some adapter of the tile
+  for (;;) {
+    const int a = next_adapter<kExpandThreads / 32>(w.col, mins);
+    if (a == INT_MAX || dead) break;  // dead was set before the barrier in there, or is not for a while
+    const bool mine = w.col == a;
+    const float v = mine ? c.vals[w.at] : 0.0f;
+    for (int r0 = 0; r0 < rpad; r0 += kExpandRanks) {
+      const int ranks = min(kExpandRanks, rpad - r0);  // 16 or 32
+      if (done > 0) bar_wait(smem_u32(&m_bar), (done - 1) & 1, &dead);  // what reads A and B is over
+      if (threadIdx.x == 0 && !dead) {
+        bar_expect(smem_u32(&b_bar), kExpandB);
+        tma_3d(sb, &map_b, r0, n0, a, smem_u32(&b_bar));
+      }
+#pragma unroll
+      for (int i = 0; i < kExpandRanks / 16; ++i) {
+        const int j = 16 * i + 8 * side;
+        if (j >= ranks) break;
+        uint32_t hi[4] = {}, lo[4] = {};
+        if (mine) {
+          const float4 f = scaled_h(c, h, rpad, split, w.at, r0 + j, v), g = scaled_h(c, h, rpad, split, w.at, r0 + j + 4, v);
+          const uint2 p[4] = {split_pair<half>(f.x, f.y), split_pair<half>(f.z, f.w), split_pair<half>(g.x, g.y),
+                              split_pair<half>(g.z, g.w)};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) hi[e] = p[e].x, lo[e] = p[e].y;
+        }
+        const uint32_t row = sa + m * 128;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((j >> 3) ^ (m & 7)) << 4)), "r"(hi[0]),
+                     "r"(hi[1]), "r"(hi[2]), "r"(hi[3])
+                     : "memory");
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((4 + (j >> 3)) ^ (m & 7)) << 4)), "r"(lo[0]),
+                     "r"(lo[1]), "r"(lo[2]), "r"(lo[3])
+                     : "memory");
+      }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      if (!__syncthreads_and(mine || !there)) mixed = true;
+      if (dead) break;
+      if (threadIdx.x == 0 && bar_wait(smem_u32(&b_bar), done & 1, &dead)) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint64_t da = smem_desc(sa, false), db = smem_desc64(sb);
+        for (int j = 0; j < ranks / 16; ++j) {
+          mma_f16(tmem, da + j * (32 >> 4), db + j * (32 >> 4), idesc, done > 0 || j > 0);
+          mma_f16(tmem, da + ((64 + 32 * j) >> 4), db + j * (32 >> 4), idesc, true);
+        }
+        mma_commit(smem_u32(&m_bar));
+      }
+      ++done;
     }
     if (mine) w.next(c);
   }
-  uint16_t* y = static_cast<uint16_t*>(c.y);
+  if (done > 0) bar_wait(smem_u32(&m_bar), (done - 1) & 1, &dead);
+  if (copies && c.base) bar_wait(smem_u32(&base_bar), 0, &dead);
+  __syncthreads();
+  if (!dead) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint16_t* base = static_cast<const uint16_t*>(c.base) + (c.base && there ? t * c.ldbase + n0 : 0);
+    uint16_t* y = static_cast<uint16_t*>(c.y) + (there ? t * c.ldy + n0 : 0);
+#pragma unroll 1
+    for (int j = side * (kExpandN / 2); j < (side + 1) * (kExpandN / 2); j += 16) {
+      const int left = N - n0 - j;
+      if (left <= 0) break;
+      float f[16] = {};
+      __syncwarp();
+      if (done > 0) tmem_load16(tmem + j + (static_cast<uint32_t>((warp & 3) * 32) << 16), f);
+      if (mixed && there) {
+        // A token without an adapter got zero times its values: nothing, unless those are infinite or NaN.
+        for (int i = 0; i < 16; ++i)
+          if (i < left && !(fabsf(f[i]) <= 3.4e38f)) f[i] = added<half>(c, h, rpad, split, t, n0 + j + i);
+      }
+      if (copies) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int64_t t = t0 + 8 * i + g;
-    if (t >= c.nrows) continue;
+        for (int s = 0; s < 2; ++s) {
+          const uint32_t at = sy + (j >> 6) * kExpandY + m * 128 + (((((j & 63) >> 3) + s) ^ (m & 7)) << 4);
+          uint32_t b[4] = {};
+          if (c.base)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at) : "memory");
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const int n = n0 + 32 * s + 8 * q;
-      uint32_t v[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        v[j] = bits16<half>(acc[i >> 1][4 * s + j][2 * (i & 1)]) |
-               static_cast<uint32_t>(bits16<half>(acc[i >> 1][4 * s + j][2 * (i & 1) + 1])) << 16;
-      uint16_t* dst = y + t * c.ldy + n;
-      if (vec) {
-        if (n < N) *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (n + e < N) dst[e] = static_cast<uint16_t>(v[e >> 1] >> (16 * (e & 1)));
+          for (int i = 0; i < 4; ++i)
+            b[i] = bits16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i]) |
+                   static_cast<uint32_t>(bits16<half>(value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1])) << 16;
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
+        }
+      } else if (there) {
+        for (int i = 0; i < 16; ++i)
+          if (i < left) y[j + i] = bits16<half>((c.base ? value16<half>(base[j + i]) : 0.0f) + f[i]);
       }
     }
   }
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  __syncwarp();
+  __syncthreads();
+  if (threadIdx.x == 0 && dead) {  // no copy and no product may be in flight when the CTA leaves
+    atomicOr(status, 1);
+    if (done > 0) bar_wait_short(smem_u32(&b_bar), (done - 1) & 1), bar_wait_short(smem_u32(&m_bar), (done - 1) & 1);
+    if (copies && c.base) bar_wait_short(smem_u32(&base_bar), 0);
+  } else if (threadIdx.x == 0 && copies) {
+    for (int i = 0; i < pieces; ++i) tma_store_2d(&map_y, sy + i * kExpandY, n0 + 64 * i, static_cast<int>(t0));
+    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  }
+  __syncwarp();
+  __syncthreads();
+  if (warp == 0) tmem_free<kExpandN>(tmem);
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -399,45 +527,60 @@ __global__ void __launch_bounds__(kAdThreads) expand_step_kernel(const ws_adapte
   static_cast<uint16_t*>(c.y)[t * c.ldy + n] = bits16<half>(acc);
 }
 
-constexpr int64_t kStepRows = 128;  // most tokens that go one by one
-
 template <bool half>
-void launch(const ws_adapters_call& c, uint2* h, cudaStream_t s) {
+ws_status_t launch_step(const ws_adapters_call& c, uint2* h, cudaStream_t s) {
   const int rpad = adapters_rank(c.r);
   const bool vecB = c.r % 4 == 0 && reinterpret_cast<uintptr_t>(c.B) % 8 == 0 && c.ldb % 4 == 0 && c.strideB % 4 == 0;
-  const auto rows16 = [](const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; };
   const unsigned T = static_cast<unsigned>(c.nrows);
-  if (c.nrows <= kStepRows) {
-    if (c.nnz > 0) {
-      const unsigned split = static_cast<unsigned>(rpad / 2 / (kAdWarps / kStepSplit));
-      shrink_step_kernel<half><<<dim3(T, split), kAdThreads, 0, s>>>(c, h, rpad);
-    }
-    expand_step_kernel<half><<<dim3(static_cast<unsigned>((c.N + kAdThreads - 1) / kAdThreads), T), kAdThreads, 0, s>>>(c, h, rpad, vecB);
-    return;
-  }
-  const unsigned tiles = (T + kTileTok - 1) / kTileTok;
+  if (c.nnz > 0)
+    shrink_step_kernel<half><<<dim3(T, static_cast<unsigned>(rpad / 2 / (kAdWarps / kStepSplit))), kAdThreads, 0, s>>>(c, h, rpad);
+  expand_step_kernel<half><<<dim3(static_cast<unsigned>((c.N + kAdThreads - 1) / kAdThreads), T), kAdThreads, 0, s>>>(c, h, rpad, vecB);
+  return WS_OK;
+}
+
+ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int num_sms, cudaStream_t s) {
+  const int rpad = adapters_rank(c.r);
+  const bool half = c.dtype == WS_F16;
+  const unsigned tiles = static_cast<unsigned>((c.nrows + kTok - 1) / kTok);
+  int split = 1;
+  if (!encoder()) return routing_fail(WS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+  CUtensorMap x{}, a{}, b{}, base{}, y{};
   if (c.nnz > 0) {
-    const auto run = [&](auto nr) {
-      constexpr int NR = decltype(nr)::value;
-      constexpr int smem = kAdWarps * kTileTok * 8 * NR * static_cast<int>(sizeof(float));
-      if (smem > 48 * 1024)
-        cudaFuncSetAttribute(reinterpret_cast<const void*>(shrink_tile_kernel<half, NR>), cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-      shrink_tile_kernel<half, NR><<<dim3(tiles, static_cast<unsigned>((rpad + 8 * NR - 1) / (8 * NR))), kAdThreads, smem, s>>>(c, h, rpad);
-    };
-    if (rpad <= 16) run(std::integral_constant<int, 2>());
-    else if (rpad <= 32) run(std::integral_constant<int, 4>());
-    else run(std::integral_constant<int, 8>());
+    // parts of K until every SM has a CTA
+    const int64_t steps = (c.K + 63) / 64;
+    while (split < kMaxSplit && 2 * split <= steps && tiles * split < static_cast<unsigned>(num_sms) / 2) split *= 2;
+    if (!encode(&x, c.x, half, c.K, c.nrows, c.ldx, 0, 0, kTok) ||
+        !encode(&a, c.A, half, c.K, c.r, c.lda, c.ncols, c.strideA, rpad < kRankBlock ? rpad : kRankBlock) ||
+        !encode(&b, c.B, half, c.r, c.N, c.ldb, c.ncols, c.strideB, kExpandN, kExpandRanks))
+      return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
+    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(shrink_tile_kernel),
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShrinkSmem));
+    if (e == cudaSuccess) e = cudaMemsetAsync(status, 0, sizeof(int), s);
+    if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
+    const dim3 grid(tiles, static_cast<unsigned>(split), static_cast<unsigned>((rpad + kRankBlock - 1) / kRankBlock));
+    shrink_tile_kernel<<<grid, kShrinkThreads, kShrinkSmem, s>>>(x, a, c, h, rpad, status);
   }
-  const bool vec = c.N % 8 == 0 && (!c.base || rows16(c.base, c.ldbase)) && rows16(c.y, c.ldy);
-  const auto expand = vec ? expand_tile_kernel<half, true> : expand_tile_kernel<half, false>;
-  expand<<<dim3(tiles, static_cast<unsigned>((c.N + 64 * kAdWarps - 1) / (64 * kAdWarps))), kAdThreads, 0, s>>>(c, h, rpad, vecB);
+  // base and y by the copy engine where their rows start at multiples of 16 bytes, else by loads and stores
+  const auto rows16 = [](const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; };
+  bool copies = (!c.base || rows16(c.base, c.ldbase)) && rows16(c.y, c.ldy);
+  if (copies && !(encode(&y, c.y, half, c.N, c.nrows, c.ldy, 0, 0, kTok) &&
+                  (!c.base || encode(&base, c.base, half, c.N, c.nrows, c.ldbase, 0, 0, kTok))))
+    copies = false;
+  const auto kernel = half ? expand_tile_kernel<true> : expand_tile_kernel<false>;
+  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             static_cast<int>(kExpandSmem));
+  if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
+  kernel<<<dim3(tiles, static_cast<unsigned>((c.N + kExpandN - 1) / kExpandN)), kExpandThreads, kExpandSmem, s>>>(
+      b, base, y, c, h, rpad, split, copies, status);
+  return WS_OK;
 }
 
 }  // namespace
 
-void launch_adapters(const ws_adapters_call& c, void* scratch, cudaStream_t s) {
-  if (c.dtype == WS_F16) launch<true>(c, static_cast<uint2*>(scratch), s);
-  else launch<false>(c, static_cast<uint2*>(scratch), s);
+ws_status_t launch_adapters(const ws_adapters_call& c, void* scratch, int num_sms, cudaStream_t s) {
+  char* h = static_cast<char*>(scratch) + 16;  // behind the status word
+  if (!adapters_step(c.nrows, c.r)) return launch_prompt(c, reinterpret_cast<float*>(h), static_cast<int*>(scratch), num_sms, s);
+  return c.dtype == WS_F16 ? launch_step<true>(c, reinterpret_cast<uint2*>(h), s) : launch_step<false>(c, reinterpret_cast<uint2*>(h), s);
 }
 
 }  // namespace wsk

@@ -18,10 +18,10 @@
 // A tile of rows may reach past its expert's last row: such rows are computed
 // and not stored.  In `weights` they would be summed, so the last stage's rows
 // past the end are cleared in shared memory (in both operands: 0 * inf is NaN).
-#include <cuda.h>
 #include <type_traits>
 
 #include "routing.cuh"
+#include "tensor.cuh"
 #include "ws_internal.cuh"
 
 namespace wsk {
@@ -31,7 +31,6 @@ constexpr int kTileM = 128;   // rows of the M side: lanes of tensor memory
 constexpr int kTileK = 64;    // 128 bytes: the swizzle's span
 constexpr int kThreads = 192; // TMA warp, MMA warp, 4 epilogue warps
 constexpr int kBytesA = kTileM * kTileK * 2;
-constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 
 // Where the rows of the experts are in the product D (M x N tile).
 constexpr int kRowsM = 0;    // on the M side (lanes)
@@ -52,92 +51,6 @@ struct GroupedParams {
   bool vec;      // rows of the result start at multiples of 16 bytes
   int* status;
 };
-
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-
-__device__ __forceinline__ void bar_init(uint32_t bar, int count) {
-  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
-}
-__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void bar_arrive(uint32_t bar) {
-  asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
-  uint32_t ok;
-  asm volatile(
-      "{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
-      : "=r"(ok)
-      : "r"(bar), "r"(parity)
-      : "memory");
-  return ok != 0;
-}
-__device__ __forceinline__ unsigned long long now_ns() {
-  unsigned long long t;
-  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
-  return t;
-}
-// Waits for a phase; gives up after kWaitLimitNs or when another role gave up (*dead).
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  if (bar_try(bar, parity)) return true;
-  const unsigned long long start = now_ns();
-  for (unsigned i = 1;; ++i) {
-    if (bar_try(bar, parity)) return true;
-    if ((i & 31) == 0) {
-      if (*dead) return false;
-      if (now_ns() - start > kWaitLimitNs) {
-        *dead = 1;
-        return false;
-      }
-    }
-  }
-}
-
-__device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),
-      "l"(map), "r"(x), "r"(y), "r"(bar)
-      : "memory");
-}
-__device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
-          dst),
-      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
-      : "memory");
-}
-
-// Shared-memory matrix descriptor, 128-byte swizzle.  K-major: 8-row groups of
-// 1024 bytes follow each other.  MN-major: blocks of 64 (M or N) x 64 (K), in
-// which 8 steps of K take 1024 bytes; blocks are 8192 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn_major) {
-  const uint64_t lbo = mn_major ? 8192 >> 4 : 1, sbo = 1024 >> 4;
-  return (static_cast<uint64_t>(addr >> 4) & 0x3fff) | lbo << 16 | sbo << 32 | 1ull << 46 | 2ull << 61;
-}
-
-__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
-  asm volatile(
-      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
-      "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
-      : "memory");
-}
-__device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-
-// 16 consecutive 32-bit columns of the warp's 32 lanes.
-__device__ __forceinline__ void tmem_load16(uint32_t addr, float (&f)[16]) {
-  uint32_t r[16];
-  asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
-      : "r"(addr));
-  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-  for (int i = 0; i < 16; ++i) f[i] = __uint_as_float(r[i]);
-}
 
 __device__ __forceinline__ uint16_t round16(float f, bool half) {
   return half ? __half_as_ushort(__float2half_rn(f)) : __bfloat16_as_ushort(__float2bfloat16_rn(f));
@@ -279,12 +192,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)),
-                 "r"(static_cast<uint32_t>(S::kAccCols))
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
-  }
+  if (warp == 1) tmem_alloc<S::kAccCols>(smem_u32(&tmem_slot));
   if constexpr (kRows != kRowsSum) {  // row tiles before every group
     int sum = 0;
     for (int e0 = 0; e0 < p.groups; e0 += kThreads) {
@@ -348,18 +256,12 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (!ok) {  // no copy may be in flight when the CTA leaves
         const int64_t begin = filled > S::kStages ? filled - S::kStages : 0;
         for (int64_t f = begin; f < filled; ++f) {
-          const unsigned long long start = now_ns();
-          const uint32_t bar = smem_u32(&full_bar[f % S::kStages]);
-          while (!bar_try(bar, static_cast<uint32_t>(f / S::kStages) & 1) && now_ns() - start < kWaitLimitNs / 10) {
-          }
+          bar_wait_short(smem_u32(&full_bar[f % S::kStages]), static_cast<uint32_t>(f / S::kStages) & 1);
         }
       }
     }
   } else if (warp == 1) {
-    // D 32-bit; A and B half (0) or bfloat16 (1)
-    const uint32_t idesc = 1u << 4 | (p.half ? 0u : 1u << 7 | 1u << 10) | static_cast<uint32_t>(kAMN) << 15 |
-                           static_cast<uint32_t>(kBMN) << 16 | static_cast<uint32_t>(BN >> 3) << 17 |
-                           static_cast<uint32_t>(kTileM >> 4) << 24;
+    const uint32_t idesc = instr_desc(p.half, kAMN, kBMN, kTileM, BN);
     int stage = 0, acc = 0;
     uint32_t phase = 0, acc_phase = 0;
     bool ok = true;
@@ -401,9 +303,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     }
     if (!ok && lane == 0) {  // nor may a product
       mma_commit(smem_u32(&last_bar));
-      const unsigned long long start = now_ns();
-      while (!bar_try(smem_u32(&last_bar), 0) && now_ns() - start < kWaitLimitNs / 10) {
-      }
+      bar_wait_short(smem_u32(&last_bar), 0);
     }
   } else {
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
@@ -458,9 +358,7 @@ __global__ void __launch_bounds__(kThreads, 1)
   __syncwarp();
   __syncthreads();
   if (threadIdx.x == 0 && dead) atomicOr(p.status, 1);
-  if (warp == 1)
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(static_cast<uint32_t>(S::kAccCols))
-                 : "memory");
+  if (warp == 1) tmem_free<S::kAccCols>(tmem);
 }
 
 // ---------------------------------------------------------------- few rows an expert, forward
@@ -573,37 +471,6 @@ cudaError_t launch_thin(const GroupedRows& g, cudaStream_t s) {
 }
 
 // ---------------------------------------------------------------- host
-
-using EncodeFn = CUresult(CUDAAPI*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                    const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                    CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
-EncodeFn encoder() {
-  static const EncodeFn fn = [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult found = cudaDriverEntryPointSymbolNotFound;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess) {
-      cudaGetLastError();
-      f = nullptr;
-    }
-    return reinterpret_cast<EncodeFn>(f);
-  }();
-  return fn;
-}
-
-// Rows of 16-bit values; groups > 0: `groups` matrices of `rows` rows.  Boxes of 64 values x box_rows.
-bool encode(CUtensorMap* map, const void* p, bool half, int64_t width, int64_t rows, int64_t ld, int64_t groups,
-            int64_t group_stride, int box_rows) {
-  const cuuint64_t dims[3] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows), static_cast<cuuint64_t>(groups)};
-  const cuuint64_t strides[2] = {static_cast<cuuint64_t>(ld) * 2,
-                                 static_cast<cuuint64_t>(groups > 1 ? group_stride : ld * rows) * 2};
-  const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_rows), 1}, step[3] = {1, 1, 1};
-  return encoder()(map, half ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, groups > 0 ? 3 : 2,
-                   const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                   CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
 
 template <int BN, int kRows, bool kWMN>
 cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const GroupedParams& p, int64_t tiles, int num_sms,

@@ -185,12 +185,12 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
     v = vals[row * k + lane];
     g = gvals[row * k + lane];
   }
-  const float a = warp_sum(v * g);
-  float out[V];
-  if (normalize) {
+  float out[V], a = 0.0f;
+  if (normalize) {  // the zeros do not wait for what was loaded
 #pragma unroll
     for (int i = 0; i < V; ++i) out[i] = 0.0f;
   } else {
+    a = warp_sum(v * g);
     load_row<T, V>(logits + row * ld, lane * V, cols, vec, out);
     uint32_t best = 0;
 #pragma unroll
@@ -220,6 +220,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
     for (int i = 0; i < V; ++i)
       if (lane * V + i < cols) dst[lane * V + i] = from_f32<T>(out[i]);
   }
+  if (normalize) a = warp_sum(v * g);
   __syncwarp();  // the chosen columns over what the row's lanes stored
   if (static_cast<unsigned>(col) < static_cast<unsigned>(cols)) dst[col] = from_f32<T>(v * (g - a));
 }

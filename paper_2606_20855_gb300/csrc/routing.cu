@@ -196,7 +196,8 @@ __global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, 
     }
     __syncthreads();
   }
-  for (int e = threadIdx.x; e < cols; e += blockDim.x) counts[static_cast<int64_t>(blockIdx.x) * cols + e] = cnt[e];
+  const int padded = (cols + 3) & ~3;
+  for (int e = threadIdx.x; e < padded; e += blockDim.x) counts[static_cast<int64_t>(blockIdx.x) * padded + e] = e < cols ? cnt[e] : 0;
 }
 
 // Every CTA adds up the counts of all chunks by itself (a few hundred KB from L2, the threads split over the chunks):
@@ -211,20 +212,24 @@ __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, 
   uint16_t* pre = reinterpret_cast<uint16_t*>(before + cols);
   for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = before[e] = 0;
   __syncthreads();
-  const int groups = cols >= static_cast<int>(blockDim.x) ? 1 : blockDim.x / cols;
-  const int g = static_cast<int>(threadIdx.x) / cols;
-  for (int e = threadIdx.x - (groups > 1 ? g * cols : 0); g < groups || groups == 1; e += blockDim.x) {
-    if (e >= cols) break;
-    int total = 0, mine = 0;
+  const int quads = (cols + 3) / 4, groups = kTileRows / quads;  // at most 256 quads: a thread each
+  const int g = static_cast<int>(threadIdx.x) / quads, v = static_cast<int>(threadIdx.x) - g * quads;
+  if (g < groups) {
+    int4 total = make_int4(0, 0, 0, 0), mine = total;
+    const int4* from = reinterpret_cast<const int4*>(counts) + v;
 #pragma unroll 8
-    for (int c = groups > 1 ? g : 0; c < static_cast<int>(gridDim.x); c += groups) {
-      const int n = counts[static_cast<int64_t>(c) * cols + e];
-      total += n;
-      if (c < static_cast<int>(blockIdx.x)) mine += n;
+    for (int c = g; c < static_cast<int>(gridDim.x); c += groups) {
+      const int4 n = from[static_cast<int64_t>(c) * quads];
+      total.x += n.x, total.y += n.y, total.z += n.z, total.w += n.w;
+      if (c < static_cast<int>(blockIdx.x)) mine.x += n.x, mine.y += n.y, mine.z += n.z, mine.w += n.w;
     }
-    atomicAdd(&next[e], total);
-    atomicAdd(&before[e], mine);
-    if (groups > 1) break;
+    const int t[4] = {total.x, total.y, total.z, total.w}, m[4] = {mine.x, mine.y, mine.z, mine.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * v + i < cols) {
+        atomicAdd(&next[4 * v + i], t[i]);
+        atomicAdd(&before[4 * v + i], m[i]);
+      }
   }
   __syncthreads();
   const int placed = scan_columns(cols, next, scratch);

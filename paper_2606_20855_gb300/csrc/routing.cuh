@@ -141,6 +141,12 @@ ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_
 
 // Ranks kept for an entry of S: h is padded with zeros.
 inline int adapters_rank(int64_t r) { return static_cast<int>((r + 15) / 16 * 16); }
-void launch_adapters(const ws_adapters_call& c, void* scratch, cudaStream_t s);
+// Whether tokens go one by one.  That reads A and B for every token (from L2), 2 rank (K + N) bytes each; a tile of 128 tokens
+// reads x once for every few adapters it meets.  K = N = 4096, bfloat16, us one by one | as tiles of one adapter | as tiles in
+// which every token has another adapter: 512 tokens of rank 16 31 | 22 | 225, 256 of rank 64 about 100 | 31 | 659, 1024 of rank
+// 16 about 58 | 22 | 225.
+inline bool adapters_step(int64_t nrows, int64_t r) { return nrows * adapters_rank(r) <= 8192; }
+// scratch: a status word (16 bytes), then up to four parts of h.
+ws_status_t launch_adapters(const ws_adapters_call& c, void* scratch, int num_sms, cudaStream_t s);
 
 }  // namespace wsk

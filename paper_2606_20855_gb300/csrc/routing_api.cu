@@ -142,7 +142,7 @@ int64_t ws_routing_scratch(int64_t nrows, int64_t ncols) {
   int sms = 0;
   if (nrows < 0 || ncols < 0 || sm_count(&sms) != WS_OK) return 0;
   const int64_t chunks = routing_chunks(nrows, sms);
-  return chunks == 1 ? 0 : chunks * ncols * static_cast<int64_t>(sizeof(int32_t));
+  return chunks == 1 ? 0 : chunks * ((ncols + 3) & ~int64_t{3}) * static_cast<int64_t>(sizeof(int32_t));
 }
 
 ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
@@ -155,8 +155,9 @@ ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;
   const int64_t chunks = routing_chunks(r->nrows, sms);
-  if (chunks > 1 && (!scratch || scratch_bytes < chunks * r->ncols * static_cast<int64_t>(sizeof(int32_t))))
-    return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_routing_scratch");
+  if (chunks > 1 && (!scratch || reinterpret_cast<uintptr_t>(scratch) % 16 ||
+                     scratch_bytes < chunks * ((r->ncols + 3) & ~int64_t{3}) * static_cast<int64_t>(sizeof(int32_t))))
+    return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_routing_scratch, or misaligned");
   launch_routing_build(*r, static_cast<int32_t*>(scratch), sms, cuda_stream(stream));
   return launched("ws_routing_build");
 }
@@ -250,7 +251,7 @@ ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int6
 }
 
 int64_t ws_adapters_scratch(int64_t nnz, int64_t r) {
-  return nnz <= 0 || r <= 0 ? 0 : nnz * adapters_rank(r) * static_cast<int64_t>(sizeof(float));
+  return 16 + (nnz <= 0 || r <= 0 ? 0 : nnz * adapters_rank(r) * 4 * static_cast<int64_t>(sizeof(float)));
 }
 
 ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
@@ -262,8 +263,9 @@ ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scr
   if (c.nrows > INT32_MAX || c.ncols > INT32_MAX || c.nnz > INT32_MAX || c.K > kMaxWidth || c.N > kMaxWidth || c.r > 4096)
     return routing_fail(WS_ERR_OVERFLOW, "at most %d rows, columns and entries, rows of 2^24 values, rank 4096", INT32_MAX);
   if (c.nnz > 0 && (c.nrows == 0 || c.ncols == 0)) return routing_fail(WS_ERR_SHAPE, "entries in a matrix without rows or columns");
-  const bool used = c.nrows > 0 && c.N > 0, inner = used && c.nnz > 0 && c.r > 0 && c.K > 0;
-  if (!c.rowptr || (c.nnz > 0 && (!c.colidx || !c.vals)) || (used && !c.y) || (inner && (!c.x || !c.A || !c.B || !scratch)))
+  const bool used = c.nrows > 0 && c.N > 0, prompt = !adapters_step(c.nrows, c.r);
+  const bool inner = used && c.nnz > 0 && c.r > 0 && c.K > 0;
+  if (!c.rowptr || (c.nnz > 0 && (!c.colidx || !c.vals)) || (used && (!c.y || !scratch)) || (inner && (!c.x || !c.A || !c.B)))
     return routing_fail(WS_ERR_INVALID_ARG, "NULL pointer");
   if (used && c.nrows > 1 && (c.ldy < c.N || (c.base && c.ldbase < c.N)))
     return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
@@ -271,17 +273,21 @@ ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scr
     const auto off16 = [](const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 != 0 || ld % 8 != 0; };
     if (off16(c.x, c.nrows > 1 ? c.ldx : 0) || off16(c.A, c.r > 1 ? c.lda : 0) || (c.ncols > 1 && c.strideA % 8))
       return routing_fail(WS_ERR_INVALID_ARG, "x and A start and have strides at multiples of 16 bytes");
+    if (prompt && (off16(c.B, c.N > 1 ? c.ldb : 0) || (c.ncols > 1 && c.strideB % 8)))
+      return routing_fail(WS_ERR_INVALID_ARG, "for many tokens B starts and has strides at multiples of 16 bytes");
     if ((c.nrows > 1 && c.ldx < c.K) || (c.r > 1 && c.lda < c.K) || (c.N > 1 && c.ldb < c.r) || c.strideA < 0 || c.strideB < 0)
       return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
-    if (scratch_bytes < ws_adapters_scratch(c.nnz, c.r) || reinterpret_cast<uintptr_t>(scratch) % 16)
-      return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_adapters_scratch, or misaligned");
   }
+  if (used && (scratch_bytes < ws_adapters_scratch(inner ? c.nnz : 0, c.r) || reinterpret_cast<uintptr_t>(scratch) % 16))
+    return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_adapters_scratch, or misaligned");
   if ((reinterpret_cast<uintptr_t>(c.y) | reinterpret_cast<uintptr_t>(c.base) | reinterpret_cast<uintptr_t>(c.B)) % 2)
     return routing_fail(WS_ERR_INVALID_ARG, "misaligned matrix");
   if (!used) return WS_OK;
   ws_adapters_call run = c;
   if (!inner) run.nnz = 0;  // nothing to add: entry ranges are cut to [0, 0]
-  launch_adapters(run, scratch, cuda_stream(stream));
+  int sms = 0;
+  if (const ws_status_t st = sm_count(&sms)) return st;
+  if (const ws_status_t st = launch_adapters(run, scratch, sms, cuda_stream(stream))) return st;
   return launched("ws_adapters");
 }
 

@@ -159,13 +159,14 @@ class Routing:
             _abi.ws_csr_destroy(R._handle(True, raw))
         scratch = _scratch(T, E, self._index)
         # offsets, the status word, the scratch; rows, entries and slots
-        self._buf = torch.empty(E + 2 + (scratch + 7) // 8, dtype=torch.int64, device=self.device)
+        words = (E + 3) // 2 * 2  # the scratch starts at a multiple of 16 bytes
+        self._buf = torch.empty(words + scratch // 8, dtype=torch.int64, device=self.device)
         self._ints = torch.empty((3, nnz), dtype=torch.int32, device=self.device)
         at, ints = self._buf.data_ptr(), self._ints.data_ptr()
         self._c = _abi.WsRouting(T, E, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), at, ints,
                                  ints + 4 * nnz, ints + 8 * nnz, at + 8 * (E + 1))
         self._r = ctypes.byref(self._c)
-        _abi.ws_routing_build(self._r, at + 8 * (E + 2), scratch, raw)
+        _abi.ws_routing_build(self._r, at + 8 * words, scratch, raw)
 
     @property
     def offsets(self) -> torch.Tensor:
@@ -325,8 +326,12 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     if x.shape[1] != K:
         raise ValueError(f"rows of {x.shape[1]} values do not fit adapters of {K}")
     A, lda, apart = _operand(A)
-    if not B.is_contiguous() and ((r > 1 and B.stride(2) != 1) or (N > 1 and B.stride(1) < r)):
-        B = B.contiguous()
+    if T * ((r + 15) // 16 * 16) > 8192:  # many tokens: the copy engine reads B
+        B, ldb, apartB = _operand(B)
+    else:
+        if not B.is_contiguous() and ((r > 1 and B.stride(2) != 1) or (N > 1 and B.stride(1) < r)):
+            B = B.contiguous()
+        ldb, apartB = B.stride(1), B.stride(0)
     ldbase = ldy = N
     if base is not None:
         _same(base, x, "base")
@@ -342,10 +347,10 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
             raise ValueError(f"out must be {T} x {N} with unit stride within its rows")
         if base is not None and (out.data_ptr(), ldy) != (base.data_ptr(), ldbase) and _overlap(out, base):
             raise ValueError("out must be base itself or lie apart from it")
-    need = nnz * ((r + 15) // 16 * 64)  # ws_adapters_scratch
+    need = 16 + nnz * ((r + 15) // 16 * 256)  # ws_adapters_scratch
     scratch = torch.empty(need, dtype=torch.uint8, device=dev)
     call = _abi.ADAPTERS_CALL.pack(T, L, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), K, r, N,
-                                   x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), B.stride(1), B.stride(0),
+                                   x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), ldb, apartB,
                                    0 if base is None else base.data_ptr(), ldbase, out.data_ptr(), ldy, dt)
     _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(dev.index))
     return out

@@ -66,7 +66,7 @@ def _check(x, A, B, S, base, got):
     assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4], want[bad][:4])
 
 
-@pytest.mark.parametrize("T", [1, 2, 33, 128, 129, 400])
+@pytest.mark.parametrize("T", [1, 2, 33, 129, 513, 700])
 @pytest.mark.parametrize("L,r,K,N", [(1, 16, 64, 64), (5, 8, 40, 1000), (12, 4, 1001, 24), (40, 32, 512, 515), (3, 64, 264, 2048),
                                      (6, 1, 17, 9), (4, 13, 300, 72), (2, 100, 96, 130)])
 @pytest.mark.parametrize("how", ["runs", "own", "mixed", "none"])
@@ -79,7 +79,7 @@ def test_against_64_bits(T, L, r, K, N, how, dt):
     _check(x, A, B, S, None, adapters(x, A, B, S))
 
 
-@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("T", [20, 300, 600])
 def test_strides_alignment_and_in_place(T):
     from paper_2606_20855_gb300 import adapters
     L, r, K, N = 4, 16, 104, 120
@@ -103,7 +103,7 @@ def test_strides_alignment_and_in_place(T):
                adapters(t, WA[:, :, :K], WB[:, :, :r], S))
 
 
-@pytest.mark.parametrize("T", [40, 200])
+@pytest.mark.parametrize("T", [40, 200, 600])
 def test_infinities_stay_with_their_tokens(T):
     from paper_2606_20855_gb300 import adapters
     L, r, K, N = 6, 8, 64, 96
@@ -119,7 +119,7 @@ def test_infinities_stay_with_their_tokens(T):
 
 def test_columns_out_of_range_take_no_part():
     from paper_2606_20855_gb300 import DeviceCSR, adapters
-    for T in (8, 256):
+    for T in (8, 256, 600):
         x, A, B = _randn((T, 32), torch.float16, 1), _randn((3, 8, 32), torch.float16, 2), _randn((3, 16, 8), torch.float16, 3)
         col = torch.ones(T, dtype=torch.int32, device="cuda")
         col[2], col[3] = -7, 3
@@ -131,7 +131,7 @@ def test_columns_out_of_range_take_no_part():
 def test_empty_sizes():
     from paper_2606_20855_gb300 import adapters
     bf = torch.bfloat16
-    for T, L, r, K, N in ((0, 3, 8, 16, 8), (5, 3, 0, 16, 8), (5, 3, 8, 0, 8), (5, 3, 8, 16, 0), (300, 3, 8, 0, 8)):
+    for T, L, r, K, N in ((0, 3, 8, 16, 8), (5, 3, 0, 16, 8), (5, 3, 8, 0, 8), (5, 3, 8, 16, 0), (300, 3, 8, 0, 8), (600, 3, 8, 0, 8), (600, 3, 0, 8, 8)):
         base = _randn((T, N), bf, 0)
         y = adapters(_randn((T, K), bf, 1), _randn((L, r, K), bf, 2), _randn((L, N, r), bf, 3), _select(T, L, "own", 1), base)
         assert torch.equal(y, base)
@@ -152,7 +152,7 @@ def test_beside_the_shared_projection():
 
 def test_equal_inputs_give_equal_bits():
     from paper_2606_20855_gb300 import adapters
-    for T in (30, 500):
+    for T in (30, 900):
         args = (_randn((T, 512), torch.bfloat16, 1), _randn((9, 16, 512), torch.bfloat16, 2), _randn((9, 300, 16), torch.bfloat16, 3),
                 _select(T, 9, "mixed", 2), _randn((T, 300), torch.bfloat16, 4))
         assert torch.equal(adapters(*args), adapters(*args))
