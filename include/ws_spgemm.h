@@ -437,22 +437,21 @@ ws_status_t ws_routing_combine_backward(const ws_routing* r, const void* gy, int
  * Products by column of R: column e has a matrix W[e], N x K, row-major (ldw
  * values from row to row, `stride` from matrix to matrix), and the rows of its
  * slots.  bfloat16 or half, sums in 32 bits, one rounding.
- *   matmul           ys[s] = W[e] xs[s]                     xs: nnz x K, ys: nnz x N
- *   matmul_rows      gxs[s] = W[e]^T gys[s]                 gys: nnz x N, gxs: nnz x K
- *   matmul_weights   gW[e] = sum over s of gys[s] xs[s]^T   zero for columns without entries
- * Rows behind the placed entries are not written (matmul, matmul_rows).  The inputs'
- * addresses and strides are multiples of 16 bytes; outputs need no alignment
- * beyond their type's.  N, K <= 2^24.
+ *   matmul            ys[s] = W[e] xs[s]                     xs: nnz x K, ys: nnz x N
+ *   matmul_backward   gxs[s] = W[e]^T gys[s]                 gys: nnz x N, gxs: nnz x K; NULL: not wanted, W is not read
+ *                     gW[e] = sum over s of gys[s] xs[s]^T   zero for columns without entries; NULL: not wanted, xs is not read
+ * Rows behind the placed entries are not written (ys, gxs).  N, K <= 2^24.
+ * An input whose address or strides are not multiples of 16 bytes is first
+ * copied to `scratch` (16-byte aligned), which has to have room for 16 bytes for every 8 values, or part of
+ * them, of its rows; scratch may be NULL where all inputs are aligned.
  */
 ws_status_t ws_routing_matmul(const ws_routing* r, const void* xs, int64_t ldxs, const void* W, int64_t ldw,
                               int64_t stride, int64_t N, int64_t K, void* ys, int64_t ldys, ws_dtype_t dtype,
-                              ws_stream_t stream);
-ws_status_t ws_routing_matmul_rows(const ws_routing* r, const void* gys, int64_t ldgys, const void* W, int64_t ldw,
-                                   int64_t stride, int64_t N, int64_t K, void* gxs, int64_t ldgxs, ws_dtype_t dtype,
-                                   ws_stream_t stream);
-ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int64_t ldgys, const void* xs,
-                                      int64_t ldxs, int64_t N, int64_t K, void* gW, int64_t ldgw, int64_t stride,
-                                      ws_dtype_t dtype, ws_stream_t stream);
+                              void* scratch, int64_t scratch_bytes, ws_stream_t stream);
+ws_status_t ws_routing_matmul_backward(const ws_routing* r, const void* gys, int64_t ldgys, const void* xs, int64_t ldxs,
+                                       const void* W, int64_t ldw, int64_t stride, int64_t N, int64_t K, void* gxs,
+                                       int64_t ldgxs, void* gW, int64_t ldgw, int64_t gstride, ws_dtype_t dtype,
+                                       void* scratch, int64_t scratch_bytes, ws_stream_t stream);
 
 /*
  * ws_adapters -- low-rank adapters of many requests beside a projection they
@@ -462,10 +461,11 @@ ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int6
  * range take no part).  bfloat16 or half; inner products A[a] x[t] are summed in
  * 32 bits and, times the value, kept as pairs of 16-bit values (for half up to
  * 65504), the result is summed in 32 bits and rounded once.  "Many tokens":
- * nrows times r, rounded up to a multiple of 16, is above 8192.  x and A, and
- * for many tokens B, start and have strides at multiples of 16 bytes.  base may
- * be NULL (zero) and may be y itself.
- * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned; for
+ * nrows times r, rounded up to a multiple of 16, is above 8192.  base may be
+ * NULL (zero) and may be y itself.
+ * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned, and for
+ * many tokens 16 bytes more for every 8 values, or part of them, of the rows of
+ * each of x, A and B whose address or strides are not multiples of 16 bytes.  For
  * many tokens and nnz > 0 its first int is 0 after the call, or nonzero if a
  * kernel's bounded waits ran out.  Queued on `stream`; nothing is allocated.
  */

@@ -61,9 +61,9 @@ SIGNATURES = [
     ("ws_routing_dispatch_backward", _i32, [_p, _p, _i64, _p, _i64, _i64, _i32, _p]),
     ("ws_routing_combine", _i32, [_p, _p, _i64, _p, _i64, _i64, _i32, _p]),
     ("ws_routing_combine_backward", _i32, [_p, _p, _i64, _p, _i64, _p, _i64, _p, _i64, _i32, _p]),
-    ("ws_routing_matmul", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p]),
-    ("ws_routing_matmul_rows", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p]),
-    ("ws_routing_matmul_weights", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _p, _i64, _i64, _i32, _p]),
+    ("ws_routing_matmul", _i32, [_p, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _i32, _p, _i64, _p]),
+    ("ws_routing_matmul_backward", _i32, [_p, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _p, _i64, _i64,
+                                          _i32, _p, _i64, _p]),
     ("ws_adapters_scratch", _i64, [_i64, _i64]),
     ("ws_adapters", _i32, [ctypes.c_char_p, _p, _i64, _p]),
 ]
@@ -274,20 +274,17 @@ def ws_routing_combine_backward(r, gy: int, ldgy: int, ys: int, ldys: int, gys: 
 
 
 def ws_routing_matmul(r, xs: int, ldxs: int, W: int, ldw: int, stride: int, N: int, K: int, ys: int, ldys: int,
-                      dtype: int, stream: int) -> None:
-    _check("ws_routing_matmul", load().ws_routing_matmul(r, xs, ldxs, W, ldw, stride, N, K, ys, ldys, dtype, stream))
+                      dtype: int, scratch: int, scratch_bytes: int, stream: int) -> None:
+    _check("ws_routing_matmul", load().ws_routing_matmul(r, xs, ldxs, W, ldw, stride, N, K, ys, ldys, dtype, scratch,
+                                                         scratch_bytes, stream))
 
 
-def ws_routing_matmul_rows(r, gys: int, ldgys: int, W: int, ldw: int, stride: int, N: int, K: int, gxs: int,
-                           ldgxs: int, dtype: int, stream: int) -> None:
-    _check("ws_routing_matmul_rows", load().ws_routing_matmul_rows(r, gys, ldgys, W, ldw, stride, N, K, gxs, ldgxs,
-                                                                   dtype, stream))
-
-
-def ws_routing_matmul_weights(r, gys: int, ldgys: int, xs: int, ldxs: int, N: int, K: int, gW: int, ldgw: int,
-                              stride: int, dtype: int, stream: int) -> None:
-    _check("ws_routing_matmul_weights", load().ws_routing_matmul_weights(r, gys, ldgys, xs, ldxs, N, K, gW, ldgw,
-                                                                         stride, dtype, stream))
+def ws_routing_matmul_backward(r, gys: int, ldgys: int, xs: int, ldxs: int, W: int, ldw: int, stride: int, N: int,
+                               K: int, gxs: int, ldgxs: int, gW: int, ldgw: int, gstride: int, dtype: int,
+                               scratch: int, scratch_bytes: int, stream: int) -> None:
+    _check("ws_routing_matmul_backward", load().ws_routing_matmul_backward(
+        r, gys, ldgys, xs, ldxs, W, ldw, stride, N, K, gxs, ldgxs, gW, ldgw, gstride, dtype, scratch, scratch_bytes,
+        stream))
 
 
 def ws_adapters_scratch(nnz: int, r: int) -> int:

@@ -438,7 +438,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
 // of 4096 values and rank 16, the time of a lane's 16 steps of loads.)
 constexpr int kStepSplit = 4;
 
-template <bool half>
+// vec: the rows of x and A start at multiples of 16 bytes.
+template <bool half, bool vec>
 __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapters_call c, uint2* __restrict__ h, int rpad) {
   __shared__ float2 part[kAdWarps];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -468,7 +469,7 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
       constexpr int kStep = 256 * kStepSplit, U = 4;  // U steps whose loads are in flight together
       const int k0 = 256 * (warp % kStepSplit);
       int k = k0 + 8 * lane;
-      for (; k - 8 * lane + kStep * (U - 1) + 256 <= K; k += kStep * U) {
+      for (; vec && k - 8 * lane + kStep * (U - 1) + 256 <= K; k += kStep * U) {
         uint4 xv[U], av[U], bv[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -479,7 +480,7 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
 #pragma unroll
         for (int u = 0; u < U; ++u) add(xv[u], av[u], bv[u]);
       }
-      for (; k < K; k += kStep) add(load8(x, k, K), load8(A0, k, K), load8(A1, k, K));
+      for (; k < K; k += kStep) add(load8(x, k, K, vec), load8(A0, k, K, vec), load8(A1, k, K, vec));
       if (2 * p + 1 >= r) s1 = 0.0f;
     }
     s0 = warp_sum(s0);
@@ -532,8 +533,11 @@ ws_status_t launch_step(const ws_adapters_call& c, uint2* h, cudaStream_t s) {
   const int rpad = adapters_rank(c.r);
   const bool vecB = c.r % 4 == 0 && reinterpret_cast<uintptr_t>(c.B) % 8 == 0 && c.ldb % 4 == 0 && c.strideB % 4 == 0;
   const unsigned T = static_cast<unsigned>(c.nrows);
+  const auto rows16 = [](const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; };
+  const bool vec = rows16(c.x, T > 1 ? c.ldx : 0) && rows16(c.A, c.r > 1 ? c.lda : 0) && (c.ncols <= 1 || c.strideA % 8 == 0);
+  const auto shrink = vec ? shrink_step_kernel<half, true> : shrink_step_kernel<half, false>;
   if (c.nnz > 0)
-    shrink_step_kernel<half><<<dim3(T, static_cast<unsigned>(rpad / 2 / (kAdWarps / kStepSplit))), kAdThreads, 0, s>>>(c, h, rpad);
+    shrink<<<dim3(T, static_cast<unsigned>(rpad / 2 / (kAdWarps / kStepSplit))), kAdThreads, 0, s>>>(c, h, rpad);
   expand_step_kernel<half><<<dim3(static_cast<unsigned>((c.N + kAdThreads - 1) / kAdThreads), T), kAdThreads, 0, s>>>(c, h, rpad, vecB);
   return WS_OK;
 }

@@ -428,6 +428,34 @@ __global__ void __launch_bounds__(kDotThreads)
   }
 }
 
+// ------------------------------------------------------------------ rows for the copy engine
+
+// Rows of 16-bit values copied to rows that start at multiples of 16 bytes (the copy engine and 16-byte loads need that): a
+// thread per 16 bytes of the copy, up to three matrices in a launch, no matrix of an expert without rows.
+constexpr int kAlignThreads = 256;
+
+__global__ void __launch_bounds__(kAlignThreads) align_rows_kernel(const AlignedCopies c) {
+  int64_t at = static_cast<int64_t>(blockIdx.x) * kAlignThreads + threadIdx.x;
+  int i = 0;
+  while (i < c.count && at >= c.m[i].groups * c.m[i].rows * c.m[i].packs) at -= c.m[i].groups * c.m[i].rows * c.m[i].packs, ++i;
+  if (i == c.count) return;
+  const AlignedCopy& m = c.m[i];
+  const int64_t line = at / m.packs, group = line / m.rows, row = line - group * m.rows;
+  const int k = 8 * static_cast<int>(at - line * m.packs);
+  if (m.offsets && m.offsets[group] == m.offsets[group + 1]) return;
+  const uint16_t* src = m.src + group * m.stride + row * m.ld + k;
+  uint32_t w[4] = {};
+  if (reinterpret_cast<uintptr_t>(src) % 4 == 0 && k + 8 <= m.width) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = reinterpret_cast<const uint32_t*>(src)[j];
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (k + j < m.width) w[j >> 1] |= static_cast<uint32_t>(src[j]) << (16 * (j & 1));
+  }
+  reinterpret_cast<uint4*>(m.dst)[at] = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 // Calls f with the widest pack (16, 8, 4 or 2 bytes) that every address and row length allows.
 template <typename F>
 void for_pack(uint64_t bits, F f) {
@@ -488,6 +516,12 @@ void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cud
   allow(reinterpret_cast<const void*>(routing_place_kernel), smem);
   routing_count_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
   routing_place_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
+}
+
+void launch_align(const AlignedCopies& c, cudaStream_t s) {
+  int64_t packs = 0;
+  for (int i = 0; i < c.count; ++i) packs += c.m[i].groups * c.m[i].rows * c.m[i].packs;
+  if (packs > 0) align_rows_kernel<<<static_cast<unsigned>((packs + kAlignThreads - 1) / kAlignThreads), kAlignThreads, 0, s>>>(c);
 }
 
 void launch_dispatch(const ws_routing& r, const void* x, int64_t ldx, void* xs, int64_t ldxs, int64_t width,

@@ -97,9 +97,9 @@ __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, u
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Values k .. k + 7 of a row of K (16-byte aligned), zero past its end.
-__device__ __forceinline__ uint4 load8(const uint16_t* row, int k, int K) {
-  if (k + 8 <= K) return *reinterpret_cast<const uint4*>(row + k);
+// Values k .. k + 7 of a row of K, zero past its end; vec: the row is 16-byte aligned.
+__device__ __forceinline__ uint4 load8(const uint16_t* row, int k, int K, bool vec = true) {
+  if (vec && k + 8 <= K) return *reinterpret_cast<const uint4*>(row + k);
   uint32_t w[4] = {};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
@@ -120,6 +120,21 @@ void launch_combine(const ws_routing& r, bool weighted, const void* ys, int64_t 
                     int64_t width, ws_dtype_t dt, int num_sms, cudaStream_t s);
 void launch_combine_backward(const ws_routing& r, const void* gy, int64_t ldgy, const void* ys, int64_t ldys,
                              void* gys, int64_t ldgys, float* gvals, int64_t width, ws_dtype_t dt, cudaStream_t s);
+
+// `groups` matrices of `rows` rows of 16-bit values, copied to contiguous rows of `packs` 16-byte pieces (zeros past the width).
+struct AlignedCopy {
+  const uint16_t* src;
+  int64_t ld, stride, groups, rows;
+  int width;
+  int64_t packs;
+  uint16_t* dst;
+  const int64_t* offsets;  // group g is copied if offsets[g] != offsets[g + 1] (NULL: always)
+};
+struct AlignedCopies {
+  AlignedCopy m[3];
+  int count;
+};
+void launch_align(const AlignedCopies& c, cudaStream_t s);
 
 // Products by column of R (grouped.cu).  x: nnz rows in slot order; w: ncols matrices N x K; 16-bit values, addresses
 // and strides multiples of 16 bytes.  out is not aligned further than its type.

@@ -64,27 +64,70 @@ ws_status_t check_rows(const ws_routing* r, int64_t width, ws_dtype_t dt, std::i
   return WS_OK;
 }
 
-// A 16-bit matrix that the copy engine reads, or (read false) a result.
+// A stack of 16-bit matrices that a kernel reads in 16-byte pieces, or (read false) writes.
 struct Operand {
   const void* p;
-  int64_t rows, width, ld;
+  int64_t groups, rows, width, ld, stride;
   bool read;
+  bool aligned() const {
+    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && (rows <= 1 || ld % 8 == 0) && (groups <= 1 || stride % 8 == 0);
+  }
 };
 
-ws_status_t check_product(const ws_routing* r, int64_t N, int64_t K, ws_dtype_t dt, int64_t group_stride,
-                          std::initializer_list<Operand> all) {
+ws_status_t check_operands(std::initializer_list<Operand> all) {
+  constexpr int64_t kMost = int64_t{1} << 36;
+  for (const Operand& d : all) {
+    if (d.groups == 0 || d.rows == 0 || d.width == 0) continue;
+    if (!d.p) return routing_fail(WS_ERR_INVALID_ARG, "NULL matrix");
+    if ((d.rows > 1 && (d.ld < (d.read ? 0 : d.width) || d.ld >= kMost)) || (d.groups > 1 && (d.stride < 0 || d.stride >= kMost)))
+      return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row, negative or too large");
+    if (reinterpret_cast<uintptr_t>(d.p) % 2) return routing_fail(WS_ERR_INVALID_ARG, "misaligned matrix");
+  }
+  return WS_OK;
+}
+
+// Replaces operands whose rows do not start at multiples of 16 bytes by copies in `scratch` (one launch).
+class Aligner {
+ public:
+  Aligner(void* scratch, int64_t bytes) : at_(static_cast<char*>(scratch)), left_(bytes) {}
+  bool add(Operand* d, const int64_t* offsets = nullptr) {
+    if (d->groups == 0 || d->rows == 0 || d->width == 0) return true;
+    const int64_t packs = (d->width + 7) / 8;
+    if (d->aligned() && (d->rows <= 1 || d->ld >= d->width)) {
+      if (d->rows <= 1) d->ld = 8 * packs;
+      if (d->groups <= 1) d->stride = d->ld * d->rows;
+      return true;
+    }
+    const int64_t need = d->groups * d->rows * packs * 16;
+    if (!at_ || need > left_ || reinterpret_cast<uintptr_t>(at_) % 16) return false;
+    copies_.m[copies_.count++] = {static_cast<const uint16_t*>(d->p), d->ld, d->stride, d->groups, d->rows,
+                                  static_cast<int>(d->width), packs, reinterpret_cast<uint16_t*>(at_), offsets};
+    d->p = at_;
+    d->ld = 8 * packs;
+    d->stride = d->ld * d->rows;
+    at_ += need;
+    left_ -= need;
+    return true;
+  }
+  void run(cudaStream_t s) {
+    if (copies_.count) launch_align(copies_, s);
+  }
+
+ private:
+  char* at_;
+  int64_t left_;
+  AlignedCopies copies_{};
+};
+
+ws_status_t short_scratch() {
+  return routing_fail(WS_ERR_INVALID_ARG, "no room in scratch for copies of operands that are not 16-byte aligned");
+}
+
+ws_status_t check_product(const ws_routing* r, int64_t N, int64_t K, ws_dtype_t dt) {
   if (const ws_status_t st = check(r)) return st;
   if (dt != WS_BF16 && dt != WS_F16) return routing_fail(WS_ERR_DTYPE, "products are of bfloat16 or half matrices");
   if (N < 0 || K < 0) return routing_fail(WS_ERR_INVALID_ARG, "negative size");
   if (N > kMaxWidth || K > kMaxWidth) return routing_fail(WS_ERR_OVERFLOW, "rows of more than 2^24 values");
-  for (const Operand& d : all) {
-    if (d.rows == 0 || d.width == 0) continue;
-    if (!d.p || (d.rows > 1 && d.ld < d.width)) return routing_fail(WS_ERR_INVALID_ARG, "NULL matrix, or row stride smaller than the row");
-    if (reinterpret_cast<uintptr_t>(d.p) % (d.read ? 16 : 2) || (d.read && (d.ld % 8 || d.ld >= int64_t{1} << 36)))
-      return routing_fail(WS_ERR_INVALID_ARG, "operands of a product start and have row strides at multiples of 16 bytes");
-  }
-  if (r->ncols > 1 && (group_stride % 8 || group_stride < 0 || group_stride >= int64_t{1} << 36))
-    return routing_fail(WS_ERR_INVALID_ARG, "matrices of a product are a multiple of 16 bytes apart");
   return WS_OK;
 }
 
@@ -209,45 +252,49 @@ ws_status_t ws_routing_combine_backward(const ws_routing* r, const void* gy, int
 
 ws_status_t ws_routing_matmul(const ws_routing* r, const void* xs, int64_t ldxs, const void* W, int64_t ldw,
                               int64_t stride, int64_t N, int64_t K, void* ys, int64_t ldys, ws_dtype_t dtype,
-                              ws_stream_t stream) {
-  if (const ws_status_t st = check_product(r, N, K, dtype, stride, {{xs, r ? r->nnz : 0, K, ldxs, true}, {W, N, K, ldw, true},
-                                                                    {ys, r ? r->nnz : 0, N, ldys, false}}))
-    return st;
+                              void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
+  if (const ws_status_t st = check_product(r, N, K, dtype)) return st;
+  Operand x{xs, 1, r->nnz, K, ldxs, 0, true}, w{W, r->ncols, N, K, ldw, stride, true};
+  if (const ws_status_t st = check_operands({x, w, {ys, 1, r->nnz, N, ldys, 0, false}})) return st;
   if (r->nnz == 0 || N == 0) return WS_OK;
   if (K == 0) return zero_rows(ys, r->nnz, N, ldys, stream);
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;
-  return launch_grouped({r, dtype == WS_F16, xs, ldxs, W, ldw, stride, ys, ldys, N, K}, false, sms, cuda_stream(stream));
+  Aligner align(scratch, scratch_bytes);
+  if (!align.add(&x) || !align.add(&w, r->offsets)) return short_scratch();
+  align.run(cuda_stream(stream));
+  return launch_grouped({r, dtype == WS_F16, x.p, x.ld, w.p, w.ld, w.stride, ys, ldys, N, K}, false, sms, cuda_stream(stream));
 }
 
-ws_status_t ws_routing_matmul_rows(const ws_routing* r, const void* gys, int64_t ldgys, const void* W, int64_t ldw,
-                                   int64_t stride, int64_t N, int64_t K, void* gxs, int64_t ldgxs, ws_dtype_t dtype,
-                                   ws_stream_t stream) {
-  if (const ws_status_t st = check_product(r, N, K, dtype, stride, {{gys, r ? r->nnz : 0, N, ldgys, true}, {W, N, K, ldw, true},
-                                                                    {gxs, r ? r->nnz : 0, K, ldgxs, false}}))
+ws_status_t ws_routing_matmul_backward(const ws_routing* r, const void* gys, int64_t ldgys, const void* xs, int64_t ldxs,
+                                       const void* W, int64_t ldw, int64_t stride, int64_t N, int64_t K, void* gxs,
+                                       int64_t ldgxs, void* gW, int64_t ldgw, int64_t gstride, ws_dtype_t dtype,
+                                       void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
+  if (const ws_status_t st = check_product(r, N, K, dtype)) return st;
+  Operand g{gys, 1, r->nnz, N, ldgys, 0, true};
+  Operand x{xs, 1, gW ? r->nnz : 0, K, ldxs, 0, true}, w{W, gxs ? r->ncols : 0, N, K, ldw, stride, true};
+  if (const ws_status_t st = check_operands({g, x, w, {gxs, 1, gxs ? r->nnz : 0, K, ldgxs, 0, false},
+                                             {gW, gW ? r->ncols : 0, N, K, ldgw, gstride, false}}))
     return st;
-  if (r->nnz == 0 || K == 0) return WS_OK;
-  if (N == 0) return zero_rows(gxs, r->nnz, K, ldgxs, stream);
-  int sms = 0;
-  if (const ws_status_t st = sm_count(&sms)) return st;
-  return launch_grouped({r, dtype == WS_F16, gys, ldgys, W, ldw, stride, gxs, ldgxs, N, K}, true, sms, cuda_stream(stream));
-}
-
-ws_status_t ws_routing_matmul_weights(const ws_routing* r, const void* gys, int64_t ldgys, const void* xs,
-                                      int64_t ldxs, int64_t N, int64_t K, void* gW, int64_t ldgw, int64_t stride,
-                                      ws_dtype_t dtype, ws_stream_t stream) {
-  if (const ws_status_t st = check_product(r, N, K, dtype, 0, {{gys, r ? r->nnz : 0, N, ldgys, true}, {xs, r ? r->nnz : 0, K, ldxs, true},
-                                                               {gW, N, K, ldgw, false}}))
-    return st;
-  if (r->ncols == 0 || N == 0 || K == 0) return WS_OK;
-  if (r->nnz == 0) {
+  const bool rows = gxs && r->nnz > 0 && K > 0, weights = gW && r->ncols > 0 && N > 0 && K > 0;
+  if (rows && N == 0)
+    if (const ws_status_t st = zero_rows(gxs, r->nnz, K, ldgxs, stream)) return st;
+  if (weights && r->nnz == 0)
     for (int64_t e = 0; e < r->ncols; ++e)
-      if (const ws_status_t st = zero_rows(static_cast<char*>(gW) + 2 * e * stride, N, K, ldgw, stream)) return st;
-    return WS_OK;
-  }
+      if (const ws_status_t st = zero_rows(static_cast<char*>(gW) + 2 * e * gstride, N, K, ldgw, stream)) return st;
+  if (r->nnz == 0 || N == 0 || (!rows && !weights)) return WS_OK;
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;
-  return launch_grouped_weights({r, dtype == WS_F16, xs, ldxs, nullptr, 0, stride, gW, ldgw, N, K}, gys, ldgys, sms, cuda_stream(stream));
+  Aligner align(scratch, scratch_bytes);
+  if (!align.add(&g) || !align.add(&x) || !align.add(&w, r->offsets)) return short_scratch();
+  align.run(cuda_stream(stream));
+  if (rows)
+    if (const ws_status_t st = launch_grouped({r, dtype == WS_F16, g.p, g.ld, w.p, w.ld, w.stride, gxs, ldgxs, N, K}, true, sms,
+                                              cuda_stream(stream)))
+      return st;
+  return weights ? launch_grouped_weights({r, dtype == WS_F16, x.p, x.ld, nullptr, 0, gstride, gW, ldgw, N, K}, g.p, g.ld, sms,
+                                          cuda_stream(stream))
+                 : WS_OK;
 }
 
 int64_t ws_adapters_scratch(int64_t nnz, int64_t r) {
@@ -263,28 +310,27 @@ ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scr
   if (c.nrows > INT32_MAX || c.ncols > INT32_MAX || c.nnz > INT32_MAX || c.K > kMaxWidth || c.N > kMaxWidth || c.r > 4096)
     return routing_fail(WS_ERR_OVERFLOW, "at most %d rows, columns and entries, rows of 2^24 values, rank 4096", INT32_MAX);
   if (c.nnz > 0 && (c.nrows == 0 || c.ncols == 0)) return routing_fail(WS_ERR_SHAPE, "entries in a matrix without rows or columns");
-  const bool used = c.nrows > 0 && c.N > 0, prompt = !adapters_step(c.nrows, c.r);
+  const bool used = c.nrows > 0 && c.N > 0;
   const bool inner = used && c.nnz > 0 && c.r > 0 && c.K > 0;
-  if (!c.rowptr || (c.nnz > 0 && (!c.colidx || !c.vals)) || (used && (!c.y || !scratch)) || (inner && (!c.x || !c.A || !c.B)))
+  if (!c.rowptr || (c.nnz > 0 && (!c.colidx || !c.vals)) || (used && !scratch))
     return routing_fail(WS_ERR_INVALID_ARG, "NULL pointer");
-  if (used && c.nrows > 1 && (c.ldy < c.N || (c.base && c.ldbase < c.N)))
-    return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
-  if (inner) {
-    const auto off16 = [](const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 != 0 || ld % 8 != 0; };
-    if (off16(c.x, c.nrows > 1 ? c.ldx : 0) || off16(c.A, c.r > 1 ? c.lda : 0) || (c.ncols > 1 && c.strideA % 8))
-      return routing_fail(WS_ERR_INVALID_ARG, "x and A start and have strides at multiples of 16 bytes");
-    if (prompt && (off16(c.B, c.N > 1 ? c.ldb : 0) || (c.ncols > 1 && c.strideB % 8)))
-      return routing_fail(WS_ERR_INVALID_ARG, "for many tokens B starts and has strides at multiples of 16 bytes");
-    if ((c.nrows > 1 && c.ldx < c.K) || (c.r > 1 && c.lda < c.K) || (c.N > 1 && c.ldb < c.r) || c.strideA < 0 || c.strideB < 0)
-      return routing_fail(WS_ERR_INVALID_ARG, "row stride smaller than the row");
-  }
-  if (used && (scratch_bytes < ws_adapters_scratch(inner ? c.nnz : 0, c.r) || reinterpret_cast<uintptr_t>(scratch) % 16))
+  Operand x{c.x, 1, inner ? c.nrows : 0, c.K, c.ldx, 0, true}, A{c.A, inner ? c.ncols : 0, c.r, c.K, c.lda, c.strideA, true},
+      B{c.B, inner ? c.ncols : 0, c.N, c.r, c.ldb, c.strideB, true};
+  if (const ws_status_t st = check_operands({x, A, B, {c.y, 1, c.nrows, c.N, c.ldy, 0, false},
+                                             {c.base, 1, c.base ? c.nrows : 0, c.N, c.ldbase, 0, false}}))
+    return st;
+  const int64_t own = ws_adapters_scratch(inner ? c.nnz : 0, c.r);
+  if (used && (scratch_bytes < own || reinterpret_cast<uintptr_t>(scratch) % 16))
     return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_adapters_scratch, or misaligned");
-  if ((reinterpret_cast<uintptr_t>(c.y) | reinterpret_cast<uintptr_t>(c.base) | reinterpret_cast<uintptr_t>(c.B)) % 2)
-    return routing_fail(WS_ERR_INVALID_ARG, "misaligned matrix");
   if (!used) return WS_OK;
   ws_adapters_call run = c;
   if (!inner) run.nnz = 0;  // nothing to add: entry ranges are cut to [0, 0]
+  if (inner && !adapters_step(c.nrows, c.r)) {
+    Aligner align(static_cast<char*>(scratch) + own, scratch_bytes - own);
+    if (!align.add(&x) || !align.add(&A) || !align.add(&B)) return short_scratch();
+    align.run(cuda_stream(stream));
+    run.x = x.p, run.ldx = x.ld, run.A = A.p, run.lda = A.ld, run.strideA = A.stride, run.B = B.p, run.ldb = B.ld, run.strideB = B.stride;
+  }
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;
   if (const ws_status_t st = launch_adapters(run, scratch, sms, cuda_stream(stream))) return st;

@@ -66,19 +66,31 @@ def _matrix(t: torch.Tensor, name: str, rows: int | None):
 
 
 def _operand(t: torch.Tensor):
-    """(t, its row stride, that of the matrices of a stack): a matrix or a stack of matrices of 16-bit values whose rows
-    start at multiples of 16 bytes; t itself, or a copy with longer rows where t's do not."""
-    n = t.shape[-1]
-    if t.data_ptr() % 16 == 0:
-        if n % 8 == 0 and t.is_contiguous():
-            return t, n, n * t.shape[-2]
-        if (n <= 1 or t.stride(-1) == 1) and \
-                all(t.shape[i] == 1 or (t.stride(i) % 8 == 0 and t.stride(i) >= n) for i in range(t.dim() - 1)):
-            ld = t.stride(-2) if t.shape[-2] > 1 else (n + 7) // 8 * 8
-            return t, ld, t.stride(0) if t.dim() == 3 and t.shape[0] > 1 else ld * t.shape[-2]
-    ld = (n + 7) // 8 * 8
-    out = torch.empty((*t.shape[:-1], ld), dtype=t.dtype, device=t.device)[..., :n]
-    return out.copy_(t), ld, ld * t.shape[-2]
+    """(t, its row stride, that of a stack's matrices, bytes of a copy): a matrix or a stack of matrices of 16-bit
+    values with unit stride within a row.  The copy is made by the call where rows do not start at multiples of 16
+    bytes."""
+    shape = t.shape
+    n, rows = shape[-1], shape[-2]
+    if t.is_contiguous():
+        if n % 8 == 0 and t.data_ptr() % 16 == 0:
+            return t, n, n * rows, 0
+        return t, n, n * rows, t.numel() // max(n, 1) * ((n + 7) // 8 * 16)
+    if n > 1 and t.stride(-1) != 1:
+        return _operand(t.contiguous())
+    ld = t.stride(-2)
+    apart = t.stride(0) if t.dim() == 3 else 0
+    if t.data_ptr() % 16 == 0 and (rows <= 1 or (ld % 8 == 0 and ld >= n)) and \
+            (t.dim() == 2 or shape[0] <= 1 or apart % 8 == 0):
+        return t, ld, apart, 0
+    return t, ld, apart, t.numel() // max(n, 1) * ((n + 7) // 8 * 16)
+
+
+def _room(need: int, device):
+    """(tensor, address) of scratch; (None, 0) where none is needed."""
+    if need == 0:
+        return None, 0
+    t = torch.empty(need, dtype=torch.uint8, device=device)
+    return t, t.data_ptr()
 
 
 def topk_route(logits: torch.Tensor, k: int, normalize: bool = True, stream=None) -> DeviceCSR:
@@ -245,26 +257,28 @@ class Routing:
                                          gvals.data_ptr(), H, dt, self._queue(ys))
         return out, gvals
 
-    def _experts(self, W: torch.Tensor, like: torch.Tensor):
+    def _product(self, xs: torch.Tensor, W: torch.Tensor) -> int:
+        dt = _dtype(xs, "xs")
         if W.dim() != 3 or W.shape[0] != self.R.ncols:
             raise ValueError(f"W must be {self.R.ncols} matrices, got {tuple(W.shape)}")
-        _same(W, like, "W")
-        return _operand(W)
+        _same(W, xs, "W")
+        if xs.dim() != 2 or xs.shape[0] != self.nnz or xs.shape[1] != W.shape[2]:
+            raise ValueError(f"xs must be {self.nnz} rows of {W.shape[2]} values, got {tuple(xs.shape)}")
+        return dt
 
     def matmul(self, xs: torch.Tensor, W: torch.Tensor, stream=None) -> torch.Tensor:
         """ys[s] = W[e] xs[s] for the rows s of every column e: xs nnz x K in slot order, W E x N x K, bfloat16 or
         float16; products and sums in 32 bits, rounded once.  Rows behind the placed entries are left unwritten."""
         if stream is not None:
             return _elsewhere(self.matmul, stream, xs, W)
-        dt = _dtype(xs, "xs")
-        xs, ldx, _ = _operand(_matrix(xs, "xs", self.nnz)[0])
-        W, ldw, apart = self._experts(W, xs)
-        (_, N, K), Z = W.shape, self.nnz
-        if xs.shape[1] != K:
-            raise ValueError(f"rows of {xs.shape[1]} values do not fit matrices of {K} columns")
-        out = torch.empty((Z, N), dtype=xs.dtype, device=self.device)
-        _abi.ws_routing_matmul(self._r, xs.data_ptr(), ldx, W.data_ptr(), ldw, apart, N, K, out.data_ptr(), N, dt,
-                               self._queue(xs))
+        dt = self._product(xs, W)
+        _, N, K = W.shape
+        xs, ldx, _, a = _operand(xs)
+        W, ldw, apart, b = _operand(W)
+        out = torch.empty((self.nnz, N), dtype=xs.dtype, device=self.device)
+        room, at = _room(a + b, self.device)
+        _abi.ws_routing_matmul(self._r, xs.data_ptr(), ldx, W.data_ptr(), ldw, apart, N, K, out.data_ptr(), N, dt, at,
+                               a + b, self._queue(xs))
         return out
 
     def matmul_backward(self, grad_ys: torch.Tensor, xs: torch.Tensor, W: torch.Tensor, stream=None):
@@ -272,20 +286,19 @@ class Routing:
         column without entries), in their types."""
         if stream is not None:
             return _elsewhere(self.matmul_backward, stream, grad_ys, xs, W)
-        dt = _dtype(xs, "xs")
+        dt = self._product(xs, W)
+        E, N, K = W.shape
         _same(grad_ys, xs, "grad_ys")
-        xs, ldx, _ = _operand(_matrix(xs, "xs", self.nnz)[0])
-        g, ldg, _ = _operand(_matrix(grad_ys, "grad_ys", self.nnz)[0])
-        W, ldw, apart = self._experts(W, xs)
-        (E, N, K), Z, raw = W.shape, self.nnz, self._queue(xs)
-        if xs.shape[1] != K or g.shape[1] != N:
-            raise ValueError(f"rows of {xs.shape[1]} and {g.shape[1]} values do not fit matrices {N} x {K}")
-        gxs = torch.empty((Z, K), dtype=xs.dtype, device=self.device)
+        if grad_ys.dim() != 2 or grad_ys.shape[0] != self.nnz or grad_ys.shape[1] != N:
+            raise ValueError(f"grad_ys must be {self.nnz} rows of {N} values, got {tuple(grad_ys.shape)}")
+        g, ldg, _, a = _operand(grad_ys)
+        xs, ldx, _, b = _operand(xs)
+        W, ldw, apart, c = _operand(W)
+        gxs = torch.empty((self.nnz, K), dtype=xs.dtype, device=self.device)
         gW = torch.empty((E, N, K), dtype=xs.dtype, device=self.device)
-        _abi.ws_routing_matmul_rows(self._r, g.data_ptr(), ldg, W.data_ptr(), ldw, apart, N, K, gxs.data_ptr(), K, dt,
-                                    raw)
-        _abi.ws_routing_matmul_weights(self._r, g.data_ptr(), ldg, xs.data_ptr(), ldx, N, K, gW.data_ptr(), K, N * K,
-                                       dt, raw)
+        room, at = _room(a + b + c, self.device)
+        _abi.ws_routing_matmul_backward(self._r, g.data_ptr(), ldg, xs.data_ptr(), ldx, W.data_ptr(), ldw, apart, N, K,
+                                        gxs.data_ptr(), K, gW.data_ptr(), K, N * K, dt, at, a + b + c, self._queue(xs))
         return gxs, gW
 
     def wait(self, stream=None) -> None:
@@ -322,16 +335,14 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     nnz = colidx.numel()
     if S.ncols != L or rowptr.numel() != T + 1 or vals.numel() != nnz:
         raise ValueError(f"S must be {x.shape[0]} x {L} in CSR")
-    x, ldx, _ = _operand(_matrix(x, "x", T)[0])
-    if x.shape[1] != K:
-        raise ValueError(f"rows of {x.shape[1]} values do not fit adapters of {K}")
-    A, lda, apart = _operand(A)
-    if T * ((r + 15) // 16 * 16) > 8192:  # many tokens: the copy engine reads B
-        B, ldb, apartB = _operand(B)
-    else:
-        if not B.is_contiguous() and ((r > 1 and B.stride(2) != 1) or (N > 1 and B.stride(1) < r)):
-            B = B.contiguous()
-        ldb, apartB = B.stride(1), B.stride(0)
+    if x.dim() != 2 or x.shape[0] != T or x.shape[1] != K:
+        raise ValueError(f"x must be {T} rows of {K} values, got {tuple(x.shape)}")
+    x, ldx, _, need = _operand(x)
+    A, lda, apart, more = _operand(A)
+    B, ldb, apartB, most = _operand(B)
+    # ws_adapters_scratch, and copies for many tokens
+    rank = (r + 15) // 16 * 16
+    need = 16 + nnz * rank * 16 + (need + more + most if T * rank > 8192 else 0)
     ldbase = ldy = N
     if base is not None:
         _same(base, x, "base")
@@ -347,7 +358,6 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
             raise ValueError(f"out must be {T} x {N} with unit stride within its rows")
         if base is not None and (out.data_ptr(), ldy) != (base.data_ptr(), ldbase) and _overlap(out, base):
             raise ValueError("out must be base itself or lie apart from it")
-    need = 16 + nnz * ((r + 15) // 16 * 256)  # ws_adapters_scratch
     scratch = torch.empty(need, dtype=torch.uint8, device=dev)
     call = _abi.ADAPTERS_CALL.pack(T, L, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), K, r, N,
                                    x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), ldb, apartB,

@@ -196,6 +196,12 @@ def test_refusals():
     assert e.value.status_name == "WS_ERR_DTYPE"
     with pytest.raises(ValueError):
         plan.matmul_backward(torch.zeros((7, 9), dtype=torch.bfloat16, device="cuda"), x, W)
-    with pytest.raises(_abi.WsError) as e:  # rows of 2 bytes' alignment at the C entry
-        _abi.ws_routing_matmul(plan._r, x.data_ptr() + 2, 16, W.data_ptr(), 16, 128, 8, 16, x.data_ptr(), 8, _abi.WS_BF16, 0)
-    assert e.value.status_name == "WS_ERR_INVALID_ARG"
+    def call(ptr, room, size):
+        _abi.ws_routing_matmul(plan._r, ptr, 16, W.data_ptr(), 16, 128, 8, 16, out.data_ptr(), 8, _abi.WS_BF16, room, size, 0)
+
+    out, room = torch.zeros((7, 8), dtype=torch.bfloat16, device="cuda"), torch.zeros(1024, dtype=torch.uint8, device="cuda")
+    for ptr, at, size in ((x.data_ptr() + 2, 0, 0), (x.data_ptr() + 2, room.data_ptr(), 16), (x.data_ptr() + 2, room.data_ptr() + 8, 512),
+                          (x.data_ptr() + 1, room.data_ptr(), 1024)):  # no room for an aligned copy; odd address
+        with pytest.raises(_abi.WsError) as e:
+            call(ptr, at, size)
+        assert e.value.status_name == "WS_ERR_INVALID_ARG"
