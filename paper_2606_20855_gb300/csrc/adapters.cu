@@ -377,13 +377,21 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
     }
     if (mine) w.next(c);
   }
+  // Without the copy engine (rows that do not start at multiples of 16 bytes) the warps move base and y along their rows.
+  const auto place = [&](int row, int col) { return sy + (col >> 6) * kExpandY + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4) + 2 * (col & 7); };
+  const int columns = min(kExpandN, N - n0);
+  const int64_t rows = min(static_cast<int64_t>(kTok), c.nrows - t0);
+  if (!copies && c.base) {
+    const uint16_t* src = static_cast<const uint16_t*>(c.base) + t0 * c.ldbase + n0;
+    for (int row = warp; row < rows; row += kExpandThreads / 32)
+      for (int col = threadIdx.x & 31; col < columns; col += 32)
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(place(row, col)), "h"(src[row * c.ldbase + col]) : "memory");
+  }
   if (done > 0) bar_wait(smem_u32(&m_bar), (done - 1) & 1, &dead);
   if (copies && c.base) bar_wait(smem_u32(&base_bar), 0, &dead);
   __syncthreads();
   if (!dead) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    const uint16_t* base = static_cast<const uint16_t*>(c.base) + (c.base && there ? t * c.ldbase + n0 : 0);
-    uint16_t* y = static_cast<uint16_t*>(c.y) + (there ? t * c.ldy + n0 : 0);
 #pragma unroll 1
     for (int j = side * (kExpandN / 2); j < (side + 1) * (kExpandN / 2); j += 16) {
       const int left = N - n0 - j;
@@ -396,22 +404,17 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
         for (int i = 0; i < 16; ++i)
           if (i < left && !(fabsf(f[i]) <= 3.4e38f)) f[i] = added<half>(c, h, rpad, split, t, n0 + j + i);
       }
-      if (copies) {
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const uint32_t at = sy + (j >> 6) * kExpandY + m * 128 + (((((j & 63) >> 3) + s) ^ (m & 7)) << 4);
-          uint32_t b[4] = {};
-          if (c.base)
-            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at) : "memory");
+      for (int s = 0; s < 2; ++s) {
+        const uint32_t at = place(m, j + 8 * s);
+        uint32_t b[4] = {};
+        if (c.base)
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at) : "memory");
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            b[i] = bits16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i]) |
-                   static_cast<uint32_t>(bits16<half>(value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1])) << 16;
-          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
-        }
-      } else if (there) {
-        for (int i = 0; i < 16; ++i)
-          if (i < left) y[j + i] = bits16<half>((c.base ? value16<half>(base[j + i]) : 0.0f) + f[i]);
+        for (int i = 0; i < 4; ++i)
+          b[i] = bits16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i]) |
+                 static_cast<uint32_t>(bits16<half>(value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1])) << 16;
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
       }
     }
   }
@@ -426,6 +429,15 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
     for (int i = 0; i < pieces; ++i) tma_store_2d(&map_y, sy + i * kExpandY, n0 + 64 * i, static_cast<int>(t0));
     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
     asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+  }
+  if (!copies && !dead) {
+    uint16_t* dst = static_cast<uint16_t*>(c.y) + t0 * c.ldy + n0;
+    for (int row = warp; row < rows; row += kExpandThreads / 32)
+      for (int col = threadIdx.x & 31; col < columns; col += 32) {
+        uint16_t v;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(place(row, col)) : "memory");
+        dst[row * c.ldy + col] = v;
+      }
   }
   __syncwarp();
   __syncthreads();

@@ -31,6 +31,7 @@ constexpr int kTileM = 128;   // rows of the M side: lanes of tensor memory
 constexpr int kTileK = 64;    // 128 bytes: the swizzle's span
 constexpr int kThreads = 192; // TMA warp, MMA warp, 4 epilogue warps
 constexpr int kBytesA = kTileM * kTileK * 2;
+constexpr int kTurnBytes = 32 * 128;
 
 // Where the rows of the experts are in the product D (M x N tile).
 constexpr int kRowsM = 0;    // on the M side (lanes)
@@ -75,7 +76,7 @@ struct Shape {
   static constexpr int kStageBytes = kBytesA + kBytesB;
   static constexpr int kStages = (196 * 1024) / kStageBytes > 10 ? 10 : (196 * 1024) / kStageBytes;
   static constexpr int kAccCols = 2 * BN < 32 ? 32 : 2 * BN;  // a power of two
-  static constexpr size_t kSmem = static_cast<size_t>(kStages) * kStageBytes + 1024;
+  static constexpr size_t kSmem = static_cast<size_t>(kStages) * kStageBytes + (kRows == kRowsN ? 0 : 4 * kTurnBytes) + 1024;
 };
 
 // Tile t of the sequence that all roles of all CTAs share.  first[e]: row tiles of the groups before e.
@@ -124,40 +125,59 @@ __device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first
   return true;
 }
 
-// Where a warp turns 32 rows of 16 values, one row a lane, so that its lanes store along rows.
-using Stage = uint16_t[32][18];
-
-// Stores 16 values of a row of the result, `count` of them inside it; on: the lane's row is stored.
-// Rows that start at multiples of 16 bytes take two stores a lane; others go through `stage`, as a lane's 2-byte stores would
-// touch 32 rows at a time (3003 rows of 1003 values, K = 1000: 54 us so, 23 us turned).
-__device__ __forceinline__ void store_rows16(const GroupedParams& p, uint16_t* dst, const float (&f)[16], int count, bool on,
-                                             Stage& stage) {
-  if (!p.vec) {
-    const int lane = threadIdx.x & 31;
+// A warp's 32 rows of 64 values on their way to memory: a row of 128 bytes a lane in shared memory, its 16-byte pieces placed by the
+// row's last three bits, so that lanes that write rows and lanes that read along them meet no bank twice.
+// Stores 64 values (from column 0 of dst on, `left` of them inside the result) of the warp's 32 rows; on(row): the row is stored.
+// A lane's own row would be 32 rows a store; turned, a store covers four rows of 128 bytes (or, where rows are not 16-byte aligned, one
+// row), which leaves the load-store unit to the tile's 2 us less often: 17 experts' gradients of 1003 x 1000 from 177 rows each
+// 26 us without, %TURN% us.
+template <typename On>
+__device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t turn, uint16_t* dst, const float (&f)[64], int left, On on) {
+  const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) stage[lane][i] = round16(f[i], p.half);
-    __syncwarp();
+  for (int j = 0; j < 8; ++j) {
+    uint32_t w[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int row = 2 * i + (lane >> 4), col = lane & 15;
-      uint16_t* to = reinterpret_cast<uint16_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), row));
-      if (__shfl_sync(0xffffffffu, on, row) && col < count) to[col] = stage[row][col];
+    for (int i = 0; i < 4; ++i)
+      w[i] = round16(f[8 * j + 2 * i], p.half) | static_cast<uint32_t>(round16(f[8 * j + 2 * i + 1], p.half)) << 16;
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(turn + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]),
+                 "r"(w[2]), "r"(w[3])
+                 : "memory");
+  }
+  __syncwarp();
+  if (p.vec) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int row = 4 * i + (lane >> 3), j = lane & 7;
+      uint32_t w[4];
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                   : "r"(turn + row * 128 + ((j ^ (row & 7)) << 4))
+                   : "memory");
+      if (!on(row)) continue;
+      uint16_t* to = dst + row * p.ldo + 8 * j;
+      if (8 * j + 8 <= left) {
+        *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (8 * j + e < left) to[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+      }
     }
-    __syncwarp();
-    return;
-  }
-  if (!on) return;
-  if (count >= 16) {
-    uint32_t w[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = round16(f[2 * i], p.half) | static_cast<uint32_t>(round16(f[2 * i + 1], p.half)) << 16;
-    reinterpret_cast<uint4*>(dst)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-    reinterpret_cast<uint4*>(dst)[1] = make_uint4(w[4], w[5], w[6], w[7]);
   } else {
+#pragma unroll 4
+    for (int row = 0; row < 32; ++row) {
+      if (!on(row)) continue;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < count) dst[i] = round16(f[i], p.half);
+      for (int side = 0; side < 2; ++side) {
+        const int col = 32 * side + lane;
+        uint16_t v;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(turn + row * 128 + (((col >> 3) ^ (row & 7)) << 4) + 2 * (col & 7)) : "memory");
+        if (col < left) dst[row * p.ldo + col] = v;
+      }
+    }
   }
+  __syncwarp();
 }
 
 // a: the M side's operand (kRowsM: the experts' rows, kRowsN: W, kRowsSum: gys), b: the N side's.
@@ -174,7 +194,6 @@ __global__ void __launch_bounds__(kThreads, 1)
   __shared__ int scratch[32];
   __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages], acc_full[2], acc_empty[2], last_bar;
   __shared__ uint32_t tmem_slot;
-  __shared__ Stage stage[kRows == kRowsN ? 1 : 4];
   __shared__ volatile int dead;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -319,25 +338,14 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
-      const int m = quarter * 32 + lane;
       const uint32_t addr = tmem + acc * BN + (static_cast<uint32_t>(quarter * 32) << 16);
+      if constexpr (kRows == kRowsN) {
+        const int m = quarter * 32 + lane;
 #pragma unroll 1
-      for (int c = 0; c < BN; c += 16) {
-        float f[16] = {};
-        if constexpr (kRows == kRowsM) {
-          const int left = p.features - t.n0 - c;
-          if (left <= 0) break;
-          if (t.steps > 0) tmem_load16(addr + c, f);
-          store_rows16(p, result + (static_cast<int64_t>(t.row0) + m) * p.ldo + t.n0 + c, f, left, m < t.rows, stage[quarter]);
-        } else if constexpr (kRows == kRowsSum) {
-          const int left = p.width - t.n0 - c;
-          if (left <= 0) break;
-          if (t.steps > 0) tmem_load16(addr + c, f);
-          store_rows16(p, result + t.group * p.group_stride + (static_cast<int64_t>(t.m0) + m) * p.ldo + t.n0 + c, f, left,
-                       t.m0 + m < p.features, stage[quarter]);
-        } else {
+        for (int c = 0; c < BN; c += 16) {
           const int left = t.rows - c;
           if (left <= 0) break;
+          float f[16] = {};
           if (t.steps > 0) tmem_load16(addr + c, f);
           if (t.m0 + m < p.features) {
             uint16_t* dst = result + (static_cast<int64_t>(t.row0) + c) * p.ldo + t.m0 + m;
@@ -345,6 +353,20 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int j = 0; j < 16; ++j)
               if (j < left) dst[j * p.ldo] = round16(f[j], p.half);
           }
+        }
+      } else {
+        const uint32_t turn = base + S::kStages * S::kStageBytes + quarter * kTurnBytes;
+        const int columns = kRows == kRowsM ? p.features : p.width;
+        const int lines = (kRows == kRowsM ? t.rows : p.features - t.m0) - quarter * 32;  // rows of the warp that are stored
+        uint16_t* const to = kRows == kRowsM ? result + (static_cast<int64_t>(t.row0) + quarter * 32) * p.ldo + t.n0
+                                             : result + t.group * p.group_stride + (static_cast<int64_t>(t.m0) + quarter * 32) * p.ldo + t.n0;
+#pragma unroll 1
+        for (int c = 0; c < BN; c += 64) {
+          const int left = columns - t.n0 - c;
+          if (left <= 0 || lines <= 0) break;
+          float f[64] = {};
+          if (t.steps > 0) tmem_load64(addr + c, f);
+          store_turned(p, turn, to + c, f, left, [&](int row) { return row < lines; });
         }
       }
       if (t.steps > 0) {
@@ -520,8 +542,10 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
     else return launch_thin(g, s);
   }
   if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>());
-  // Tiles of 256 features where they still give every SM one, else of 128.
-  if ((g.r->nnz / kTileM + met / 2) * up(features, 256) >= num_sms)
+  // A tile of 128 features takes two thirds of the time of one of 256 (bound by its operands' way from L2), so the wider one is
+  // taken unless the narrower fills the SMs' last turn so much better.
+  const int64_t row_tiles = g.r->nnz / kTileM + up(met, 2);
+  if (3 * up(row_tiles * up(features, 256), num_sms) <= 2 * up(row_tiles * up(features, 128), num_sms))
     return run(integral_constant<int, 256>(), integral_constant<int, kRowsM>());
   return run(integral_constant<int, 128>(), integral_constant<int, kRowsM>());
 }

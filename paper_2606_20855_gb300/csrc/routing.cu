@@ -141,11 +141,10 @@ __device__ __forceinline__ void write_offsets(const ws_routing& r, int cols, con
 }
 
 // Entries of column e in the warps' rows; pre[w * cols + e] receives those of the warps before w.
-template <int W>
-__device__ __forceinline__ int count_column(const uint32_t* mask, uint16_t* pre, int cols, int e) {
+__device__ __forceinline__ int count_column(const uint32_t* mask, uint16_t* pre, int cols, int e, int warps) {
   int n = 0;
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
+#pragma unroll 8
+  for (int w = 0; w < warps; ++w) {
     pre[w * cols + e] = static_cast<uint16_t>(n);
     n += __popc(mask[w * cols + e]);
   }
@@ -153,22 +152,23 @@ __device__ __forceinline__ int count_column(const uint32_t* mask, uint16_t* pre,
 }
 
 // Shared memory: mask [W][cols], two int arrays [cols], pre [W][cols].
-template <int W>
-size_t build_smem(int cols) { return static_cast<size_t>(cols) * (W * 4 + 8 + W * 2); }
+size_t build_smem(int cols, int W) { return static_cast<size_t>(cols) * (W * 4 + 8 + W * 2); }
 
+// As many warps as the rows need.
 __global__ void __launch_bounds__(32 * kSmallWarps) routing_small_kernel(ws_routing r, int cols) {
+  const int warps = blockDim.x >> 5;
   extern __shared__ __align__(16) int sm[];
   __shared__ int scratch[32];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
-  int* first = sm + kSmallWarps * cols;
+  int* first = sm + warps * cols;
   uint16_t* pre = reinterpret_cast<uint16_t*>(first + 2 * cols);
   WarpRows w;
   w.start(r, threadIdx.x & ~31u);
-  clear_words(mask, kSmallWarps * cols);
+  clear_words(mask, warps * cols);
   __syncthreads();
   mark_rows(r, w, cols, mask);
   __syncthreads();
-  for (int e = threadIdx.x; e < cols; e += blockDim.x) first[e] = count_column<kSmallWarps>(mask, pre, cols, e);
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) first[e] = count_column(mask, pre, cols, e, warps);
   __syncthreads();
   const int placed = scan_columns(cols, first, scratch);
   write_offsets(r, cols, first, placed);
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, 
     __syncthreads();
     mark_rows(r, w, cols, mask);
     __syncthreads();
-    for (int e = threadIdx.x; e < cols; e += blockDim.x) before[e] = count_column<kBuildWarps>(mask, pre, cols, e);
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) before[e] = count_column(mask, pre, cols, e, kBuildWarps);
     __syncthreads();
     place_rows(r, w, cols, mask, pre, next);
     __syncthreads();
@@ -504,12 +504,13 @@ void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cud
     if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   };
   if (chunks == 1) {
-    const size_t smem = build_smem<kSmallWarps>(cols);
+    const int warps = r.nrows <= 128 ? 4 : static_cast<int>((r.nrows + 31) / 32);  // four at least, for the columns
+    const size_t smem = build_smem(cols, warps);
     allow(reinterpret_cast<const void*>(routing_small_kernel), smem);
-    routing_small_kernel<<<1, 32 * kSmallWarps, smem, s>>>(r, cols);
+    routing_small_kernel<<<1, 32 * warps, smem, s>>>(r, cols);
     return;
   }
-  const size_t smem = build_smem<kBuildWarps>(cols);
+  const size_t smem = build_smem(cols, kBuildWarps);
   const int64_t tiles = (r.nrows + kTileRows - 1) / kTileRows;
   const int64_t chunk = (tiles + chunks - 1) / chunks * kTileRows;
   allow(reinterpret_cast<const void*>(routing_count_kernel), smem);
