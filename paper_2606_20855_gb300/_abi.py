@@ -235,14 +235,17 @@ def ws_rowptr_scan_static(rowptr: int, nrows: int, stream: int) -> None:
 
 def ws_topk_route(logits: int, rows: int, cols: int, ld: int, dtype: int, k: int, normalize: bool, rowptr: int,
                   colidx: int, vals: int, stream: int) -> None:
-    _check("ws_topk_route", load().ws_topk_route(logits, rows, cols, ld, dtype, k, normalize, rowptr, colidx, vals,
-                                                 stream))
+    status = (_lib or load()).ws_topk_route(logits, rows, cols, ld, dtype, k, normalize, rowptr, colidx, vals, stream)
+    if status:
+        _check("ws_topk_route", status)
 
 
 def ws_topk_route_backward(logits: int, rows: int, cols: int, ld: int, dtype: int, k: int, normalize: bool,
                            colidx: int, vals: int, gvals: int, glogits: int, ldg: int, stream: int) -> None:
-    _check("ws_topk_route_backward", load().ws_topk_route_backward(logits, rows, cols, ld, dtype, k, normalize, colidx,
-                                                                   vals, gvals, glogits, ldg, stream))
+    status = (_lib or load()).ws_topk_route_backward(
+        logits, rows, cols, ld, dtype, k, normalize, colidx, vals, gvals, glogits, ldg, stream)
+    if status:
+        _check("ws_topk_route_backward", status)
 
 
 def ws_routing_scratch(nrows: int, ncols: int) -> int:
@@ -250,41 +253,54 @@ def ws_routing_scratch(nrows: int, ncols: int) -> int:
 
 
 def ws_routing_build(r, scratch: int, scratch_bytes: int, stream: int) -> None:
-    _check("ws_routing_build", load().ws_routing_build(r, scratch, scratch_bytes, stream))
+    status = (_lib or load()).ws_routing_build(r, scratch, scratch_bytes, stream)
+    if status:
+        _check("ws_routing_build", status)
 
 
 def ws_routing_dispatch(r, x: int, ldx: int, xs: int, ldxs: int, width: int, dtype: int, stream: int) -> None:
-    _check("ws_routing_dispatch", load().ws_routing_dispatch(r, x, ldx, xs, ldxs, width, dtype, stream))
+    status = (_lib or load()).ws_routing_dispatch(r, x, ldx, xs, ldxs, width, dtype, stream)
+    if status:
+        _check("ws_routing_dispatch", status)
 
 
 def ws_routing_dispatch_backward(r, gxs: int, ldgxs: int, gx: int, ldgx: int, width: int, dtype: int,
                                  stream: int) -> None:
-    _check("ws_routing_dispatch_backward", load().ws_routing_dispatch_backward(r, gxs, ldgxs, gx, ldgx, width, dtype,
-                                                                               stream))
+    status = (_lib or load()).ws_routing_dispatch_backward(r, gxs, ldgxs, gx, ldgx, width, dtype, stream)
+    if status:
+        _check("ws_routing_dispatch_backward", status)
 
 
 def ws_routing_combine(r, ys: int, ldys: int, y: int, ldy: int, width: int, dtype: int, stream: int) -> None:
-    _check("ws_routing_combine", load().ws_routing_combine(r, ys, ldys, y, ldy, width, dtype, stream))
+    status = (_lib or load()).ws_routing_combine(r, ys, ldys, y, ldy, width, dtype, stream)
+    if status:
+        _check("ws_routing_combine", status)
 
 
 def ws_routing_combine_backward(r, gy: int, ldgy: int, ys: int, ldys: int, gys: int, ldgys: int, gvals: int,
                                 width: int, dtype: int, stream: int) -> None:
-    _check("ws_routing_combine_backward", load().ws_routing_combine_backward(r, gy, ldgy, ys, ldys, gys, ldgys, gvals,
-                                                                             width, dtype, stream))
+    status = (_lib or load()).ws_routing_combine_backward(
+        r, gy, ldgy, ys, ldys, gys, ldgys, gvals, width, dtype, stream)
+    if status:
+        _check("ws_routing_combine_backward", status)
 
 
 def ws_routing_matmul(r, xs: int, ldxs: int, W: int, ldw: int, stride: int, N: int, K: int, ys: int, ldys: int,
                       dtype: int, scratch: int, scratch_bytes: int, stream: int) -> None:
-    _check("ws_routing_matmul", load().ws_routing_matmul(r, xs, ldxs, W, ldw, stride, N, K, ys, ldys, dtype, scratch,
-                                                         scratch_bytes, stream))
+    status = (_lib or load()).ws_routing_matmul(
+        r, xs, ldxs, W, ldw, stride, N, K, ys, ldys, dtype, scratch, scratch_bytes, stream)
+    if status:
+        _check("ws_routing_matmul", status)
 
 
 def ws_routing_matmul_backward(r, gys: int, ldgys: int, xs: int, ldxs: int, W: int, ldw: int, stride: int, N: int,
                                K: int, gxs: int, ldgxs: int, gW: int, ldgw: int, gstride: int, dtype: int,
                                scratch: int, scratch_bytes: int, stream: int) -> None:
-    _check("ws_routing_matmul_backward", load().ws_routing_matmul_backward(
+    status = (_lib or load()).ws_routing_matmul_backward(
         r, gys, ldgys, xs, ldxs, W, ldw, stride, N, K, gxs, ldgxs, gW, ldgw, gstride, dtype, scratch, scratch_bytes,
-        stream))
+        stream)
+    if status:
+        _check("ws_routing_matmul_backward", status)
 
 
 def ws_adapters_scratch(nnz: int, r: int) -> int:
@@ -293,4 +309,6 @@ def ws_adapters_scratch(nnz: int, r: int) -> int:
 
 def ws_adapters(call: bytes, scratch: int, scratch_bytes: int, stream: int) -> None:
     """``call``: the fields of struct ws_adapters_call packed by ADAPTERS_CALL."""
-    _check("ws_adapters", load().ws_adapters(call, scratch, scratch_bytes, stream))
+    status = (_lib or load()).ws_adapters(call, scratch, scratch_bytes, stream)
+    if status:
+        _check("ws_adapters", status)

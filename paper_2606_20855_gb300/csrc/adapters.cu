@@ -125,6 +125,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   const int k0 = static_cast<int>(static_cast<int64_t>(all) * blockIdx.y / gridDim.y);
   const int k1 = static_cast<int>(static_cast<int64_t>(all) * (blockIdx.y + 1) / gridDim.y);
   h += static_cast<int64_t>(blockIdx.y) * c.nnz * rpad;
+  may_start_next();
   if (threadIdx.x == 0) {
     for (int i = 0; i < kShrinkStages; ++i) {
       bar_init(smem_u32(&full_bar[i]), 1);
@@ -300,7 +301,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int dead;
   __shared__ int mins[kExpandThreads / 32];
-  const int warp = threadIdx.x >> 5, m = threadIdx.x & (kTok - 1), side = threadIdx.x / kTok;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = threadIdx.x & (kTok - 1), side = threadIdx.x / kTok;
   const uint32_t sa = (smem_u32(raw) + 1023u) & ~1023u, sy = sa + kExpandA, sb = sy + 4 * kExpandY;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTok, t = t0 + m;
   const int N = static_cast<int>(c.N);
@@ -327,6 +328,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   const uint32_t tmem = tmem_slot;
   const uint32_t idesc = instr_desc(half, false, false, kTok, kExpandN);
 
+  wait_for_last();  // the inner products
   int done = 0;        // products of 32 ranks
   bool mixed = false;  // some token does not have some adapter of the tile
   for (;;) {
@@ -383,9 +385,14 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   const int64_t rows = min(static_cast<int64_t>(kTok), c.nrows - t0);
   if (!copies && c.base) {
     const uint16_t* src = static_cast<const uint16_t*>(c.base) + t0 * c.ldbase + n0;
-    for (int row = warp; row < rows; row += kExpandThreads / 32)
-      for (int col = threadIdx.x & 31; col < columns; col += 32)
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(place(row, col)), "h"(src[row * c.ldbase + col]) : "memory");
+    for (int row = warp; row < rows; row += kExpandThreads / 32) {
+      uint16_t v[kExpandN / 32];
+#pragma unroll
+      for (int i = 0; i < kExpandN / 32; ++i) v[i] = 32 * i + lane < columns ? src[row * c.ldbase + 32 * i + lane] : 0;
+#pragma unroll
+      for (int i = 0; i < kExpandN / 32; ++i)
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(place(row, 32 * i + lane)), "h"(v[i]) : "memory");
+    }
   }
   if (done > 0) bar_wait(smem_u32(&m_bar), (done - 1) & 1, &dead);
   if (copies && c.base) bar_wait(smem_u32(&base_bar), 0, &dead);
@@ -432,12 +439,15 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   }
   if (!copies && !dead) {
     uint16_t* dst = static_cast<uint16_t*>(c.y) + t0 * c.ldy + n0;
-    for (int row = warp; row < rows; row += kExpandThreads / 32)
-      for (int col = threadIdx.x & 31; col < columns; col += 32) {
-        uint16_t v;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(place(row, col)) : "memory");
-        dst[row * c.ldy + col] = v;
-      }
+    for (int row = warp; row < rows; row += kExpandThreads / 32) {
+      uint16_t v[kExpandN / 32];
+#pragma unroll
+      for (int i = 0; i < kExpandN / 32; ++i)
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v[i]) : "r"(place(row, 32 * i + lane)) : "memory");
+#pragma unroll
+      for (int i = 0; i < kExpandN / 32; ++i)
+        if (32 * i + lane < columns) dst[row * c.ldy + 32 * i + lane] = v[i];
+    }
   }
   __syncwarp();
   __syncthreads();
@@ -586,8 +596,10 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
   const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
                                              static_cast<int>(kExpandSmem));
   if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
-  kernel<<<dim3(tiles, static_cast<unsigned>((c.N + kExpandN - 1) / kExpandN)), kExpandThreads, kExpandSmem, s>>>(
-      b, base, y, c, h, rpad, split, copies, status);
+  const dim3 grid(tiles, static_cast<unsigned>((c.N + kExpandN - 1) / kExpandN));
+  const cudaError_t launched = launch_early(kernel, grid, kExpandThreads, kExpandSmem, s, b, base, y, c,
+                                            static_cast<const float*>(h), rpad, split, copies, status);
+  if (launched != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(launched));
   return WS_OK;
 }
 

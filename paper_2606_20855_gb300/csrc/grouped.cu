@@ -49,7 +49,7 @@ struct GroupedParams {
   int64_t ldo;   // values between rows of the result
   int64_t group_stride;  // kRowsSum: values between gW[e]
   bool half;
-  bool vec;      // rows of the result start at multiples of 16 bytes
+  int vec;       // rows of the result start at multiples of so many bytes: 16, 8, 4 or 2
   int* status;
 };
 
@@ -145,38 +145,45 @@ __device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t tu
                  : "memory");
   }
   __syncwarp();
-  if (p.vec) {
+  // B bytes a lane: 16, 8, 4 or 2, as the rows of the result start
+  const auto along = [&](auto bytes) {
+    constexpr int B = decltype(bytes)::value, kValues = B / 2, kLanes = B == 2 ? 32 : 128 / B, kRowsAtOnce = 32 / kLanes;
+    constexpr int kSides = 64 / (kLanes * kValues);  // 2 where a lane moves 2 bytes, else 1
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int row = 4 * i + (lane >> 3), j = lane & 7;
-      uint32_t w[4];
-      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                   : "r"(turn + row * 128 + ((j ^ (row & 7)) << 4))
-                   : "memory");
-      if (!on(row)) continue;
-      uint16_t* to = dst + row * p.ldo + 8 * j;
-      if (8 * j + 8 <= left) {
-        *reinterpret_cast<uint4*>(to) = make_uint4(w[0], w[1], w[2], w[3]);
-      } else {
+    for (int i = 0; i < 32 / kRowsAtOnce; ++i) {
+      const int row = i * kRowsAtOnce + lane / kLanes;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (8 * j + e < left) to[e] = static_cast<uint16_t>(w[e >> 1] >> (16 * (e & 1)));
+      for (int side = 0; side < kSides; ++side) {
+        const int col = kValues * (lane % kLanes) + 32 * side;
+        Pack<uint16_t, kValues> v;
+        const uint32_t at = turn + row * 128 + (((col >> 3) ^ (row & 7)) << 4) + 2 * (col & 7);
+        if constexpr (B == 16) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+        } else if constexpr (B == 8) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+          asm volatile("ld.shared.v2.b32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+        } else if constexpr (B == 4) {
+          asm volatile("ld.shared.b32 %0, [%1];" : "=r"(*reinterpret_cast<uint32_t*>(&v)) : "r"(at) : "memory");
+        } else {
+          asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v.v[0]) : "r"(at) : "memory");
+        }
+        if (!on(row)) continue;
+        uint16_t* to = dst + row * p.ldo + col;
+        if (col + kValues <= left) {
+          *reinterpret_cast<Pack<uint16_t, kValues>*>(to) = v;
+        } else {
+#pragma unroll
+          for (int e = 0; e < kValues; ++e)
+            if (col + e < left) to[e] = v.v[e];
+        }
       }
     }
-  } else {
-#pragma unroll 4
-    for (int row = 0; row < 32; ++row) {
-      if (!on(row)) continue;
-#pragma unroll
-      for (int side = 0; side < 2; ++side) {
-        const int col = 32 * side + lane;
-        uint16_t v;
-        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(turn + row * 128 + (((col >> 3) ^ (row & 7)) << 4) + 2 * (col & 7)) : "memory");
-        if (col < left) dst[row * p.ldo + col] = v;
-      }
-    }
-  }
+  };
+  if (p.vec == 16) along(std::integral_constant<int, 16>());
+  else if (p.vec == 8) along(std::integral_constant<int, 8>());
+  else if (p.vec == 4) along(std::integral_constant<int, 4>());
+  else along(std::integral_constant<int, 2>());
   __syncwarp();
 }
 
@@ -508,6 +515,8 @@ cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const GroupedPara
 
 int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
 
+int row_alignment(uint64_t bits) { return bits % 16 == 0 ? 16 : bits % 8 == 0 ? 8 : bits % 4 == 0 ? 4 : 2; }
+
 template <bool kWMN>
 cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool* encoded) {
   const int64_t features = kWMN ? g.K : g.N, depth = kWMN ? g.N : g.K;
@@ -520,7 +529,7 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
   p.out = g.out;
   p.ldo = g.ldo;
   p.half = g.half;
-  p.vec = reinterpret_cast<uintptr_t>(g.out) % 16 == 0 && g.ldo % 8 == 0;
+  p.vec = row_alignment(reinterpret_cast<uintptr_t>(g.out) | static_cast<uint64_t>(g.ldo * 2));
   p.status = g.r->status;
   CUtensorMap x, w;
   const int64_t met = g.r->nnz < g.r->ncols ? g.r->nnz : g.r->ncols;  // groups that can have rows
@@ -537,9 +546,12 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
   };
   using std::integral_constant;
   // Few rows an expert: W's features fill the 128 lanes and the rows are the short side.
-  if (mean <= 12) {
-    if constexpr (kWMN) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>());
-    else return launch_thin(g, s);
+  // Forward: pieces of 16 rows and 32 features also where they all are at work at once (24 rows of three experts, K = 1520, N =
+  // 304: 14 us in tiles of 128 features, 8 us so).
+  if constexpr (kWMN) {
+    if (mean <= 12) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>());
+  } else {
+    if (mean <= 12 || (g.r->nnz / kThinRows + met) * up(features, kThinFeatures) <= 2 * num_sms) return launch_thin(g, s);
   }
   if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>());
   // A tile of 128 features takes two thirds of the time of one of 256 (bound by its operands' way from L2), so the wider one is
@@ -572,7 +584,7 @@ ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_
   p.ldo = g.ldo;
   p.group_stride = g.group_stride;
   p.half = g.half;
-  p.vec = reinterpret_cast<uintptr_t>(g.out) % 16 == 0 && g.ldo % 8 == 0 && g.group_stride % 8 == 0;
+  p.vec = row_alignment(reinterpret_cast<uintptr_t>(g.out) | static_cast<uint64_t>(g.ldo * 2) | static_cast<uint64_t>(g.group_stride * 2));
   p.status = g.r->status;
   CUtensorMap a, b;
   if (!encode(&a, gys, g.half, g.N, g.r->nnz, ldgys, 0, 0, 64) || !encode(&b, g.x, g.half, g.K, g.r->nnz, g.ldx, 0, 0, 64))

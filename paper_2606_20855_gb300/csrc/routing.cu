@@ -179,6 +179,7 @@ __global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, 
   extern __shared__ __align__(16) int sm[];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
   int* cnt = sm + kBuildWarps * cols;
+  may_start_next();
   for (int e = threadIdx.x; e < cols; e += blockDim.x) cnt[e] = 0;
   const int64_t begin = chunk * blockIdx.x, end = min(begin + chunk, r.nrows);
   for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
@@ -201,7 +202,7 @@ __global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, 
 }
 
 // Every CTA adds up the counts of all chunks by itself (a few hundred KB from L2, the threads split over the chunks):
-// a launch less than a scan of its own.
+// a launch less than a scan of its own.  It marks its first tile while the counting launch still runs.
 __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, int cols, int64_t chunk,
                                                                   const int32_t* counts) {
   extern __shared__ __align__(16) int sm[];
@@ -210,8 +211,14 @@ __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, 
   int* next = sm + kBuildWarps * cols;  // first slot of the tile in every column
   int* before = next + cols;            // entries of the chunks before this one
   uint16_t* pre = reinterpret_cast<uint16_t*>(before + cols);
+  const int64_t begin = chunk * blockIdx.x, end = min(begin + chunk, r.nrows);
+  WarpRows w;
+  w.start(r, begin + (threadIdx.x & ~31u));
+  clear_words(mask, kBuildWarps * cols);
   for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = before[e] = 0;
   __syncthreads();
+  mark_rows(r, w, cols, mask);
+  wait_for_last();
   const int quads = (cols + 3) / 4, groups = kTileRows / quads;  // at most 256 quads: a thread each
   const int g = static_cast<int>(threadIdx.x) / quads, v = static_cast<int>(threadIdx.x) - g * quads;
   if (g < groups) {
@@ -235,10 +242,15 @@ __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, 
   const int placed = scan_columns(cols, next, scratch);
   if (blockIdx.x == 0) write_offsets(r, cols, next, placed);
   __syncthreads();
-  for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
-  const int64_t begin = chunk * blockIdx.x, end = min(begin + chunk, r.nrows);
-  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
-    WarpRows w;
+  for (int e = threadIdx.x; e < cols; e += blockDim.x) {
+    next[e] += before[e];
+    before[e] = count_column(mask, pre, cols, e, kBuildWarps);
+  }
+  __syncthreads();
+  place_rows(r, w, cols, mask, pre, next);
+  for (int64_t row0 = begin + kTileRows; row0 < end; row0 += kTileRows) {
+    __syncthreads();
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
     w.start(r, row0 + (threadIdx.x & ~31u));
     clear_words(mask, kBuildWarps * cols);
     __syncthreads();
@@ -247,8 +259,6 @@ __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, 
     for (int e = threadIdx.x; e < cols; e += blockDim.x) before[e] = count_column(mask, pre, cols, e, kBuildWarps);
     __syncthreads();
     place_rows(r, w, cols, mask, pre, next);
-    __syncthreads();
-    for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
   }
 }
 
@@ -516,7 +526,7 @@ void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cud
   allow(reinterpret_cast<const void*>(routing_count_kernel), smem);
   allow(reinterpret_cast<const void*>(routing_place_kernel), smem);
   routing_count_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
-  routing_place_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
+  launch_early(routing_place_kernel, dim3(static_cast<unsigned>(chunks)), kTileRows, smem, s, r, cols, chunk, counts);
 }
 
 void launch_align(const AlignedCopies& c, cudaStream_t s) {

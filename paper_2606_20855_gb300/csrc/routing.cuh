@@ -106,6 +106,25 @@ __device__ __forceinline__ uint4 load8(const uint16_t* row, int k, int K, bool v
     if (k + i < K) w[i >> 1] |= static_cast<uint32_t>(row[k + i]) << (16 * (i & 1));
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
+// A kernel that may start while the one before it on the stream still runs (as soon as all of that one's CTAs have called
+// may_start_next, or are done) and calls wait_for_last before it touches what that one writes or reads.
+template <typename... P, typename... A>
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, A... args) {
+  cudaLaunchAttribute early{};
+  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  early.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t config{};
+  config.gridDim = grid;
+  config.blockDim = dim3(threads);
+  config.dynamicSmemBytes = smem;
+  config.stream = s;
+  config.attrs = &early;
+  config.numAttrs = 1;
+  return cudaLaunchKernelEx(&config, kernel, static_cast<P>(args)...);
+}
+__device__ __forceinline__ void may_start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_last() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // Launchers.  They queue kernels on s and leave errors to cudaGetLastError.
 void launch_topk_route(const void* logits, int64_t rows, int cols, int64_t ld, ws_dtype_t dt, int k, bool normalize,
                        int64_t* rowptr, int32_t* colidx, float* vals, cudaStream_t s);
