@@ -392,17 +392,19 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---------------------------------------------------------------- few rows an expert, forward
 //
-// Bound by W, each met expert's once.  A CTA takes 32 features and up to 16 rows of an expert; its eight warps split K and
-// read W straight into the operands of the warp-level matrix instruction (16 features x 8 rows), 16 bytes a load, four steps
-// in flight; the warps' sums meet in shared memory.  Against a tile of 128 features on the tcgen05 path the GPU gets four
-// times as many pieces of work: six rows of four experts each, N = 1024, K = 2048, bfloat16: 31 us there.
+// Bound by W, each met expert's once.  A CTA takes 32 features and up to eight rows of an expert; its eight warps split K and
+// read W straight into the operands of the warp-level matrix instruction (16 features x 8 rows), 16 bytes a load, two steps
+// in flight, three CTAs on an SM; the warps' sums meet in shared memory.  Six rows of four experts each of 64, N = 1024, K =
+// 2048, bfloat16 (84 MB of W, 12.4 us at the copy rate): 18 us; in tiles of 128 features on the tcgen05 path 31 us
+// (a fourth of the pieces of work); with four steps and two CTAs 18-19 us, two and four 22 us, three and three 25 us; with the
+// loads as asynchronous copies to shared memory 29 us.
 
 constexpr int kThinThreads = 256;
 constexpr int kThinWarps = kThinThreads / 32;
-constexpr int kThinRows = 16, kThinFeatures = 32;
+constexpr int kThinRows = 8, kThinFeatures = 32;
 
 template <bool half>
-__global__ void __launch_bounds__(kThinThreads, 2)
+__global__ void __launch_bounds__(kThinThreads, 3)
     thin_kernel(const int64_t* __restrict__ offsets, int groups, const uint16_t* __restrict__ x, int64_t ldx,
                 const uint16_t* __restrict__ W, int64_t ldw, int64_t group_stride, uint16_t* __restrict__ y, int64_t ldy,
                 int N, int K) {
@@ -432,51 +434,41 @@ __global__ void __launch_bounds__(kThinThreads, 2)
   if (e < 0) return;
   const int f0 = blockIdx.x * kThinFeatures;
   const uint16_t* wrow[4];
-  const uint16_t* xrow[2];
 #pragma unroll
   for (int i = 0; i < 4; ++i) wrow[i] = W + e * group_stride + min(f0 + 8 * i + g, N - 1) * ldw;
+  const uint16_t* xrow = x + (static_cast<int64_t>(row0) + min(g, rows - 1)) * ldx;
+  float acc[2][4] = {};
+  const auto step = [&](const uint4(&wv)[4], const uint4& xv) {
 #pragma unroll
-  for (int i = 0; i < 2; ++i) xrow[i] = x + (static_cast<int64_t>(row0) + min(8 * i + g, rows - 1)) * ldx;
-  const bool both = rows > 8;
-  float acc[2][2][4] = {};
-  const auto step = [&](const uint4(&wv)[4], const uint4(&xv)[2]) {
-#pragma unroll
-    for (int m = 0; m < 2; ++m)
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        mma16<half>(acc[m][j], wv[2 * m].x, wv[2 * m + 1].x, wv[2 * m].y, wv[2 * m + 1].y, xv[j].x, xv[j].y);
-        mma16<half>(acc[m][j], wv[2 * m].z, wv[2 * m + 1].z, wv[2 * m].w, wv[2 * m + 1].w, xv[j].z, xv[j].w);
-      }
+    for (int m = 0; m < 2; ++m) {
+      mma16<half>(acc[m], wv[2 * m].x, wv[2 * m + 1].x, wv[2 * m].y, wv[2 * m + 1].y, xv.x, xv.y);
+      mma16<half>(acc[m], wv[2 * m].z, wv[2 * m + 1].z, wv[2 * m].w, wv[2 * m + 1].w, xv.z, xv.w);
+    }
   };
-  constexpr int kStep = 32 * kThinWarps, U = 4;
+  constexpr int kStep = 32 * kThinWarps, U = 2;  // U steps whose loads are in flight together
   int k = 32 * warp + 8 * q;
   for (; k - 8 * q + kStep * (U - 1) + 32 <= K; k += kStep * U) {
-    uint4 wv[U][4], xv[U][2];
+    uint4 wv[U][4], xv[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) wv[u][i] = *reinterpret_cast<const uint4*>(wrow[i] + k + kStep * u);
-      xv[u][0] = *reinterpret_cast<const uint4*>(xrow[0] + k + kStep * u);
-      xv[u][1] = both ? *reinterpret_cast<const uint4*>(xrow[1] + k + kStep * u) : make_uint4(0, 0, 0, 0);
+      xv[u] = *reinterpret_cast<const uint4*>(xrow + k + kStep * u);
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) step(wv[u], xv[u]);
   }
 #pragma unroll 1
   for (; k - 8 * q < K; k += kStep) {
-    uint4 wv[4], xv[2];
+    uint4 wv[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) wv[i] = load8(wrow[i], k, K);
-#pragma unroll
-    for (int i = 0; i < 2; ++i) xv[i] = load8(xrow[i], k, K);
-    step(wv, xv);
+    step(wv, load8(xrow, k, K));
   }
 #pragma unroll
   for (int m = 0; m < 2; ++m)
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) red[warp][16 * m + 8 * (i >> 1) + g][8 * j + 2 * q + (i & 1)] = acc[m][j][i];
+    for (int i = 0; i < 4; ++i) red[warp][16 * m + 8 * (i >> 1) + g][2 * q + (i & 1)] = acc[m][i];
   __syncthreads();
   for (int i = threadIdx.x; i < kThinFeatures * rows; i += kThinThreads) {
     const int f = i % kThinFeatures, row = i / kThinFeatures;
