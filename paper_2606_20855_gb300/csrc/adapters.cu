@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int dead;
   __shared__ int list[kList], mins[kShrinkThreads / 32];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTok;
   const int r0 = blockIdx.z * kRankBlock, n = min(kRankBlock, rpad - r0);  // of one adapter
@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
   int stage = 0, acc = 0;
   uint32_t phase = 0, acc_phase = 0;
   int filled = 0;
-  bool ok = true;
+  bool ok = true, ready = false;  // ready: the role's next stage is known to be empty, or full
   for (;;) {
     int items = 0;
     while (items < kList) {
@@ -168,34 +168,41 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
     __syncthreads();
     if (items == 0) break;
     if (warp == 0) {
-      if (lane == 0) {
+      if (elect_one()) {
         for (int i = 0; ok && i < items; i += group) {
           const int these = min(group, items - i);
           for (int k = k0; k < k1; ++k) {
-            if (!bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead)) {
+            if (!ready && !bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead)) {
               ok = false;
               break;
             }
+            const int next = stage + 1 == kShrinkStages ? 0 : stage + 1;
+            const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
+            ready = bar_try(smem_u32(&empty_bar[next]), next_phase ^ 1);
             const uint32_t bar = smem_u32(&full_bar[stage]), at = base + stage * kShrinkStage;
             const int rows = min(kRankBlock, rpad);  // of the copy; past r they are zero
             bar_expect(bar, kTok * 128 + these * rows * 128);
             tma_2d(at, &map_x, 64 * k, static_cast<int>(t0), bar);
             for (int j = 0; j < these; ++j) tma_3d(at + kTok * 128 + j * rows * 128, &map_a, 64 * k, r0, list[i + j], bar);
             ++filled;
-            if (++stage == kShrinkStages) stage = 0, phase ^= 1;
+            stage = next;
+            phase = next_phase;
           }
         }
       }
     } else if (warp == 1) {
-      if (lane == 0) {
+      if (elect_one()) {
         for (int i = 0; ok && i < items; i += group) {
           const uint32_t idesc = instr_desc(c.dtype == WS_F16, false, false, kTok, n * min(group, items - i));
           ok = bar_wait(smem_u32(&acc_empty[acc]), acc_phase ^ 1, &dead);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           for (int k = k0; ok && k < k1; ++k) {
-            ok = bar_wait(smem_u32(&full_bar[stage]), phase, &dead);
+            ok = ready || bar_wait(smem_u32(&full_bar[stage]), phase, &dead);
             if (!ok) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const int next = stage + 1 == kShrinkStages ? 0 : stage + 1;
+            const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
+            ready = bar_try(smem_u32(&full_bar[next]), next_phase);
             const uint32_t at = base + stage * kShrinkStage;
             const uint64_t da = smem_desc(at, false), db = smem_desc(at + kTok * 128, false);
 #pragma unroll
@@ -203,7 +210,8 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
               mma_f16(tmem + acc * kRankBlock, da + j * (32 >> 4), db + j * (32 >> 4), idesc, k > k0 || j > 0);
             mma_commit(smem_u32(&empty_bar[stage]));
             if (k == k1 - 1) mma_commit(smem_u32(&acc_full[acc]));
-            if (++stage == kShrinkStages) stage = 0, phase ^= 1;
+            stage = next;
+            phase = next_phase;
           }
           if (++acc == 2) acc = 0, acc_phase ^= 1;
         }
@@ -212,8 +220,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
       for (int i = 0; ok && i < items; ++i) {
         const int at = i % group;
         if (at == 0) {
-          const bool got = lane != 0 || bar_wait(smem_u32(&acc_full[acc]), acc_phase, &dead);
-          ok = __shfl_sync(0xffffffffu, got, 0);
+          ok = bar_wait_warp(smem_u32(&acc_full[acc]), acc_phase, &dead);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         }

@@ -29,9 +29,9 @@ namespace {
 
 constexpr int kTileM = 128;   // rows of the M side: lanes of tensor memory
 constexpr int kTileK = 64;    // 128 bytes: the swizzle's span
-constexpr int kThreads = 192; // TMA warp, MMA warp, 4 epilogue warps
 constexpr int kBytesA = kTileM * kTileK * 2;
 constexpr int kTurnBytes = 32 * 128;
+constexpr double kPairRows = 512;  // rows an expert from which on its row tiles go in pairs
 
 // Where the rows of the experts are in the product D (M x N tile).
 constexpr int kRowsM = 0;    // on the M side (lanes)
@@ -66,30 +66,36 @@ struct Tile {
   int steps;     // stages of the contraction
 };
 
+// A warp that copies, one that multiplies, four that store; where rows are summed over, one that clears.
+template <int kRows>
+constexpr int kThreadsOf = kRows == kRowsSum ? 224 : 192;
+
 // Rows of a group in a tile, unless they are summed over.
 template <int BN, int kRows>
 constexpr int kRowTileOf = kRows == kRowsM ? kTileM : BN;
 
-template <int BN, int kRows>
+template <int BN, int kRows, bool kPair = false>
 struct Shape {
-  static constexpr int kBytesB = BN * kTileK * 2;
+  static constexpr int kBytesB = (kPair ? BN / 2 : BN) * kTileK * 2;
   static constexpr int kStageBytes = kBytesA + kBytesB;
   static constexpr int kStages = (196 * 1024) / kStageBytes > 10 ? 10 : (196 * 1024) / kStageBytes;
   static constexpr int kAccCols = 2 * BN < 32 ? 32 : 2 * BN;  // a power of two
   static constexpr size_t kSmem = static_cast<size_t>(kStages) * kStageBytes + (kRows == kRowsN ? 0 : 4 * kTurnBytes) + 1024;
 };
 
-// Tile t of the sequence that all roles of all CTAs share.  first[e]: row tiles of the groups before e.
-template <int BN, int kRows>
-__device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first, int64_t t, Tile* out) {
+// Tile t of the sequence that all roles of all CTAs share.  first[e]: row tiles of the groups before e.  kPair: t is two
+// tiles one below the other, of which `rank` is the CTA's.
+template <int BN, int kRows, bool kPair>
+__device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first, int64_t t, int rank, Tile* out) {
+  constexpr int kSpan = kPair ? 2 * kTileM : kTileM;
   if constexpr (kRows == kRowsSum) {
-    const int mt = (p.features + kTileM - 1) / kTileM, nt = (p.width + BN - 1) / BN;
+    const int mt = (p.features + kSpan - 1) / kSpan, nt = (p.width + BN - 1) / BN;
     const int64_t each = static_cast<int64_t>(mt) * nt;
     if (t >= each * p.groups) return false;
     const int e = static_cast<int>(t / each);
     const int i = static_cast<int>(t - each * e);
     out->group = e;
-    out->m0 = i % mt * kTileM;
+    out->m0 = i % mt * kSpan + rank * kTileM;
     out->n0 = i / mt * BN;
     const int64_t b = p.offsets[e], n = p.offsets[e + 1] - b;
     out->row0 = static_cast<int>(b);
@@ -97,7 +103,7 @@ __device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first
     out->steps = static_cast<int>((n + kTileK - 1) / kTileK);
   } else {
     constexpr int kFeat = kRows == kRowsM ? BN : kTileM;
-    constexpr int kRowTile = kRowTileOf<BN, kRows>;
+    constexpr int kRowTile = kPair ? kSpan : kRowTileOf<BN, kRows>;
     const int ft = (p.features + kFeat - 1) / kFeat;
     const int64_t q = t / ft;
     if (q >= first[p.groups]) return false;
@@ -116,8 +122,8 @@ __device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first
     const int r = 8 * band + in % high, f = in / high;
     out->group = e;
     const int64_t b = p.offsets[e];
-    out->row0 = static_cast<int>(b) + r * kRowTile;
-    out->rows = static_cast<int>(p.offsets[e + 1] - b) - r * kRowTile;
+    out->row0 = static_cast<int>(b) + r * kRowTile + rank * kTileM;
+    out->rows = static_cast<int>(p.offsets[e + 1] - b) - r * kRowTile - rank * kTileM;  // none or fewer: nothing is stored
     out->m0 = kRows == kRowsM ? 0 : f * kFeat;
     out->n0 = kRows == kRowsM ? f * kFeat : 0;
     out->steps = (p.depth + kTileK - 1) / kTileK;
@@ -189,41 +195,56 @@ __device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t tu
 
 // a: the M side's operand (kRowsM: the experts' rows, kRowsN: W, kRowsSum: gys), b: the N side's.
 // kWMN: W's contraction index runs along its rows (MN-major).
-template <int BN, int kRows, bool kWMN>
-__global__ void __launch_bounds__(kThreads, 1)
+// kPair: two CTAs, whose tiles lie one below the other, multiply as one (256 x 256): each holds its 128 rows of the M side and half of
+// the N side, so that a stage takes 32 KB of shared memory and of the way from L2 instead of 48, and six stages fit where four did.
+// Rank 0 issues the products and counts both CTAs' bytes at its barriers (rank 1 counting its own and telling rank 0 cost a microsecond a
+// stage).  8198 rows of eight experts, 2048 -> 8192: 206 us a call with pairs, 214 us without; 32768 rows of 32 experts, 2048 x 2048,
+// with gradients: 653 and 665 us.
+template <int BN, int kRows, bool kWMN, bool kPair>
+__global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const GroupedParams p) {
-  using S = Shape<BN, kRows>;
+  using S = Shape<BN, kRows, kPair>;
   constexpr bool kAMN = kRows == kRowsSum || (kRows == kRowsN && kWMN);
   constexpr bool kBMN = kRows == kRowsSum || (kRows == kRowsM && kWMN);
+  constexpr int kHalfN = kPair ? BN / 2 : BN;  // of the N side in this CTA
   extern __shared__ uint8_t raw[];
   __shared__ int first[kRouteMaxCols + 1];
   __shared__ int scratch[32];
   __shared__ __align__(8) uint64_t full_bar[S::kStages], empty_bar[S::kStages], acc_full[2], acc_empty[2], last_bar;
+  // stages with rows behind a group's last: have come, and are cleared
+  __shared__ __align__(8) uint64_t tail_bar[kRows == kRowsSum ? S::kStages : 1], clear_bar[kRows == kRowsSum ? S::kStages : 1];
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int dead;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31;
   const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+  const int rank = kPair ? blockIdx.x & 1 : 0;
+  const int64_t team = kPair ? blockIdx.x >> 1 : blockIdx.x, teams = kPair ? gridDim.x >> 1 : gridDim.x;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < S::kStages; ++i) {
       bar_init(smem_u32(&full_bar[i]), 1);
       bar_init(smem_u32(&empty_bar[i]), 1);
+      if constexpr (kRows == kRowsSum) {
+        bar_init(smem_u32(&tail_bar[i]), 1);
+        bar_init(smem_u32(&clear_bar[i]), kPair ? 2 : 1);
+      }
     }
     for (int i = 0; i < 2; ++i) {
       bar_init(smem_u32(&acc_full[i]), 1);
-      bar_init(smem_u32(&acc_empty[i]), 4);
+      bar_init(smem_u32(&acc_empty[i]), kPair ? 8 : 4);
     }
     bar_init(smem_u32(&last_bar), 1);
     dead = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
-  if (warp == 1) tmem_alloc<S::kAccCols>(smem_u32(&tmem_slot));
+  if (warp == 1) tmem_alloc<S::kAccCols, kPair>(smem_u32(&tmem_slot));
   if constexpr (kRows != kRowsSum) {  // row tiles before every group
     int sum = 0;
-    for (int e0 = 0; e0 < p.groups; e0 += kThreads) {
+    for (int e0 = 0; e0 < p.groups; e0 += kThreadsOf<kRows>) {
       const int e = e0 + threadIdx.x;
-      const int n = e < p.groups ? static_cast<int>((p.offsets[e + 1] - p.offsets[e] + kRowTileOf<BN, kRows> - 1) / kRowTileOf<BN, kRows>) : 0;
+      constexpr int kRowTile = kPair ? 2 * kTileM : kRowTileOf<BN, kRows>;
+      const int n = e < p.groups ? static_cast<int>((p.offsets[e + 1] - p.offsets[e] + kRowTile - 1) / kRowTile) : 0;
       int all = 0;
       const int before = block_exclusive_scan(n, scratch, &all);
       if (e < p.groups) first[e] = sum + before;
@@ -233,103 +254,158 @@ __global__ void __launch_bounds__(kThreads, 1)
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   __syncthreads();
+  if constexpr (kPair) pair_sync();  // the other CTA's barriers are there
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elect_one()) {
       int stage = 0;
       uint32_t phase = 0;
-      int64_t filled = 0;  // stages whose copies were started
-      bool ok = true;
+      bool ok = true, ready = false;  // ready: the stage is known to be empty
       Tile t;
-      for (int64_t i = blockIdx.x; ok && tile_at<BN, kRows>(p, first, i, &t); i += gridDim.x) {
+      for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
         for (int k = 0; k < t.steps; ++k) {
-          if (!bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead)) {
+          if (!ready && !bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead)) {
             ok = false;
             break;
           }
-          const uint32_t bar = smem_u32(&full_bar[stage]);
+          const int next = stage + 1 == S::kStages ? 0 : stage + 1;
+          const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
+          ready = bar_try(smem_u32(&empty_bar[next]), next_phase ^ 1);
           const uint32_t sa = base + stage * S::kStageBytes, sb = sa + kBytesA;
           const int at = k * kTileK;
-          bar_expect(bar, S::kStageBytes);
+          const bool tail = kRows == kRowsSum && t.rows - at < kTileK;
+          uint32_t bar = smem_u32(&full_bar[stage]);
+          if (tail) {  // counted apart, for the warp that clears
+            if (rank == 0) bar_arrive(bar);
+            bar = smem_u32(&tail_bar[kRows == kRowsSum ? stage : 0]);
+            bar_expect(bar, S::kStageBytes);
+          } else if (!kPair) {
+            bar_expect(bar, S::kStageBytes);
+          } else if (rank == 0) {
+            bar_expect(bar, 2 * S::kStageBytes);
+          } else {
+            bar = at_first(bar);
+          }
+          const auto copy2 = [&](uint32_t dst, const CUtensorMap* map, int x, int y) {
+            if (kPair && rank == 1 && !tail) tma_2d_first(dst, map, x, y, bar);
+            else tma_2d(dst, map, x, y, bar);
+          };
+          const auto copy3 = [&](uint32_t dst, const CUtensorMap* map, int x, int y, int z) {
+            if (kPair && rank == 1 && !tail) tma_3d_first(dst, map, x, y, z, bar);
+            else tma_3d(dst, map, x, y, z, bar);
+          };
           if constexpr (kRows == kRowsM) {
-            tma_2d(sa, &map_a, at, t.row0, bar);
+            copy2(sa, &map_a, at, t.row0);
             if constexpr (kBMN) {
 #pragma unroll
-              for (int j = 0; j < BN / 64; ++j) tma_3d(sb + j * 8192, &map_b, t.n0 + 64 * j, at, t.group, bar);
+              for (int j = 0; j < kHalfN / 64; ++j) copy3(sb + j * 8192, &map_b, t.n0 + rank * kHalfN + 64 * j, at, t.group);
             } else {
-              tma_3d(sb, &map_b, at, t.n0, t.group, bar);
+              copy3(sb, &map_b, at, t.n0 + rank * kHalfN, t.group);
             }
           } else if constexpr (kRows == kRowsN) {
             if constexpr (kAMN) {
 #pragma unroll
-              for (int j = 0; j < kTileM / 64; ++j) tma_3d(sa + j * 8192, &map_a, t.m0 + 64 * j, at, t.group, bar);
+              for (int j = 0; j < kTileM / 64; ++j) copy3(sa + j * 8192, &map_a, t.m0 + 64 * j, at, t.group);
             } else {
-              tma_3d(sa, &map_a, at, t.m0, t.group, bar);
+              copy3(sa, &map_a, at, t.m0, t.group);
             }
-            tma_2d(sb, &map_b, at, t.row0, bar);
+            copy2(sb, &map_b, at, t.row0);
           } else {
 #pragma unroll
-            for (int j = 0; j < kTileM / 64; ++j) tma_2d(sa + j * 8192, &map_a, t.m0 + 64 * j, t.row0 + at, bar);
+            for (int j = 0; j < kTileM / 64; ++j) copy2(sa + j * 8192, &map_a, t.m0 + 64 * j, t.row0 + at);
 #pragma unroll
-            for (int j = 0; j < BN / 64; ++j) tma_2d(sb + j * 8192, &map_b, t.n0 + 64 * j, t.row0 + at, bar);
+            for (int j = 0; j < kHalfN / 64; ++j) copy2(sb + j * 8192, &map_b, t.n0 + rank * kHalfN + 64 * j, t.row0 + at);
           }
-          ++filled;
-          if (++stage == S::kStages) stage = 0, phase ^= 1;
+          stage = next;
+          phase = next_phase;
         }
       }
-      if (!ok) {  // no copy may be in flight when the CTA leaves
-        const int64_t begin = filled > S::kStages ? filled - S::kStages : 0;
-        for (int64_t f = begin; f < filled; ++f) {
-          bar_wait_short(smem_u32(&full_bar[f % S::kStages]), static_cast<uint32_t>(f / S::kStages) & 1);
+      if constexpr (kPair)  // the other CTA's arrivals at this one's barriers are in
+        for (int i = 0; ok && i < S::kStages; ++i) {
+          ok = bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead);
+          if (++stage == S::kStages) stage = 0, phase ^= 1;
+        }
+      if (!ok) {  // no copy may be in flight when the CTA leaves: time enough for any
+        const unsigned long long start = now_ns();
+        while (now_ns() - start < kWaitLimitNs / 100) {
         }
       }
     }
   } else if (warp == 1) {
-    const uint32_t idesc = instr_desc(p.half, kAMN, kBMN, kTileM, BN);
-    int stage = 0, acc = 0;
-    uint32_t phase = 0, acc_phase = 0;
-    bool ok = true;
-    Tile t;
-    for (int64_t i = blockIdx.x; ok && tile_at<BN, kRows>(p, first, i, &t); i += gridDim.x) {
-      if (t.steps == 0) continue;
-      bool got = lane != 0 || bar_wait(smem_u32(&acc_empty[acc]), acc_phase ^ 1, &dead);
-      ok = __shfl_sync(0xffffffffu, got, 0);
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      for (int k = 0; ok && k < t.steps; ++k) {
-        got = lane != 0 || bar_wait(smem_u32(&full_bar[stage]), phase, &dead);
-        ok = __shfl_sync(0xffffffffu, got, 0);
-        if (!ok) break;
+    if (rank == 0 && elect_one()) {
+      const uint32_t idesc = instr_desc(p.half, kAMN, kBMN, kPair ? 2 * kTileM : kTileM, BN);
+      int stage = 0, acc = 0;
+      uint32_t phase = 0, acc_phase = 0;
+      uint32_t cleared = 0;  // bit i: how often, modulo two, rows of stage i were cleared
+      bool ok = true, ready = false;  // ready: the stage is known to be full
+      Tile t;
+      for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
+        if (t.steps == 0) continue;
+        ok = bar_wait<kPair>(smem_u32(&acc_empty[acc]), acc_phase ^ 1, &dead);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t sa = base + stage * S::kStageBytes, sb = sa + kBytesA;
-        if constexpr (kRows == kRowsSum) {
-          const int rows = t.rows - k * kTileK;
-          if (rows < kTileK) {  // the rows behind the group's last
-            for (int b = 0; b < S::kStageBytes / 8192; ++b)
-              for (int c = rows * 8 + lane; c < kTileK * 8; c += 32)
-                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(sa + b * 8192 + c * 16), "r"(0) : "memory");
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
+        for (int k = 0; ok && k < t.steps; ++k) {
+          const uint32_t sa = base + stage * S::kStageBytes, sb = sa + kBytesA;
+          const int next = stage + 1 == S::kStages ? 0 : stage + 1;
+          const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
+          if (kRows == kRowsSum && t.rows - k * kTileK < kTileK) {
+            ok = bar_wait<kPair>(smem_u32(&clear_bar[stage]), cleared >> stage & 1, &dead);
+            cleared ^= 1u << stage;
+          } else if (!ready) {
+            ok = bar_wait(smem_u32(&full_bar[stage]), phase, &dead);
           }
-        }
-        if (lane == 0) {
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          ready = bar_try(smem_u32(&full_bar[next]), next_phase);
           const uint64_t da = smem_desc(sa, kAMN), db = smem_desc(sb, kBMN);
 #pragma unroll
-          for (int j = 0; j < kTileK / 16; ++j)
-            mma_f16(tmem + acc * BN, da + j * (kAMN ? 2048 >> 4 : 32 >> 4), db + j * (kBMN ? 2048 >> 4 : 32 >> 4), idesc,
-                    k > 0 || j > 0);
-          mma_commit(smem_u32(&empty_bar[stage]));
-          if (k == t.steps - 1) mma_commit(smem_u32(&acc_full[acc]));
+          for (int j = 0; j < kTileK / 16; ++j) {
+            const uint64_t a = da + j * (kAMN ? 2048 >> 4 : 32 >> 4), b = db + j * (kBMN ? 2048 >> 4 : 32 >> 4);
+            if constexpr (kPair) mma_f16_pair(tmem + acc * BN, a, b, idesc, k > 0 || j > 0);
+            else mma_f16(tmem + acc * BN, a, b, idesc, k > 0 || j > 0);
+          }
+          if constexpr (kPair) mma_commit_pair(smem_u32(&empty_bar[stage]));
+          else mma_commit(smem_u32(&empty_bar[stage]));
+          if (k == t.steps - 1) {
+            if constexpr (kPair) mma_commit_pair(smem_u32(&acc_full[acc]));
+            else mma_commit(smem_u32(&acc_full[acc]));
+          }
+          stage = next;
+          phase = next_phase;
         }
-        __syncwarp();
-        if (++stage == S::kStages) stage = 0, phase ^= 1;
+        if (++acc == 2) acc = 0, acc_phase ^= 1;
       }
-      if (++acc == 2) acc = 0, acc_phase ^= 1;
+      if (!ok) {  // nor may a product be under way
+        if constexpr (kPair) mma_commit_pair(smem_u32(&last_bar));
+        else mma_commit(smem_u32(&last_bar));
+        bar_wait_short(smem_u32(&last_bar), 0);
+      }
     }
-    if (!ok && lane == 0) {  // nor may a product
-      mma_commit(smem_u32(&last_bar));
-      bar_wait_short(smem_u32(&last_bar), 0);
+  } else if (kRows == kRowsSum && warp == 6) {
+    // clears the rows behind a group's last in the stage that holds them
+    int64_t steps = 0;
+    uint32_t cleared = 0;
+    bool ok = true;
+    Tile t;
+    for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
+      steps += t.steps;
+      const int rows = t.rows - (t.steps - 1) * kTileK;
+      if (t.steps == 0 || rows == kTileK) continue;
+      const int stage = static_cast<int>((steps - 1) % S::kStages);
+      ok = bar_wait_warp(smem_u32(&tail_bar[stage]), cleared >> stage & 1, &dead);
+      if (!ok) break;
+      const uint32_t at = base + stage * S::kStageBytes;
+      for (int b = 0; b < S::kStageBytes / 8192; ++b)
+        for (int c = rows * 8 + lane; c < kTileK * 8; c += 32)
+          asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + b * 8192 + c * 16), "r"(0) : "memory");
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      __syncwarp();
+      if (elect_one()) {
+        if constexpr (kPair) bar_arrive_first(smem_u32(&clear_bar[stage]));
+        else bar_arrive(smem_u32(&clear_bar[stage]));
+      }
+      cleared ^= 1u << stage;
     }
   } else {
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
@@ -338,10 +414,9 @@ __global__ void __launch_bounds__(kThreads, 1)
     bool ok = true;
     Tile t;
     uint16_t* const result = static_cast<uint16_t*>(p.out);
-    for (int64_t i = blockIdx.x; ok && tile_at<BN, kRows>(p, first, i, &t); i += gridDim.x) {
+    for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
       if (t.steps > 0) {
-        const bool got = lane != 0 || bar_wait(smem_u32(&acc_full[acc]), acc_phase, &dead);
-        ok = __shfl_sync(0xffffffffu, got, 0);
+        ok = bar_wait_warp(smem_u32(&acc_full[acc]), acc_phase, &dead);
         if (!ok) break;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       }
@@ -379,15 +454,19 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (t.steps > 0) {
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
-        if (lane == 0) bar_arrive(smem_u32(&acc_empty[acc]));
+        if (lane == 0) {
+          if constexpr (kPair) bar_arrive_first(smem_u32(&acc_empty[acc]));
+          else bar_arrive(smem_u32(&acc_empty[acc]));
+        }
         if (++acc == 2) acc = 0, acc_phase ^= 1;
       }
     }
   }
   __syncwarp();
   __syncthreads();
+  if constexpr (kPair) pair_sync();  // nothing of the other CTA's is on its way here
   if (threadIdx.x == 0 && dead) atomicOr(p.status, 1);
-  if (warp == 1) tmem_free<S::kAccCols>(tmem);
+  if (warp == 1) tmem_free<S::kAccCols, kPair>(tmem);
 }
 
 // ---------------------------------------------------------------- few rows an expert, forward
@@ -493,16 +572,33 @@ cudaError_t launch_thin(const GroupedRows& g, cudaStream_t s) {
 
 // ---------------------------------------------------------------- host
 
-template <int BN, int kRows, bool kWMN>
+template <int BN, int kRows, bool kWMN, bool kPair = false>
 cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const GroupedParams& p, int64_t tiles, int num_sms,
                    cudaStream_t s) {
-  using S = Shape<BN, kRows>;
-  const auto kernel = grouped_kernel<BN, kRows, kWMN>;
+  using S = Shape<BN, kRows, kPair>;
+  const auto kernel = grouped_kernel<BN, kRows, kWMN, kPair>;
   const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel),
                                              cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(S::kSmem));
   if (e != cudaSuccess) return e;
-  kernel<<<static_cast<unsigned>(tiles < num_sms ? tiles : num_sms), kThreads, S::kSmem, s>>>(a, b, p);
-  return cudaGetLastError();
+  const int64_t teams = kPair ? num_sms / 2 : num_sms;
+  const unsigned grid = static_cast<unsigned>((tiles < teams ? tiles : teams) * (kPair ? 2 : 1));
+  if constexpr (kPair) {
+    cudaLaunchAttribute pair{};
+    pair.id = cudaLaunchAttributeClusterDimension;
+    pair.val.clusterDim.x = 2;
+    pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
+    cudaLaunchConfig_t config{};
+    config.gridDim = dim3(grid);
+    config.blockDim = dim3(kThreadsOf<kRows>);
+    config.dynamicSmemBytes = S::kSmem;
+    config.stream = s;
+    config.attrs = &pair;
+    config.numAttrs = 1;
+    return cudaLaunchKernelEx(&config, kernel, a, b, p);
+  } else {
+    kernel<<<grid, kThreadsOf<kRows>, S::kSmem, s>>>(a, b, p);
+    return cudaGetLastError();
+  }
 }
 
 int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
@@ -526,32 +622,37 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
   CUtensorMap x, w;
   const int64_t met = g.r->nnz < g.r->ncols ? g.r->nnz : g.r->ncols;  // groups that can have rows
   const double mean = static_cast<double>(g.r->nnz) / static_cast<double>(g.r->ncols);
-  const auto run = [&](auto bn, auto side) {
+  const auto run = [&](auto bn, auto side, auto pair) {
     constexpr int BN = decltype(bn)::value, kRows = decltype(side)::value;
+    constexpr bool kPair = decltype(pair)::value;
     constexpr int kRowTile = kRowTileOf<BN, kRows>;
     constexpr int kFeat = kRows == kRowsM ? BN : kTileM;
     *encoded = encode(&x, g.x, g.half, depth, g.r->nnz, g.ldx, 0, 0, kRowTile) &&
-               encode(&w, g.w, g.half, g.K, g.N, g.ldw, g.r->ncols, g.group_stride, kWMN ? 64 : kFeat);
+               encode(&w, g.w, g.half, g.K, g.N, g.ldw, g.r->ncols, g.group_stride, kWMN ? 64 : kPair ? kFeat / 2 : kFeat);
     if (!*encoded) return cudaSuccess;
-    const int64_t tiles = (g.r->nnz / kRowTile + met) * up(features, kFeat);
-    return launch<BN, kRows, kWMN>(kRows == kRowsM ? x : w, kRows == kRowsM ? w : x, p, tiles, num_sms, s);
+    const int64_t tiles = (g.r->nnz / (kPair ? 2 * kRowTile : kRowTile) + met) * up(features, kFeat);
+    return launch<BN, kRows, kWMN, kPair>(kRows == kRowsM ? x : w, kRows == kRowsM ? w : x, p, tiles, num_sms, s);
   };
   using std::integral_constant;
   // Few rows an expert: W's features fill the 128 lanes and the rows are the short side.
   // Forward: pieces of 16 rows and 32 features also where they all are at work at once (24 rows of three experts, K = 1520, N =
   // 304: 14 us in tiles of 128 features, 8 us so).
   if constexpr (kWMN) {
-    if (mean <= 12) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>());
+    if (mean <= 12) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>(), std::false_type());
   } else {
     if (mean <= 12 || (g.r->nnz / kThinRows + met) * up(features, kThinFeatures) <= 2 * num_sms) return launch_thin(g, s);
   }
-  if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>());
+  if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>(), std::false_type());
+  // Pairs of row tiles where experts have enough of them that an odd one left over costs less than pairs gain (two in a hundred at
+  // 1024 rows an expert; an odd tile is half a tile's time lost per expert, which at 512 rows is one in eight of half the experts).
+  if (mean >= kPairRows && (g.r->nnz / (2 * kTileM) + up(met, 2)) * up(features, 256) >= num_sms / 2)
+    return run(integral_constant<int, 256>(), integral_constant<int, kRowsM>(), std::true_type());
   // A tile of 128 features takes two thirds of the time of one of 256 (bound by its operands' way from L2), so the wider one is
   // taken unless the narrower fills the SMs' last turn so much better.
   const int64_t row_tiles = g.r->nnz / kTileM + up(met, 2);
   if (3 * up(row_tiles * up(features, 256), num_sms) <= 2 * up(row_tiles * up(features, 128), num_sms))
-    return run(integral_constant<int, 256>(), integral_constant<int, kRowsM>());
-  return run(integral_constant<int, 128>(), integral_constant<int, kRowsM>());
+    return run(integral_constant<int, 256>(), integral_constant<int, kRowsM>(), std::false_type());
+  return run(integral_constant<int, 128>(), integral_constant<int, kRowsM>(), std::false_type());
 }
 
 }  // namespace
@@ -582,7 +683,10 @@ ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_
   if (!encode(&a, gys, g.half, g.N, g.r->nnz, ldgys, 0, 0, 64) || !encode(&b, g.x, g.half, g.K, g.r->nnz, g.ldx, 0, 0, 64))
     return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
   const int64_t wide = g.r->ncols * up(g.N, kTileM) * up(g.K, 256);
-  const cudaError_t e = wide >= num_sms
+  const int64_t pairs = g.r->ncols * up(g.N, 2 * kTileM) * up(g.K, 256);
+  const cudaError_t e = pairs >= num_sms / 2 && up(g.N, kTileM) % 2 == 0
+                            ? launch<256, kRowsSum, false, true>(a, b, p, pairs, num_sms, s)
+                        : wide >= num_sms
                             ? launch<256, kRowsSum, false>(a, b, p, wide, num_sms, s)
                             : launch<128, kRowsSum, false>(a, b, p, g.r->ncols * up(g.N, kTileM) * up(g.K, 128), num_sms, s);
   return e == cudaSuccess ? WS_OK : routing_fail(WS_ERR_CUDA, "grouped product: %s", cudaGetErrorString(e));

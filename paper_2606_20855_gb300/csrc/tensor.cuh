@@ -13,6 +13,14 @@ namespace wsk {
 
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 
+// One lane of a warp, all of whose lanes are here: the compiler then knows that a single thread runs what follows, and does not
+// wrap each copy and matrix instruction in a loop over lanes.
+__device__ __forceinline__ bool elect_one() {
+  uint32_t on;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(on));
+  return on != 0;
+}
+
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 
 __device__ __forceinline__ void bar_init(uint32_t bar, int count) {
@@ -33,17 +41,32 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
       : "memory");
   return ok != 0;
 }
+// The same for arrivals from the other CTA of a pair.
+__device__ __forceinline__ bool bar_try_pair(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
 __device__ __forceinline__ unsigned long long now_ns() {
   unsigned long long t;
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
   return t;
 }
+// An answer of bar_try takes more than 200 cycles (measured), about half of what a stage's products take: the loops below ask for
+// the next stage before they work on this one, and wait only if the answer was no.
+//
 // Waits for a phase; gives up after kWaitLimitNs or when another role gave up (*dead).
+template <bool kPair = false>
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  if (bar_try(bar, parity)) return true;
+  const auto there = [&] { return kPair ? bar_try_pair(bar, parity) : bar_try(bar, parity); };
+  if (there()) return true;
   const unsigned long long start = now_ns();
   for (unsigned i = 1;; ++i) {
-    if (bar_try(bar, parity)) return true;
+    if (there()) return true;
     if ((i & 31) == 0) {
       if (*dead) return false;
       if (now_ns() - start > kWaitLimitNs) {
@@ -54,6 +77,11 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   }
 }
 
+// The same for a whole warp: one lane asks.
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, volatile int* dead) {
+  const bool got = (threadIdx.x & 31) != 0 || bar_wait(bar, parity, dead);
+  return __shfl_sync(0xffffffffu, got, 0);
+}
 // The same for what is waited for on the way out.
 __device__ __forceinline__ void bar_wait_short(uint32_t bar, uint32_t parity) {
   const unsigned long long start = now_ns();
@@ -62,14 +90,20 @@ __device__ __forceinline__ void bar_wait_short(uint32_t bar, uint32_t parity) {
 }
 
 // Columns of tensor memory, by a whole warp; the address is written to shared memory.
-template <int kCols>
+template <int kCols, bool kPair = false>
 __device__ __forceinline__ void tmem_alloc(uint32_t slot) {
-  asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(kCols) : "memory");
-  asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  if constexpr (kPair) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(kCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+  } else {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(kCols) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+  }
 }
-template <int kCols>
+template <int kCols, bool kPair = false>
 __device__ __forceinline__ void tmem_free(uint32_t tmem) {
-  asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+  if constexpr (kPair) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
+  else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kCols) : "memory");
 }
 
 __device__ __forceinline__ void tma_2d(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
@@ -84,6 +118,32 @@ __device__ __forceinline__ void tma_3d(uint32_t dst, const CUtensorMap* map, int
           dst),
       "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
       : "memory");
+}
+
+// Copies to this CTA whose bytes are counted at a barrier of the pair's CTA of rank 0.
+__device__ __forceinline__ void tma_2d_first(uint32_t dst, const CUtensorMap* map, int x, int y, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(
+          dst),
+      "l"(map), "r"(x), "r"(y), "r"(bar)
+      : "memory");
+}
+__device__ __forceinline__ void tma_3d_first(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::
+          "r"(dst),
+      "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
+}
+// Where the CTA of rank 0 has what lies at `at` here.
+__device__ __forceinline__ uint32_t at_first(uint32_t at) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(at));
+  return r;
+}
+// Both CTAs of a pair (a cluster of two) meet.
+__device__ __forceinline__ void pair_sync() {
+  asm volatile("barrier.cluster.arrive.aligned;\n barrier.cluster.wait.aligned;" ::: "memory");
 }
 
 __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t src, int x, int y) {
@@ -117,6 +177,25 @@ __device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint
 }
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+
+// A product of a pair: A's upper and lower 128 rows and the halves of B's columns lie in the two CTAs' shared memory at the same
+// places, each CTA's tensor memory receives its rows.  Issued by the CTA of rank 0.
+__device__ __forceinline__ void mma_f16_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+      "l"(a), "l"(b), "r"(idesc), "r"(static_cast<uint32_t>(accumulate))
+      : "memory");
+}
+// The arrival at the barriers of both.
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+               "h"(static_cast<uint16_t>(3))
+               : "memory");
+}
+// Arrival at the barrier of the pair's CTA of rank 0 that lies where `bar` does in this one.
+__device__ __forceinline__ void bar_arrive_first(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(at_first(bar)) : "memory");
 }
 
 // 16 consecutive 32-bit columns of the warp's 32 lanes.

@@ -81,6 +81,10 @@ def test_many_tiles_per_sm():
     Z = sum(counts)
     _check(_plan(counts), counts, _randn((Z, 712), torch.bfloat16, 1), _randn((6, 2056, 712), torch.bfloat16, 2, 0.3),
            _randn((Z, 2056), torch.bfloat16, 3))
+    counts = [700, 0, 1300, 5, 2000]  # tiles in pairs, in all three products
+    Z = sum(counts)
+    _check(_plan(counts), counts, _randn((Z, 2304), torch.float16, 1), _randn((5, 1280, 2304), torch.float16, 2, 0.3),
+           _randn((Z, 1280), torch.float16, 3))
     counts = [9] * 900
     _check(_plan(counts), counts, _randn((8100, 264), torch.float16, 1), _randn((900, 400, 264), torch.float16, 2, 0.3),
            _randn((8100, 400), torch.float16, 3))
