@@ -350,17 +350,28 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
         bar_expect(smem_u32(&b_bar), kExpandB);
         tma_3d(sb, &map_b, r0, n0, a, smem_u32(&b_bar));
       }
+      float4 part[kExpandRanks / 16][2][kMaxSplit];  // all of the thread's loads in flight at once
+#pragma unroll
+      for (int i = 0; i < kExpandRanks / 16; ++i)
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+#pragma unroll
+          for (int k = 0; k < kMaxSplit; ++k)
+            part[i][e][k] = mine && 16 * i < ranks && k < split
+                                ? *reinterpret_cast<const float4*>(h + (static_cast<int64_t>(k) * c.nnz + w.at) * rpad + r0 + 16 * i + 8 * side + 4 * e)
+                                : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
       for (int i = 0; i < kExpandRanks / 16; ++i) {
         const int j = 16 * i + 8 * side;
         if (j >= ranks) break;
-        uint32_t hi[4] = {}, lo[4] = {};
-        if (mine) {
-          const float4 f = scaled_h(c, h, rpad, split, w.at, r0 + j, v), g = scaled_h(c, h, rpad, split, w.at, r0 + j + 4, v);
-          const uint2 p[4] = {split_pair<half>(f.x, f.y), split_pair<half>(f.z, f.w), split_pair<half>(g.x, g.y),
-                              split_pair<half>(g.z, g.w)};
+        uint32_t hi[4], lo[4];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) hi[e] = p[e].x, lo[e] = p[e].y;
+        for (int e = 0; e < 2; ++e) {
+          float4 f = part[i][e][0];
+#pragma unroll
+          for (int k = 1; k < kMaxSplit; ++k) f.x += part[i][e][k].x, f.y += part[i][e][k].y, f.z += part[i][e][k].z, f.w += part[i][e][k].w;
+          const uint2 a01 = split_pair<half>(v * f.x, v * f.y), a23 = split_pair<half>(v * f.z, v * f.w);
+          hi[2 * e] = a01.x, lo[2 * e] = a01.y, hi[2 * e + 1] = a23.x, lo[2 * e + 1] = a23.y;
         }
         const uint32_t row = sa + m * 128;
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((j >> 3) ^ (m & 7)) << 4)), "r"(hi[0]),

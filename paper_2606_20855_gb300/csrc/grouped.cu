@@ -643,8 +643,9 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
     if (mean <= 12 || (g.r->nnz / kThinRows + met) * up(features, kThinFeatures) <= 2 * num_sms) return launch_thin(g, s);
   }
   if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>(), std::false_type());
-  // Pairs of row tiles where experts have enough of them that an odd one left over costs less than pairs gain (two in a hundred at
-  // 1024 rows an expert; an odd tile is half a tile's time lost per expert, which at 512 rows is one in eight of half the experts).
+  // Pairs of row tiles where experts have enough of them that the odd one left over costs less than pairs gain.  2048 -> 4096, TFLOP/s
+  // in pairs | one by one: 256 rows an expert 1060 | 1073, 512 1327 | 1277, 1024 1490 | 1364, 4096 1692 | 1536; with gradients 256
+  // 634 | 679, 512 1029 | 1039, 1024 1318 | 1238, 4096 1615 | 1517.
   if (mean >= kPairRows && (g.r->nnz / (2 * kTileM) + up(met, 2)) * up(features, 256) >= num_sms / 2)
     return run(integral_constant<int, 256>(), integral_constant<int, kRowsM>(), std::true_type());
   // A tile of 128 features takes two thirds of the time of one of 256 (bound by its operands' way from L2), so the wider one is
@@ -684,7 +685,9 @@ ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_
     return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
   const int64_t wide = g.r->ncols * up(g.N, kTileM) * up(g.K, 256);
   const int64_t pairs = g.r->ncols * up(g.N, 2 * kTileM) * up(g.K, 256);
-  const cudaError_t e = pairs >= num_sms / 2 && up(g.N, kTileM) % 2 == 0
+  const bool paired = static_cast<double>(g.r->nnz) >= kPairRows * static_cast<double>(g.r->ncols) && pairs >= num_sms / 2 &&
+                      up(g.N, kTileM) % 2 == 0;
+  const cudaError_t e = paired
                             ? launch<256, kRowsSum, false, true>(a, b, p, pairs, num_sms, s)
                         : wide >= num_sms
                             ? launch<256, kRowsSum, false>(a, b, p, wide, num_sms, s)

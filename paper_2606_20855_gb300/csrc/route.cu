@@ -82,6 +82,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
 #pragma unroll
     for (int i = 1; i < V; ++i) best = max(best, key[i]);
     uint32_t bound = 0;
+#pragma unroll 4
     for (int r = 0; r < k; ++r) {  // equal maxima leave together: the bound is lower then, not wrong
       bound = __reduce_max_sync(0xffffffffu, best);
       if (best == bound) best = 0;
@@ -116,6 +117,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
       chosen = lane < k;
     } else {
       uint32_t left = my_key;
+#pragma unroll 4
       for (int r = 0; r < k; ++r) {
         const uint32_t top = __reduce_max_sync(0xffffffffu, left);
         if (lane == __ffs(__ballot_sync(0xffffffffu, left == top)) - 1) left = 0, chosen = true;
@@ -175,6 +177,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
                                bool normalize, const int32_t* __restrict__ colidx, const float* __restrict__ vals,
                                const float* __restrict__ gvals, T* __restrict__ glogits, int64_t ldg, bool vecg) {
   constexpr int N = V * sizeof(T) >= 16 ? 16 / sizeof(T) : V;
+  __shared__ __align__(16) float lines[kRouteWarps][32 * V];
   const int lane = threadIdx.x & 31;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRouteWarps + (threadIdx.x >> 5);
   if (row >= rows) return;
@@ -186,7 +189,7 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
     g = gvals[row * k + lane];
   }
   float out[V], a = 0.0f;
-  if (normalize) {  // the zeros do not wait for what was loaded
+  if (normalize) {
 #pragma unroll
     for (int i = 0; i < V; ++i) out[i] = 0.0f;
   } else {
@@ -206,23 +209,28 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
 #pragma unroll
     for (int i = 0; i < V; ++i) out[i] *= scale;
   }
+  // the chosen columns over the others, in shared memory: every value of the row is stored once
+  float* line = lines[threadIdx.x >> 5];
+#pragma unroll
+  for (int i = 0; i < V; ++i) line[lane * V + i] = out[i];
+  if (normalize) a = warp_sum(v * g);
+  __syncwarp();
+  if (static_cast<unsigned>(col) < static_cast<unsigned>(cols)) line[col] = v * (g - a);
+  __syncwarp();
   T* dst = glogits + row * ldg;
   if (vecg && lane * V + V <= cols) {
 #pragma unroll
     for (int i = 0; i < V; i += N) {
       float part[N];
 #pragma unroll
-      for (int j = 0; j < N; ++j) part[j] = out[i + j];
+      for (int j = 0; j < N; ++j) part[j] = line[lane * V + i + j];
       *reinterpret_cast<Pack<T, N>*>(dst + lane * V + i) = pack<T, N>(part);
     }
+  } else if (vecg) {
+    for (int i = lane * V; i < cols; ++i) dst[i] = from_f32<T>(line[i]);  // the row's last lane, and none after it
   } else {
-#pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (lane * V + i < cols) dst[lane * V + i] = from_f32<T>(out[i]);
+    for (int i = lane; i < cols; i += 32) dst[i] = from_f32<T>(line[i]);
   }
-  if (normalize) a = warp_sum(v * g);
-  __syncwarp();  // the chosen columns over what the row's lanes stored
-  if (static_cast<unsigned>(col) < static_cast<unsigned>(cols)) dst[col] = from_f32<T>(v * (g - a));
 }
 
 template <typename F>
