@@ -106,8 +106,9 @@ __device__ __forceinline__ int next_adapter(int col, int* mins) {
 
 // h of 128 tokens over one part of K: one lane fetches x's and A's values through a ring of stages, one multiplies (D: tokens x
 // ranks, two accumulators), a thread per token stores.  Adapters of up to 32 or 16 ranks go two or four to a pass: a tile at
-// the border of two requests then reads x once, like the others.  (8191 tokens of 4096 halves, rank 32: 24 us with
-// tiles of 32 tokens on the warp-level instruction, 29 us with a pass for each adapter, 19 us so.)
+// the border of two requests then reads x once, like the others.  (8191 tokens of 4096 halves, rank 32, 67 MB of x, 10 us at the copy
+// rate: 16 us; 24 us with tiles of 32 tokens on the warp-level instruction, 29 us with a pass for each adapter, 19 us without
+// asking for a stage ahead.)
 __global__ void __launch_bounds__(kShrinkThreads, 1)
     shrink_tile_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_a,
                        const ws_adapters_call c, float* __restrict__ h, int rpad, int* status) {
@@ -296,8 +297,9 @@ __device__ __noinline__ float added(const ws_adapters_call& c, const float* h, i
 
 // 256 values of 128 tokens: base arrives while the products run; the sums go through the same piece of shared memory to y.  Two
 // CTAs share an SM, so that one's latencies (row pointer, column, h and B, product, store) pass under the other's
-// work.  (8191 tokens, rank 32, 2048 halves: 31 us on the warp-level instruction, 38 us in columns of 128 values, 34 us with a CTA that
-// keeps v h for two columns, 30 us so.)
+// work.  8192 tokens, 2048 halves: 17 us without adapters (base to y, 67 MB; 10 us at the copy rate), 20 us with rank 16, 24 us with
+// rank 32; on the warp-level instruction 31 us, in columns of 128 values 38 us, with a CTA that keeps v h for two columns 34 us,
+// with a thread for each token's v h 25-28 us (its loads touch 32 rows at a time).
 template <bool half>
 __global__ void __launch_bounds__(kExpandThreads, 2)
     expand_tile_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_base,
@@ -307,7 +309,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   __shared__ __align__(8) uint64_t base_bar, b_bar, m_bar;
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int dead;
-  __shared__ int mins[kExpandThreads / 32];
+  __shared__ int mins[kExpandThreads / 32], entry[kTok];
+  __shared__ float value[kTok];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = threadIdx.x & (kTok - 1), side = threadIdx.x / kTok;
   const uint32_t sa = (smem_u32(raw) + 1023u) & ~1023u, sy = sa + kExpandA, sb = sy + 4 * kExpandY;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTok, t = t0 + m;
@@ -342,7 +345,11 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
     const int a = next_adapter<kExpandThreads / 32>(w.col, mins);
     if (a == INT_MAX || dead) break;  // dead was set before the barrier in there, or is not for a while
     const bool mine = w.col == a;
-    const float v = mine ? c.vals[w.at] : 0.0f;
+    if (side == 0) {
+      entry[m] = mine ? w.at : -1;
+      value[m] = mine ? c.vals[w.at] : 0.0f;
+    }
+    __syncthreads();
     for (int r0 = 0; r0 < rpad; r0 += kExpandRanks) {
       const int ranks = min(kExpandRanks, rpad - r0);  // 16 or 32
       if (done > 0) bar_wait(smem_u32(&m_bar), (done - 1) & 1, &dead);  // what reads A and B is over
@@ -350,36 +357,32 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
         bar_expect(smem_u32(&b_bar), kExpandB);
         tma_3d(sb, &map_b, r0, n0, a, smem_u32(&b_bar));
       }
-      float4 part[kExpandRanks / 16][2][kMaxSplit];  // all of the thread's loads in flight at once
+      // v h of 128 tokens, four ranks a thread and turn, neighbouring threads along a token's ranks; all loads in flight at once
+      const int log_quads = ranks == kExpandRanks ? 3 : 2;
+      constexpr int kTurns = kTok * (kExpandRanks / 4) / kExpandThreads;
+      float4 part[kTurns][kMaxSplit];
 #pragma unroll
-      for (int i = 0; i < kExpandRanks / 16; ++i)
+      for (int i = 0; i < kTurns; ++i) {
+        const int at = threadIdx.x + kExpandThreads * i, e = at >> log_quads < kTok ? entry[at >> log_quads] : -1;
 #pragma unroll
-        for (int e = 0; e < 2; ++e)
+        for (int k = 0; k < kMaxSplit; ++k)
+          part[i][k] = e >= 0 && k < split ? *reinterpret_cast<const float4*>(h + (static_cast<int64_t>(k) * c.nnz + e) * rpad + r0 +
+                                                                               4 * (at & ((1 << log_quads) - 1)))
+                                           : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      }
 #pragma unroll
-          for (int k = 0; k < kMaxSplit; ++k)
-            part[i][e][k] = mine && 16 * i < ranks && k < split
-                                ? *reinterpret_cast<const float4*>(h + (static_cast<int64_t>(k) * c.nnz + w.at) * rpad + r0 + 16 * i + 8 * side + 4 * e)
-                                : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      for (int i = 0; i < kTurns; ++i) {
+        const int at = threadIdx.x + kExpandThreads * i, row = at >> log_quads, quad = at & ((1 << log_quads) - 1);
+        if (row >= kTok) break;
+        float4 f = part[i][0];
 #pragma unroll
-      for (int i = 0; i < kExpandRanks / 16; ++i) {
-        const int j = 16 * i + 8 * side;
-        if (j >= ranks) break;
-        uint32_t hi[4], lo[4];
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          float4 f = part[i][e][0];
-#pragma unroll
-          for (int k = 1; k < kMaxSplit; ++k) f.x += part[i][e][k].x, f.y += part[i][e][k].y, f.z += part[i][e][k].z, f.w += part[i][e][k].w;
-          const uint2 a01 = split_pair<half>(v * f.x, v * f.y), a23 = split_pair<half>(v * f.z, v * f.w);
-          hi[2 * e] = a01.x, lo[2 * e] = a01.y, hi[2 * e + 1] = a23.x, lo[2 * e + 1] = a23.y;
-        }
-        const uint32_t row = sa + m * 128;
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((j >> 3) ^ (m & 7)) << 4)), "r"(hi[0]),
-                     "r"(hi[1]), "r"(hi[2]), "r"(hi[3])
-                     : "memory");
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(row + (((4 + (j >> 3)) ^ (m & 7)) << 4)), "r"(lo[0]),
-                     "r"(lo[1]), "r"(lo[2]), "r"(lo[3])
-                     : "memory");
+        for (int k = 1; k < kMaxSplit; ++k) f.x += part[i][k].x, f.y += part[i][k].y, f.z += part[i][k].z, f.w += part[i][k].w;
+        const float s = value[row];
+        const uint2 a01 = split_pair<half>(s * f.x, s * f.y), a23 = split_pair<half>(s * f.z, s * f.w);
+        const uint32_t to = sa + row * 128 + 8 * (quad & 1), hi = to + (((quad >> 1) ^ (row & 7)) << 4),
+                       lo = to + (((4 + (quad >> 1)) ^ (row & 7)) << 4);
+        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(hi), "r"(a01.x), "r"(a23.x) : "memory");
+        asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(lo), "r"(a01.y), "r"(a23.y) : "memory");
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       if (!__syncthreads_and(mine || !there)) mixed = true;
