@@ -440,8 +440,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
           asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at) : "memory");
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          b[i] = bits16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i]) |
-                 static_cast<uint32_t>(bits16<half>(value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1])) << 16;
+          b[i] = pair16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i],
+                              value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1]);
         asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
       }
     }

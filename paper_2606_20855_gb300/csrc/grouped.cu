@@ -16,8 +16,9 @@
 // is given to the tensor cores as "MN-major", never transposed by a copy.
 //
 // A tile of rows may reach past its expert's last row: such rows are computed
-// and not stored.  In `weights` they would be summed, so the last stage's rows
-// past the end are cleared in shared memory (in both operands: 0 * inf is NaN).
+// and not stored.  In `weights` they would be summed, so the last stage is
+// multiplied as far as it has rows, in steps of 16, and the rows past the end in the last
+// step are cleared in shared memory (in both operands: 0 * inf is NaN).
 #include <type_traits>
 
 #include "routing.cuh"
@@ -140,12 +141,17 @@ __device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first
 template <typename On>
 __device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t turn, uint16_t* dst, const float (&f)[64], int left, On on) {
   const int lane = threadIdx.x & 31;
+  uint32_t all[32];
+  if (p.half) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) all[i] = pair16<true>(f[2 * i], f[2 * i + 1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) all[i] = pair16<false>(f[2 * i], f[2 * i + 1]);
+  }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      w[i] = round16(f[8 * j + 2 * i], p.half) | static_cast<uint32_t>(round16(f[8 * j + 2 * i + 1], p.half)) << 16;
+    const uint32_t* w = all + 4 * j;
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(turn + lane * 128 + ((j ^ (lane & 7)) << 4)), "r"(w[0]), "r"(w[1]),
                  "r"(w[2]), "r"(w[3])
                  : "memory");
@@ -349,7 +355,8 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
           const uint32_t sa = base + stage * S::kStageBytes, sb = sa + kBytesA;
           const int next = stage + 1 == S::kStages ? 0 : stage + 1;
           const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
-          if (kRows == kRowsSum && t.rows - k * kTileK < kTileK) {
+          const int rows = kRows == kRowsSum ? t.rows - k * kTileK : kTileK;  // in the stage, or more
+          if (kRows == kRowsSum && rows < kTileK) {
             ok = bar_wait<kPair>(smem_u32(&clear_bar[stage]), cleared >> stage & 1, &dead);
             cleared ^= 1u << stage;
           } else if (!ready) {
@@ -361,6 +368,7 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
           const uint64_t da = smem_desc(sa, kAMN), db = smem_desc(sb, kBMN);
 #pragma unroll
           for (int j = 0; j < kTileK / 16; ++j) {
+            if (kRows == kRowsSum && 16 * j >= rows) break;
             const uint64_t a = da + j * (kAMN ? 2048 >> 4 : 32 >> 4), b = db + j * (kBMN ? 2048 >> 4 : 32 >> 4);
             if constexpr (kPair) mma_f16_pair(tmem + acc * BN, a, b, idesc, k > 0 || j > 0);
             else mma_f16(tmem + acc * BN, a, b, idesc, k > 0 || j > 0);
@@ -383,7 +391,7 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
       }
     }
   } else if (kRows == kRowsSum && warp == 6) {
-    // clears the rows behind a group's last in the stage that holds them
+    // clears the rows behind a group's last, up to the next multiple of 16, in the stage that holds them
     int64_t steps = 0;
     uint32_t cleared = 0;
     bool ok = true;
@@ -397,7 +405,7 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
       if (!ok) break;
       const uint32_t at = base + stage * S::kStageBytes;
       for (int b = 0; b < S::kStageBytes / 8192; ++b)
-        for (int c = rows * 8 + lane; c < kTileK * 8; c += 32)
+        for (int c = rows * 8 + lane; c < ((rows + 15) & ~15) * 8; c += 32)
           asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(at + b * 8192 + c * 16), "r"(0) : "memory");
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       __syncwarp();

@@ -79,6 +79,17 @@ __device__ __forceinline__ uint16_t bits16(float f) {
   if constexpr (half) return __half_as_ushort(__float2half_rn(f));
   else return __bfloat16_as_ushort(__float2bfloat16_rn(f));
 }
+// Two of them, a in the lower half.
+template <bool half>
+__device__ __forceinline__ uint32_t pair16(float a, float b) {
+  if constexpr (half) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  } else {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+  }
+}
 // The warp-level matrix instruction: d (16 x 8) += a (16 x 16) b (16 x 8).  Lane 4 g + q holds rows g (a0, a2) and g + 8 (a1,
 // a3) of a and column g of b; a0, a1, b0 are one pair of the contraction index, a2, a3, b1 another, the same pairs for all
 // lanes of a q.  d: rows g (d0, d1) and g + 8, columns 2 q and 2 q + 1.
