@@ -179,7 +179,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
             }
             const int next = stage + 1 == kShrinkStages ? 0 : stage + 1;
             const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
-            ready = bar_try(smem_u32(&empty_bar[next]), next_phase ^ 1);
+            ready = bar_ask(smem_u32(&empty_bar[next]), next_phase ^ 1);
             const uint32_t bar = smem_u32(&full_bar[stage]), at = base + stage * kShrinkStage;
             const int rows = min(kRankBlock, rpad);  // of the copy; past r they are zero
             bar_expect(bar, kTok * 128 + these * rows * 128);
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const int next = stage + 1 == kShrinkStages ? 0 : stage + 1;
             const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
-            ready = bar_try(smem_u32(&full_bar[next]), next_phase);
+            ready = bar_ask(smem_u32(&full_bar[next]), next_phase);
             const uint32_t at = base + stage * kShrinkStage;
             const uint64_t da = smem_desc(at, false), db = smem_desc(at + kTok * 128, false);
 #pragma unroll

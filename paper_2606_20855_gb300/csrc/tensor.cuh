@@ -56,8 +56,18 @@ __device__ __forceinline__ unsigned long long now_ns() {
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
   return t;
 }
-// An answer of bar_try takes more than 200 cycles (measured), about half of what a stage's products take: the loops below ask for
-// the next stage before they work on this one, and wait only if the answer was no.
+// Whether the phase is over, asked without a wait.
+__device__ __forceinline__ bool bar_ask(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile(
+      "{\n .reg .pred p;\n mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}\n"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity)
+      : "memory");
+  return ok != 0;
+}
+// An answer of bar_try takes more than 200 cycles (measured), about half of what a stage's products take: the loops of the kernels
+// ask for the next stage, without a wait, before they work on this one, and wait only if the answer was no.
 //
 // Waits for a phase; gives up after kWaitLimitNs or when another role gave up (*dead).
 template <bool kPair = false>
