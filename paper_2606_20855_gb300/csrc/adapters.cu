@@ -618,7 +618,7 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
                                              static_cast<int>(kExpandSmem));
   if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
   const dim3 grid(tiles, static_cast<unsigned>((c.N + kExpandN - 1) / kExpandN));
-  const cudaError_t launched = launch_early(kernel, grid, kExpandThreads, kExpandSmem, s, b, base, y, c,
+  const cudaError_t launched = launch_early(kernel, grid, kExpandThreads, kExpandSmem, s, 1, b, base, y, c,
                                             static_cast<const float*>(h), rpad, split, copies, status);
   if (launched != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(launched));
   return WS_OK;

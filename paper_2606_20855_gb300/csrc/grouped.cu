@@ -245,6 +245,7 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) tmem_alloc<S::kAccCols, kPair>(smem_u32(&tmem_slot));
+  wait_for_last();
   if constexpr (kRows != kRowsSum) {  // row tiles before every group
     int sum = 0;
     for (int e0 = 0; e0 < p.groups; e0 += kThreadsOf<kRows>) {
@@ -263,6 +264,7 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
   if constexpr (kPair) pair_sync();  // the other CTA's barriers are there
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = tmem_slot;
+  may_start_next();
 
   if (warp == 0) {
     if (elect_one()) {
@@ -492,14 +494,15 @@ constexpr int kThinRows = 8, kThinFeatures = 32;
 
 template <bool half>
 __global__ void __launch_bounds__(kThinThreads, 3)
-    thin_kernel(const int64_t* __restrict__ offsets, int groups, const uint16_t* __restrict__ x, int64_t ldx,
-                const uint16_t* __restrict__ W, int64_t ldw, int64_t group_stride, uint16_t* __restrict__ y, int64_t ldy,
+    thin_kernel(const int64_t* offsets, int groups, const uint16_t* x, int64_t ldx,
+                const uint16_t* W, int64_t ldw, int64_t group_stride, uint16_t* y, int64_t ldy,
                 int N, int K) {
   __shared__ float red[kThinWarps][kThinFeatures][kThinRows + 1];
   __shared__ int scratch[32];
   __shared__ int found[3];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
   if (threadIdx.x == 0) found[0] = -1;
+  wait_for_last();
   int sum = 0;
   const int want = blockIdx.y;
   for (int e0 = 0; e0 < groups && sum <= want; e0 += kThinThreads) {
@@ -572,10 +575,9 @@ cudaError_t launch_thin(const GroupedRows& g, cudaStream_t s) {
   const dim3 grid(static_cast<unsigned>((g.N + kThinFeatures - 1) / kThinFeatures),
                   static_cast<unsigned>(g.r->nnz / kThinRows + met));
   const auto kernel = g.half ? thin_kernel<true> : thin_kernel<false>;
-  kernel<<<grid, kThinThreads, 0, s>>>(g.r->offsets, static_cast<int>(g.r->ncols), static_cast<const uint16_t*>(g.x), g.ldx,
-                                       static_cast<const uint16_t*>(g.w), g.ldw, g.group_stride,
-                                       static_cast<uint16_t*>(g.out), g.ldo, static_cast<int>(g.N), static_cast<int>(g.K));
-  return cudaGetLastError();
+  return launch_early(kernel, grid, kThinThreads, 0, s, 1, g.r->offsets, static_cast<int>(g.r->ncols), static_cast<const uint16_t*>(g.x),
+                      g.ldx, static_cast<const uint16_t*>(g.w), g.ldw, g.group_stride, static_cast<uint16_t*>(g.out), g.ldo,
+                      static_cast<int>(g.N), static_cast<int>(g.K));
 }
 
 // ---------------------------------------------------------------- host
@@ -590,23 +592,7 @@ cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const GroupedPara
   if (e != cudaSuccess) return e;
   const int64_t teams = kPair ? num_sms / 2 : num_sms;
   const unsigned grid = static_cast<unsigned>((tiles < teams ? tiles : teams) * (kPair ? 2 : 1));
-  if constexpr (kPair) {
-    cudaLaunchAttribute pair{};
-    pair.id = cudaLaunchAttributeClusterDimension;
-    pair.val.clusterDim.x = 2;
-    pair.val.clusterDim.y = pair.val.clusterDim.z = 1;
-    cudaLaunchConfig_t config{};
-    config.gridDim = dim3(grid);
-    config.blockDim = dim3(kThreadsOf<kRows>);
-    config.dynamicSmemBytes = S::kSmem;
-    config.stream = s;
-    config.attrs = &pair;
-    config.numAttrs = 1;
-    return cudaLaunchKernelEx(&config, kernel, a, b, p);
-  } else {
-    kernel<<<grid, kThreadsOf<kRows>, S::kSmem, s>>>(a, b, p);
-    return cudaGetLastError();
-  }
+  return launch_early(kernel, dim3(grid), kThreadsOf<kRows>, S::kSmem, s, kPair ? 2 : 1, a, b, p);
 }
 
 int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }

@@ -159,6 +159,7 @@ __global__ void __launch_bounds__(32 * kSmallWarps) routing_small_kernel(ws_rout
   const int warps = blockDim.x >> 5;
   extern __shared__ __align__(16) int sm[];
   __shared__ int scratch[32];
+  may_start_next();
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
   int* first = sm + warps * cols;
   uint16_t* pre = reinterpret_cast<uint16_t*>(first + 2 * cols);
@@ -218,6 +219,7 @@ __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, 
   for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = before[e] = 0;
   __syncthreads();
   mark_rows(r, w, cols, mask);
+  may_start_next();
   wait_for_last();
   const int quads = (cols + 3) / 4, groups = kTileRows / quads;  // at most 256 quads: a thread each
   const int g = static_cast<int>(threadIdx.x) / quads, v = static_cast<int>(threadIdx.x) - g * quads;
@@ -285,8 +287,10 @@ __device__ __forceinline__ void zero_rest(const ws_routing& r, char* rows, int64
 // A warp per (row, segment of 32 U packs): the segment is read once and stored to every slot of the row.
 template <typename P, int U>
 __global__ void __launch_bounds__(kMoveThreads)
-    dispatch_kernel(ws_routing r, const char* __restrict__ x, int64_t ldx, char* __restrict__ xs, int64_t ldxs,
+    dispatch_kernel(ws_routing r, const char* x, int64_t ldx, char* xs, int64_t ldxs,
                     int packs, int segs) {
+  may_start_next();
+  wait_for_last();
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * kMoveWarps + (threadIdx.x >> 5);
   zero_rest<P>(r, xs, ldxs, packs, unit, static_cast<int64_t>(gridDim.x) * kMoveWarps, threadIdx.x & 31, 32);
   const int64_t row = unit / segs;
@@ -316,8 +320,10 @@ constexpr int kSumThreads = 128;
 
 template <typename T, int N, bool weighted>
 __global__ void __launch_bounds__(kSumThreads, 8)
-    combine_kernel(ws_routing r, const T* __restrict__ ys, int64_t ldys, T* __restrict__ y, int64_t ldy, int packs,
+    combine_kernel(ws_routing r, const T* ys, int64_t ldys, T* y, int64_t ldy, int packs,
                    int log_group, int parts) {
+  may_start_next();
+  wait_for_last();
   constexpr int kBatch = 4;
   const int group = 1 << log_group;
   const int64_t unit = (static_cast<int64_t>(blockIdx.x) * kSumThreads + threadIdx.x) >> log_group;
@@ -384,8 +390,10 @@ __device__ __forceinline__ void store_group(T* p, int count, const float (&f)[N]
 
 template <typename T, int M>
 __global__ void __launch_bounds__(kDotThreads)
-    combine_backward_kernel(ws_routing r, const T* __restrict__ gy, int64_t ldgy, const T* __restrict__ ys,
-                            int64_t ldys, T* __restrict__ gys, int64_t ldgys, float* __restrict__ gvals, int width) {
+    combine_backward_kernel(ws_routing r, const T* gy, int64_t ldgy, const T* ys,
+                            int64_t ldys, T* gys, int64_t ldgys, float* gvals, int width) {
+  may_start_next();
+  wait_for_last();
   constexpr int N = 16 / sizeof(T);
   __shared__ float part[kDotThreads / 32][kDotGroup];
   const int64_t row = blockIdx.x;
@@ -445,6 +453,8 @@ __global__ void __launch_bounds__(kDotThreads)
 constexpr int kAlignThreads = 256;
 
 __global__ void __launch_bounds__(kAlignThreads) align_rows_kernel(const AlignedCopies c) {
+  may_start_next();
+  wait_for_last();
   int64_t at = static_cast<int64_t>(blockIdx.x) * kAlignThreads + threadIdx.x;
   int i = 0;
   while (i < c.count && at >= c.m[i].groups * c.m[i].rows * c.m[i].packs) at -= c.m[i].groups * c.m[i].rows * c.m[i].packs, ++i;
@@ -526,13 +536,13 @@ void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cud
   allow(reinterpret_cast<const void*>(routing_count_kernel), smem);
   allow(reinterpret_cast<const void*>(routing_place_kernel), smem);
   routing_count_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
-  launch_early(routing_place_kernel, dim3(static_cast<unsigned>(chunks)), kTileRows, smem, s, r, cols, chunk, counts);
+  launch_early(routing_place_kernel, dim3(static_cast<unsigned>(chunks)), kTileRows, smem, s, 1, r, cols, chunk, counts);
 }
 
 void launch_align(const AlignedCopies& c, cudaStream_t s) {
   int64_t packs = 0;
   for (int i = 0; i < c.count; ++i) packs += c.m[i].groups * c.m[i].rows * c.m[i].packs;
-  if (packs > 0) align_rows_kernel<<<static_cast<unsigned>((packs + kAlignThreads - 1) / kAlignThreads), kAlignThreads, 0, s>>>(c);
+  if (packs > 0) launch_early(align_rows_kernel, dim3(static_cast<unsigned>((packs + kAlignThreads - 1) / kAlignThreads)), kAlignThreads, 0, s, 1, c);
 }
 
 void launch_dispatch(const ws_routing& r, const void* x, int64_t ldx, void* xs, int64_t ldxs, int64_t width,
@@ -547,10 +557,10 @@ void launch_dispatch(const ws_routing& r, const void* x, int64_t ldx, void* xs, 
     // Four packs a lane where the warps still fill the GPU, else one: a short call lasts as long as its longest warp.
     if (r.nrows * static_cast<int64_t>(packs) >= 32 * 4 * 8192) {
       const int segs = (packs + 127) / 128;
-      dispatch_kernel<P, 4><<<warp_grid(r.nrows * segs), kMoveThreads, 0, s>>>(r, src, ldx * z, dst, ldxs * z, packs, segs);
+      launch_early(dispatch_kernel<P, 4>, dim3(warp_grid(r.nrows * segs)), kMoveThreads, 0, s, 1, r, src, ldx * z, dst, ldxs * z, packs, segs);
     } else {
       const int segs = (packs + 31) / 32;
-      dispatch_kernel<P, 1><<<warp_grid(r.nrows * segs), kMoveThreads, 0, s>>>(r, src, ldx * z, dst, ldxs * z, packs, segs);
+      launch_early(dispatch_kernel<P, 1>, dim3(warp_grid(r.nrows * segs)), kMoveThreads, 0, s, 1, r, src, ldx * z, dst, ldxs * z, packs, segs);
     }
   });
 }
@@ -570,8 +580,8 @@ void launch_combine(const ws_routing& r, bool weighted, const void* ys, int64_t 
         const int group = 1 << log_group;
         const int parts = r.nrows * group >= int64_t{8} * kSumThreads * num_sms ? 1 : (packs + group - 1) / group;
         const auto kernel = weighted ? combine_kernel<T, N, true> : combine_kernel<T, N, false>;
-        kernel<<<static_cast<unsigned>((r.nrows * parts * group + kSumThreads - 1) / kSumThreads), kSumThreads, 0, s>>>(
-            r, static_cast<const T*>(ys), ldys, static_cast<T*>(y), ldy, packs, log_group, parts);
+        launch_early(kernel, dim3(static_cast<unsigned>((r.nrows * parts * group + kSumThreads - 1) / kSumThreads)), kSumThreads, 0, s, 1,
+                     r, static_cast<const T*>(ys), ldys, static_cast<T*>(y), ldy, packs, log_group, parts);
       }
     });
   });
@@ -587,8 +597,7 @@ void launch_combine_backward(const ws_routing& r, const void* gy, int64_t ldgy, 
                constexpr int B = decltype(b)::value;
                if constexpr (B >= static_cast<int>(sizeof(T))) {
                  constexpr int N = B / sizeof(T);
-                 combine_backward_kernel<T, N><<<static_cast<unsigned>(r.nrows), kDotThreads, 0, s>>>(
-                     r, static_cast<const T*>(gy), ldgy, static_cast<const T*>(ys), ldys, static_cast<T*>(gys), ldgys,
+                 launch_early(combine_backward_kernel<T, N>, dim3(static_cast<unsigned>(r.nrows)), kDotThreads, 0, s, 1, r, static_cast<const T*>(gy), ldgy, static_cast<const T*>(ys), ldys, static_cast<T*>(gys), ldgys,
                      gvals, static_cast<int>(width));
                }
              });

@@ -118,19 +118,23 @@ __device__ __forceinline__ uint4 load8(const uint16_t* row, int k, int K, bool v
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
 // A kernel that may start while the one before it on the stream still runs (as soon as all of that one's CTAs have called
-// may_start_next, or are done) and calls wait_for_last before it touches what that one writes or reads.
+// may_start_next, or are done) and calls wait_for_last before it touches what that one writes or reads.  Every CTA calls it, so that the
+// kernel's end comes after the end of the one before.  `together`: CTAs of a cluster.
 template <typename... P, typename... A>
-cudaError_t launch_early(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, A... args) {
-  cudaLaunchAttribute early{};
-  early.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-  early.val.programmaticStreamSerializationAllowed = 1;
+cudaError_t launch_early(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t s, int together, A... args) {
+  cudaLaunchAttribute attrs[2]{};
+  attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attrs[0].val.programmaticStreamSerializationAllowed = 1;
+  attrs[1].id = cudaLaunchAttributeClusterDimension;
+  attrs[1].val.clusterDim.x = together;
+  attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
   cudaLaunchConfig_t config{};
   config.gridDim = grid;
   config.blockDim = dim3(threads);
   config.dynamicSmemBytes = smem;
   config.stream = s;
-  config.attrs = &early;
-  config.numAttrs = 1;
+  config.attrs = attrs;
+  config.numAttrs = together > 1 ? 2 : 1;
   return cudaLaunchKernelEx(&config, kernel, static_cast<P>(args)...);
 }
 __device__ __forceinline__ void may_start_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
