@@ -466,8 +466,8 @@ ws_status_t ws_routing_matmul_backward(const ws_routing* r, const void* gys, int
  * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned, and for
  * many tokens 16 bytes more for every 8 values, or part of them, of the rows of
  * each of x, A and B whose address or strides are not multiples of 16 bytes.  For
- * many tokens and nnz > 0 its first int is 0 after the call, or nonzero if a
- * kernel's bounded waits ran out.  Queued on `stream`; nothing is allocated.
+ * many tokens its first int is 0 after the call, or nonzero if a kernel's bounded
+ * waits ran out.  Queued on `stream`; nothing is allocated.
  */
 typedef struct ws_adapters_call {
   int64_t nrows, ncols, nnz;

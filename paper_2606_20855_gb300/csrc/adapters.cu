@@ -318,6 +318,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   const int n0 = blockIdx.y * kExpandN;
   const int pieces = min(4, (N - n0 + 63) / 64);  // of 64 values that are there
   const bool there = t < c.nrows;
+  // S and base are there before the inner products start; without those, what comes before is another call, which may write them
+  if (c.nnz == 0) wait_for_last();
   if (threadIdx.x == 0) {
     bar_init(smem_u32(&base_bar), 1);
     bar_init(smem_u32(&b_bar), 1);
@@ -478,7 +480,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
 // ---------------------------------------------------------------- few tokens
 
 // A CTA per token and two pairs of ranks: four warps a pair, each with a quarter of K.  (One warp a pair: 12.4 us for 48 tokens
-// of 4096 values and rank 16, the time of a lane's 16 steps of loads.)
+// of 4096 values and rank 16, the time of a lane's 16 steps of loads; so 6.4 us.)
 constexpr int kStepSplit = 4;
 
 // vec: the rows of x and A start at multiples of 16 bytes.
@@ -540,7 +542,8 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
   }
 }
 
-// A thread per value of y.
+// A thread per value of y: its row of B against v h, which every thread of the CTA reads.  Bound by latencies: 48 tokens of rank 16,
+// 4096 values, 6.3 MB of B: 5 us.
 template <bool half>
 __global__ void __launch_bounds__(kAdThreads) expand_step_kernel(const ws_adapters_call c, const uint2* __restrict__ h, int rpad, bool vecB) {
   const int64_t n = static_cast<int64_t>(blockIdx.x) * kAdThreads + threadIdx.x, t = blockIdx.y;
@@ -591,6 +594,8 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
   const unsigned tiles = static_cast<unsigned>((c.nrows + kTok - 1) / kTok);
   int split = 1;
   if (!encoder()) return routing_fail(WS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
+  cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int), s);
+  if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
   CUtensorMap x{}, a{}, b{}, base{}, y{};
   if (c.nnz > 0) {
     // parts of K until every SM has a CTA
@@ -600,9 +605,8 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
         !encode(&a, c.A, half, c.K, c.r, c.lda, c.ncols, c.strideA, rpad < kRankBlock ? rpad : kRankBlock) ||
         !encode(&b, c.B, half, c.r, c.N, c.ldb, c.ncols, c.strideB, kExpandN, kExpandRanks))
       return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
-    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(shrink_tile_kernel),
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kShrinkSmem));
-    if (e == cudaSuccess) e = cudaMemsetAsync(status, 0, sizeof(int), s);
+    e = cudaFuncSetAttribute(reinterpret_cast<const void*>(shrink_tile_kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                             static_cast<int>(kShrinkSmem));
     if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
     const dim3 grid(tiles, static_cast<unsigned>(split), static_cast<unsigned>((rpad + kRankBlock - 1) / kRankBlock));
     shrink_tile_kernel<<<grid, kShrinkThreads, kShrinkSmem, s>>>(x, a, c, h, rpad, status);
@@ -614,8 +618,8 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
                   (!c.base || encode(&base, c.base, half, c.N, c.nrows, c.ldbase, 0, 0, kTok))))
     copies = false;
   const auto kernel = half ? expand_tile_kernel<true> : expand_tile_kernel<false>;
-  const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             static_cast<int>(kExpandSmem));
+  e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                           static_cast<int>(kExpandSmem));
   if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
   const dim3 grid(tiles, static_cast<unsigned>((c.N + kExpandN - 1) / kExpandN));
   const cudaError_t launched = launch_early(kernel, grid, kExpandThreads, kExpandSmem, s, 1, b, base, y, c,

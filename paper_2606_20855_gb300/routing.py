@@ -312,15 +312,16 @@ class Routing:
 
 
 def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, base: torch.Tensor | None = None,
-             out: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+             out: torch.Tensor | None = None, stream=None, wait: bool = False) -> torch.Tensor:
     """y[t] = base[t] + sum over row t of S of value * B[a] (A[a] x[t]): low-rank adapters of many requests beside the
     projection they share (``base``, its result; None for zero).
 
     x: T x K, A: L x r x K, B: L x N x r, base: T x N, bfloat16 or float16; S: T x L in CSR, float32 values, rows empty
-    for tokens without an adapter.  ``out`` may be ``base``: the adapters' part is then added in place.
+    for tokens without an adapter.  ``out`` may be ``base``: the adapters' part is then added in place.  ``wait``: waits for the
+    result and raises if a kernel gave up a wait.
     """
     if stream is not None:
-        return _elsewhere(adapters, stream, x, A, B, S, base, out)
+        return _elsewhere(adapters, stream, x, A, B, S, base, out, wait=wait)
     dt = _dtype(x, "x")
     (La, r, K), (L, N, rb) = A.shape, B.shape
     if La != L or r != rb:
@@ -363,6 +364,10 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
                                    x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), ldb, apartB,
                                    0 if base is None else base.data_ptr(), ldbase, out.data_ptr(), ldy, dt)
     _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(dev.index))
+    if wait:
+        torch.cuda.current_stream(dev).synchronize()
+        if T * rank > 8192 and N > 0 and scratch[:4].view(torch.int32).item():
+            raise _abi.WsError("adapters", 8, "a kernel gave up a wait")
     return out
 
 

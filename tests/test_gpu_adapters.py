@@ -150,6 +150,24 @@ def test_beside_the_shared_projection():
     _check(x, A, B, S, want, adapters(x, A, B, S, base, out=base))
 
 
+@pytest.mark.parametrize("how", ["none", "runs"])
+def test_base_from_the_product_before(how):
+    """base is the result of a product that may still run when the call is queued."""
+    from paper_2606_20855_gb300 import DeviceCSR, Routing, adapters
+    T, K, N, L, r, dt = 4096, 1024, 1024, 4, 16, torch.bfloat16
+    x, W = _randn((T, K), dt, 90), _randn((1, N, K), dt, 91, K ** -0.5)
+    A, B = _randn((L, r, K), dt, 92, K ** -0.5), _randn((L, N, r), dt, 93)
+    one = DeviceCSR(T, 1, torch.arange(T + 1, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda"),
+                    torch.ones(T, device="cuda"))
+    plan, S = Routing(one), _select(T, L, how, 94)
+    torch.cuda.synchronize()
+    for _ in range(4):
+        base = plan.matmul(x, W)
+        got = adapters(x, A, B, S, base, wait=True)
+        _check(x, A, B, S, base, got)
+        base.fill_(float("nan"))
+
+
 def test_equal_inputs_give_equal_bits():
     from paper_2606_20855_gb300 import adapters
     for T in (30, 900):
