@@ -27,12 +27,16 @@ namespace {
 // ---------------------------------------------------------------- R transposed
 
 // A tile is 32 rows for each warp of a CTA: 32 warps where one CTA builds the
-// plan alone (a single launch), eight where many CTAs do (a launch that counts
-// and one that places).  Bound by latencies, not bytes: 33 rows of eight entries
-// over 64 columns 5 us in the single launch, 8191 rows of eight over 64 columns
-// 4 + 8 us, 16,385 rows of four over 257 columns 4 + 15 us in the two.
-constexpr int kSmallWarps = 32, kBuildWarps = 8;
-constexpr int kSmallRows = 32 * kSmallWarps, kTileRows = 32 * kBuildWarps;
+// plan alone (a single launch), eight or 16 where many CTAs do (a launch that
+// counts and one that places).  Bound by latencies, not bytes: 33 rows of eight
+// entries over 64 columns 5 us in the single launch; in the two 8191 rows of
+// eight over 64 columns 7 us, 16,385 rows of four over 257 columns 9 us.
+constexpr int kSmallWarps = 32, kSmallRows = 32 * kSmallWarps;
+// A tile's warps.  More of them make fewer chunks, whose counts every CTA adds up (rows / (32 W) times cols of them); fewer are less work
+// for a CTA.  us with 8 | 16 warps: 8191 rows of four over 256 columns 7.7 | 8.1, 16,385 over 128 7.8 | 8.1, over 256 10.2 | 8.9,
+// 65,537 over 96 13.8 | 10.0, of eight over 512 32 | 20; with 32 warps 13 for 16,385 over 257, where 16 take 9.
+int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
+int build_warps(int64_t rows, int64_t cols) { return cols == 0 || rows < 3'000'000 / cols ? 8 : 16; }
 constexpr int kHeld = 8;  // entries that a lane holds at once: loads in flight, and rows of 8 entries walked once
 
 // The entries of a warp's 32 rows, kHeld a lane at a time.
@@ -178,24 +182,25 @@ __global__ void __launch_bounds__(32 * kSmallWarps) routing_small_kernel(ws_rout
   place_rows(r, w, cols, mask, pre, first);
 }
 
-__global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, int cols, int64_t chunk, int32_t* counts) {
+template <int W>
+__global__ void __launch_bounds__(32 * W) routing_count_kernel(ws_routing r, int cols, int64_t chunk, int32_t* counts) {
   extern __shared__ __align__(16) int sm[];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
-  int* cnt = sm + kBuildWarps * cols;
+  int* cnt = sm + W * cols;
   may_start_next();
   for (int e = threadIdx.x; e < cols; e += blockDim.x) cnt[e] = 0;
   const int64_t begin = chunk * blockIdx.x, end = min(begin + chunk, r.nrows);
-  for (int64_t row0 = begin; row0 < end; row0 += kTileRows) {
+  for (int64_t row0 = begin; row0 < end; row0 += 32 * W) {
     WarpRows w;
     w.start(r, row0 + (threadIdx.x & ~31u));
-    clear_words(mask, kBuildWarps * cols);
+    clear_words(mask, W * cols);
     __syncthreads();
     mark_rows(r, w, cols, mask);
     __syncthreads();
     for (int e = threadIdx.x; e < cols; e += blockDim.x) {
       int n = 0;
 #pragma unroll
-      for (int i = 0; i < kBuildWarps; ++i) n += __popc(mask[i * cols + e]);
+      for (int i = 0; i < W; ++i) n += __popc(mask[i * cols + e]);
       cnt[e] += n;
     }
     __syncthreads();
@@ -206,24 +211,25 @@ __global__ void __launch_bounds__(kTileRows) routing_count_kernel(ws_routing r, 
 
 // Every CTA adds up the counts of all chunks by itself (a few hundred KB from L2, the threads split over the chunks):
 // a launch less than a scan of its own.  It marks its first tile while the counting launch still runs.
-__global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, int cols, int64_t chunk,
-                                                                  const int32_t* counts) {
+template <int W>
+__global__ void __launch_bounds__(32 * W) routing_place_kernel(ws_routing r, int cols, int64_t chunk,
+                                                               const int32_t* counts) {
   extern __shared__ __align__(16) int sm[];
   __shared__ int scratch[32];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
-  int* next = sm + kBuildWarps * cols;  // first slot of the tile in every column
+  int* next = sm + W * cols;            // first slot of the tile in every column
   int* before = next + cols;            // entries of the chunks before this one
   uint16_t* pre = reinterpret_cast<uint16_t*>(before + cols);
   const int64_t begin = chunk * blockIdx.x, end = min(begin + chunk, r.nrows);
   WarpRows w;
   w.start(r, begin + (threadIdx.x & ~31u));
-  clear_words(mask, kBuildWarps * cols);
+  clear_words(mask, W * cols);
   for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = before[e] = 0;
   __syncthreads();
   mark_rows(r, w, cols, mask);
   may_start_next();
   wait_for_last();
-  const int quads = (cols + 3) / 4, groups = kTileRows / quads;  // at most 256 quads: a thread each
+  const int quads = (cols + 3) / 4, groups = 32 * W / quads;  // at most 256 quads: a thread each, or more
   const int g = static_cast<int>(threadIdx.x) / quads, v = static_cast<int>(threadIdx.x) - g * quads;
   if (g < groups) {
     int4 total = make_int4(0, 0, 0, 0), mine = total;
@@ -248,19 +254,19 @@ __global__ void __launch_bounds__(kTileRows) routing_place_kernel(ws_routing r, 
   __syncthreads();
   for (int e = threadIdx.x; e < cols; e += blockDim.x) {
     next[e] += before[e];
-    before[e] = count_column(mask, pre, cols, e, kBuildWarps);
+    before[e] = count_column(mask, pre, cols, e, W);
   }
   __syncthreads();
   place_rows(r, w, cols, mask, pre, next);
-  for (int64_t row0 = begin + kTileRows; row0 < end; row0 += kTileRows) {
+  for (int64_t row0 = begin + 32 * W; row0 < end; row0 += 32 * W) {
     __syncthreads();
     for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
     w.start(r, row0 + (threadIdx.x & ~31u));
-    clear_words(mask, kBuildWarps * cols);
+    clear_words(mask, W * cols);
     __syncthreads();
     mark_rows(r, w, cols, mask);
     __syncthreads();
-    for (int e = threadIdx.x; e < cols; e += blockDim.x) before[e] = count_column(mask, pre, cols, e, kBuildWarps);
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) before[e] = count_column(mask, pre, cols, e, W);
     __syncthreads();
     place_rows(r, w, cols, mask, pre, next);
   }
@@ -516,16 +522,15 @@ unsigned warp_grid(int64_t units) { return static_cast<unsigned>((units + kMoveW
 }  // namespace
 
 // As many chunks as SMs at most, of whole tiles.
-int64_t routing_chunks(int64_t nrows, int num_sms) {
+int64_t routing_chunks(int64_t nrows, int64_t ncols, int num_sms) {
   if (nrows <= kSmallRows) return 1;
-  const int64_t tiles = (nrows + kTileRows - 1) / kTileRows;
-  const int64_t each = (tiles + num_sms - 1) / num_sms;
-  return (tiles + each - 1) / each;
+  const int64_t tiles = up(nrows, 32 * build_warps(nrows, ncols));
+  return up(tiles, up(tiles, num_sms));
 }
 
 void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cudaStream_t s) {
   const int cols = static_cast<int>(r.ncols);
-  const int64_t chunks = routing_chunks(r.nrows, num_sms);
+  const int64_t chunks = routing_chunks(r.nrows, cols, num_sms);
   const auto allow = [&](const void* kernel, size_t smem) {
     if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
   };
@@ -536,13 +541,17 @@ void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cud
     routing_small_kernel<<<1, 32 * warps, smem, s>>>(r, cols);
     return;
   }
-  const size_t smem = build_smem(cols, kBuildWarps);
-  const int64_t tiles = (r.nrows + kTileRows - 1) / kTileRows;
-  const int64_t chunk = (tiles + chunks - 1) / chunks * kTileRows;
-  allow(reinterpret_cast<const void*>(routing_count_kernel), smem);
-  allow(reinterpret_cast<const void*>(routing_place_kernel), smem);
-  routing_count_kernel<<<static_cast<unsigned>(chunks), kTileRows, smem, s>>>(r, cols, chunk, counts);
-  launch_early(routing_place_kernel, dim3(static_cast<unsigned>(chunks)), kTileRows, smem, s, 1, r, cols, chunk, counts);
+  const auto both = [&](auto warps) {
+    constexpr int W = decltype(warps)::value;
+    const size_t smem = build_smem(cols, W);
+    const int64_t chunk = up(up(r.nrows, 32 * W), chunks) * 32 * W;
+    allow(reinterpret_cast<const void*>(routing_count_kernel<W>), smem);
+    allow(reinterpret_cast<const void*>(routing_place_kernel<W>), smem);
+    routing_count_kernel<W><<<static_cast<unsigned>(chunks), 32 * W, smem, s>>>(r, cols, chunk, counts);
+    launch_early(routing_place_kernel<W>, dim3(static_cast<unsigned>(chunks)), 32 * W, smem, s, 1, r, cols, chunk, counts);
+  };
+  if (build_warps(r.nrows, cols) == 8) both(std::integral_constant<int, 8>());
+  else both(std::integral_constant<int, 16>());
 }
 
 void launch_align(const AlignedCopies& c, cudaStream_t s) {

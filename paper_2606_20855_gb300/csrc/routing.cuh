@@ -146,7 +146,7 @@ void launch_topk_route(const void* logits, int64_t rows, int cols, int64_t ld, w
 void launch_topk_route_backward(const void* logits, int64_t rows, int cols, int64_t ld, ws_dtype_t dt, int k,
                                 bool normalize, const int32_t* colidx, const float* vals, const float* gvals,
                                 void* glogits, int64_t ldg, cudaStream_t s);
-int64_t routing_chunks(int64_t nrows, int num_sms);  // chunks of rows counted apart (1: one launch does it all)
+int64_t routing_chunks(int64_t nrows, int64_t ncols, int num_sms);  // chunks of rows counted apart (1: one launch does it all)
 void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cudaStream_t s);
 void launch_dispatch(const ws_routing& r, const void* x, int64_t ldx, void* xs, int64_t ldxs, int64_t width,
                      ws_dtype_t dt, cudaStream_t s);

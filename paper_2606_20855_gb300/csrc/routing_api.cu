@@ -184,7 +184,7 @@ ws_status_t ws_topk_route_backward(const void* logits, int64_t rows, int64_t col
 int64_t ws_routing_scratch(int64_t nrows, int64_t ncols) {
   int sms = 0;
   if (nrows < 0 || ncols < 0 || sm_count(&sms) != WS_OK) return 0;
-  const int64_t chunks = routing_chunks(nrows, sms);
+  const int64_t chunks = routing_chunks(nrows, ncols, sms);
   return chunks == 1 ? 0 : chunks * ((ncols + 3) & ~int64_t{3}) * static_cast<int64_t>(sizeof(int32_t));
 }
 
@@ -197,7 +197,7 @@ ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch
   }
   int sms = 0;
   if (const ws_status_t st = sm_count(&sms)) return st;
-  const int64_t chunks = routing_chunks(r->nrows, sms);
+  const int64_t chunks = routing_chunks(r->nrows, r->ncols, sms);
   if (chunks > 1 && (!scratch || reinterpret_cast<uintptr_t>(scratch) % 16 ||
                      scratch_bytes < chunks * ((r->ncols + 3) & ~int64_t{3}) * static_cast<int64_t>(sizeof(int32_t))))
     return routing_fail(WS_ERR_INVALID_ARG, "scratch smaller than ws_routing_scratch, or misaligned");

@@ -174,6 +174,13 @@ def test_sorted_by_column(T, E, kind):
     assert torch.equal(plan.slots[entries].long(), torch.arange(R.nnz, device="cuda"))
 
 
+@pytest.mark.parametrize("T,E,kind", [(2929, 1024, "ragged"), (2930, 1024, "8"), (12_000, 300, "ragged"), (23_437, 128, "4"),
+                                      (23_438, 128, "sparse"), (100_001, 33, "ragged")])
+def test_many_rows_and_columns_sorted(T, E, kind):
+    """Both sides of the size from which tiles have more warps."""
+    test_sorted_by_column(T, E, kind)
+
+
 @pytest.mark.parametrize("T,E", [(0, 4), (0, 0), (5, 0), (5, 7), (3000, 7)])
 def test_no_entries(T, E):
     from paper_2606_20855_gb300 import Routing
