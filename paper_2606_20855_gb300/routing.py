@@ -170,11 +170,12 @@ class Routing:
         if validate:
             _abi.ws_csr_destroy(R._handle(True, raw))
         scratch = _scratch(T, E, self._index)
-        # offsets, the status word, the scratch; rows, entries and slots
-        words = (E + 3) // 2 * 2  # the scratch starts at a multiple of 16 bytes
-        self._buf = torch.empty(words + scratch // 8, dtype=torch.int64, device=self.device)
-        self._ints = torch.empty((3, nnz), dtype=torch.int32, device=self.device)
-        at, ints = self._buf.data_ptr(), self._ints.data_ptr()
+        # one array: offsets, the status word, the scratch (at a multiple of 16 bytes); rows, entries and slots
+        words = (E + 3) // 2 * 2
+        self._lead = lead = words + scratch // 8
+        self._buf = torch.empty(lead + (3 * nnz + 1) // 2, dtype=torch.int64, device=self.device)
+        at = self._buf.data_ptr()
+        ints = at + 8 * lead
         self._c = _abi.WsRouting(T, E, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), at, ints,
                                  ints + 4 * nnz, ints + 8 * nnz, at + 8 * (E + 1))
         self._r = ctypes.byref(self._c)
@@ -184,17 +185,20 @@ class Routing:
     def offsets(self) -> torch.Tensor:
         return self._buf[:self.R.ncols + 1]
 
+    def _part(self, i: int) -> torch.Tensor:
+        return self._buf[self._lead:].view(torch.int32)[i * self.nnz:(i + 1) * self.nnz]
+
     @property
     def rows(self) -> torch.Tensor:
-        return self._ints[0]
+        return self._part(0)
 
     @property
     def entries(self) -> torch.Tensor:
-        return self._ints[1]
+        return self._part(1)
 
     @property
     def slots(self) -> torch.Tensor:
-        return self._ints[2]
+        return self._part(2)
 
     def _queue(self, t: torch.Tensor) -> int:
         """The current stream, for a call with t; the plan's arrays stay allocated until it is done with them."""
@@ -203,7 +207,7 @@ class Routing:
         raw = _raw_stream(self._index)
         if raw != self._stream:
             s = torch.cuda.current_stream(self.device)
-            for u in (self._buf, self._ints, self.R.rowptr, self.R.colidx, self.R.vals):
+            for u in (self._buf, self.R.rowptr, self.R.colidx, self.R.vals):
                 u.record_stream(s)
         return raw
 
