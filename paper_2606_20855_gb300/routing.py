@@ -102,7 +102,7 @@ def topk_route(logits: torch.Tensor, k: int, normalize: bool = True, stream=None
     dt = _dtype(logits, "logits")
     x, ld = _matrix(logits, "logits", None)
     (T, E), k, dev = x.shape, int(k), x.device
-    if not 1 <= k <= min(E, 32):
+    if k < 1 or k > E or k > 32:
         raise ValueError(f"k must be in 1..min(columns, 32), got {k} of {E}")
     rowptr = torch.empty(T + 1, dtype=torch.int64, device=dev)
     colidx = torch.empty(T * k, dtype=torch.int32, device=dev)
@@ -200,10 +200,19 @@ class Routing:
     def slots(self) -> torch.Tensor:
         return self._part(2)
 
-    def _queue(self, t: torch.Tensor) -> int:
-        """The current stream, for a call with t; the plan's arrays stay allocated until it is done with them."""
-        if t.device.index != self._index:
-            raise TypeError("the rows and the routing matrix must be on one device")
+    def _rows_of(self, t: torch.Tensor, rows: int, name: str):
+        """(t, its row stride, the length of its rows, their type), t being `rows` rows on the plan's device."""
+        dt, shape = _ROW_DTYPES.get(t.dtype), t.shape
+        if dt is None or len(shape) != 2 or shape[0] != rows or t.get_device() != self._index or not t.is_contiguous():
+            dt = _dtype(t, name)
+            t, ld = _matrix(t, name, rows)
+            if t.get_device() != self._index:
+                raise TypeError("the rows and the routing matrix must be on one device")
+            return t, ld, shape[1], dt
+        return t, shape[1], shape[1], dt
+
+    def _queue(self) -> int:
+        """The current stream, for a call; the plan's arrays stay allocated until it is done with them."""
         raw = _raw_stream(self._index)
         if raw != self._stream:
             s = torch.cuda.current_stream(self.device)
@@ -215,74 +224,69 @@ class Routing:
         """xs[slot] = x[row]: the rows of x (T x H) in slot order (nnz x H)."""
         if stream is not None:
             return _elsewhere(self.dispatch, stream, x)
-        dt = _dtype(x, "x")
-        x, ld = _matrix(x, "x", self.R.nrows)
-        H = x.shape[1]
+        x, ld, H, dt = self._rows_of(x, self.R.nrows, "x")
         out = torch.empty((self.nnz, H), dtype=x.dtype, device=self.device)
-        _abi.ws_routing_dispatch(self._r, x.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue(x))
+        _abi.ws_routing_dispatch(self._r, x.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue())
         return out
 
     def dispatch_backward(self, grad_xs: torch.Tensor, stream=None) -> torch.Tensor:
         """Gradient of x: gx[i] = sum of grad_xs over the slots of row i."""
         if stream is not None:
             return _elsewhere(self.dispatch_backward, stream, grad_xs)
-        dt = _dtype(grad_xs, "grad_xs")
-        g, ld = _matrix(grad_xs, "grad_xs", self.nnz)
-        H = g.shape[1]
+        g, ld, H, dt = self._rows_of(grad_xs, self.nnz, "grad_xs")
         out = torch.empty((self.R.nrows, H), dtype=g.dtype, device=self.device)
-        _abi.ws_routing_dispatch_backward(self._r, g.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue(g))
+        _abi.ws_routing_dispatch_backward(self._r, g.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue())
         return out
 
     def combine(self, ys: torch.Tensor, stream=None) -> torch.Tensor:
         """y[i] = sum over row i of R's value times ys[slot]."""
         if stream is not None:
             return _elsewhere(self.combine, stream, ys)
-        dt = _dtype(ys, "ys")
-        ys, ld = _matrix(ys, "ys", self.nnz)
-        H = ys.shape[1]
+        ys, ld, H, dt = self._rows_of(ys, self.nnz, "ys")
         out = torch.empty((self.R.nrows, H), dtype=ys.dtype, device=self.device)
-        _abi.ws_routing_combine(self._r, ys.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue(ys))
+        _abi.ws_routing_combine(self._r, ys.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue())
         return out
 
     def combine_backward(self, grad_y: torch.Tensor, ys: torch.Tensor, stream=None):
         """Gradients of ys (value times grad_y's row) and of R's values (the products of grad_y's and ys's rows)."""
         if stream is not None:
             return _elsewhere(self.combine_backward, stream, grad_y, ys)
-        dt = _dtype(ys, "ys")
-        _same(grad_y, ys, "grad_y")
-        ys, ld = _matrix(ys, "ys", self.nnz)
-        g, ldg = _matrix(grad_y, "grad_y", self.R.nrows)
-        H = ys.shape[1]
-        if g.shape[1] != H:
+        ys, ld, H, dt = self._rows_of(ys, self.nnz, "ys")
+        g, ldg, same, dtg = self._rows_of(grad_y, self.R.nrows, "grad_y")
+        if dtg != dt:
+            raise TypeError("grad_y must have the other matrix's type and device")
+        if same != H:
             raise ValueError("grad_y and ys differ in the length of their rows")
         out = torch.empty((self.nnz, H), dtype=ys.dtype, device=self.device)
         gvals = torch.empty(self.nnz, dtype=torch.float32, device=self.device)
         _abi.ws_routing_combine_backward(self._r, g.data_ptr(), ldg, ys.data_ptr(), ld, out.data_ptr(), H,
-                                         gvals.data_ptr(), H, dt, self._queue(ys))
+                                         gvals.data_ptr(), H, dt, self._queue())
         return out, gvals
 
-    def _product(self, xs: torch.Tensor, W: torch.Tensor) -> int:
-        dt = _dtype(xs, "xs")
-        if W.dim() != 3 or W.shape[0] != self.R.ncols:
-            raise ValueError(f"W must be {self.R.ncols} matrices, got {tuple(W.shape)}")
-        _same(W, xs, "W")
-        if xs.dim() != 2 or xs.shape[0] != self.nnz or xs.shape[1] != W.shape[2]:
-            raise ValueError(f"xs must be {self.nnz} rows of {W.shape[2]} values, got {tuple(xs.shape)}")
-        return dt
+    def _product(self, xs: torch.Tensor, W: torch.Tensor):
+        """(type, N, K) of a product."""
+        dt, stack, rows = _dtype(xs, "xs"), W.shape, xs.shape
+        if len(stack) != 3 or stack[0] != self.R.ncols:
+            raise ValueError(f"W must be {self.R.ncols} matrices, got {tuple(stack)}")
+        if W.dtype != xs.dtype or not W.get_device() == xs.get_device() == self._index:
+            raise TypeError("W and xs must have one type and be on the routing matrix's device")
+        _, N, K = stack
+        if len(rows) != 2 or rows[0] != self.nnz or rows[1] != K:
+            raise ValueError(f"xs must be {self.nnz} rows of {K} values, got {tuple(rows)}")
+        return dt, N, K
 
     def matmul(self, xs: torch.Tensor, W: torch.Tensor, stream=None) -> torch.Tensor:
         """ys[s] = W[e] xs[s] for the rows s of every column e: xs nnz x K in slot order, W E x N x K, bfloat16 or
         float16; products and sums in 32 bits, rounded once.  Rows behind the placed entries are left unwritten."""
         if stream is not None:
             return _elsewhere(self.matmul, stream, xs, W)
-        dt = self._product(xs, W)
-        _, N, K = W.shape
+        dt, N, K = self._product(xs, W)
         xs, ldx, _, a = _operand(xs)
         W, ldw, apart, b = _operand(W)
         out = torch.empty((self.nnz, N), dtype=xs.dtype, device=self.device)
         room, at = _room(a + b, self.device)
         _abi.ws_routing_matmul(self._r, xs.data_ptr(), ldx, W.data_ptr(), ldw, apart, N, K, out.data_ptr(), N, dt, at,
-                               a + b, self._queue(xs))
+                               a + b, self._queue())
         return out
 
     def matmul_backward(self, grad_ys: torch.Tensor, xs: torch.Tensor, W: torch.Tensor, stream=None):
@@ -290,8 +294,7 @@ class Routing:
         column without entries), in their types."""
         if stream is not None:
             return _elsewhere(self.matmul_backward, stream, grad_ys, xs, W)
-        dt = self._product(xs, W)
-        E, N, K = W.shape
+        (dt, N, K), E = self._product(xs, W), self.R.ncols
         _same(grad_ys, xs, "grad_ys")
         if grad_ys.dim() != 2 or grad_ys.shape[0] != self.nnz or grad_ys.shape[1] != N:
             raise ValueError(f"grad_ys must be {self.nnz} rows of {N} values, got {tuple(grad_ys.shape)}")
@@ -302,14 +305,14 @@ class Routing:
         gW = torch.empty((E, N, K), dtype=xs.dtype, device=self.device)
         room, at = _room(a + b + c, self.device)
         _abi.ws_routing_matmul_backward(self._r, g.data_ptr(), ldg, xs.data_ptr(), ldx, W.data_ptr(), ldw, apart, N, K,
-                                        gxs.data_ptr(), K, gW.data_ptr(), K, N * K, dt, at, a + b + c, self._queue(xs))
+                                        gxs.data_ptr(), K, gW.data_ptr(), K, N * K, dt, at, a + b + c, self._queue())
         return gxs, gW
 
     def wait(self, stream=None) -> None:
         """Waits for the stream and raises if a product's kernel gave up a wait since the plan was built."""
         if stream is not None:
             return _elsewhere(self.wait, stream)
-        self._queue(self._buf)
+        self._queue()
         torch.cuda.current_stream(self.device).synchronize()
         if int(self._buf[self.R.ncols + 1]) & 0xFFFFFFFF:
             raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
