@@ -157,10 +157,10 @@ class Routing:
         rowptr, colidx, vals = R.rowptr, R.colidx, R.vals
         if vals.dtype != torch.float32:
             raise TypeError(f"a routing matrix has float32 values, got {vals.dtype}")
-        if rowptr.dtype != torch.int64 or colidx.dtype != torch.int32 or \
-                not (rowptr.is_cuda and colidx.is_cuda and vals.is_cuda) or \
+        if rowptr.dtype != torch.int64 or colidx.dtype != torch.int32 or rowptr.get_device() < 0 or \
+                not rowptr.get_device() == colidx.get_device() == vals.get_device() or \
                 not (rowptr.is_contiguous() and colidx.is_contiguous() and vals.is_contiguous()):
-            raise TypeError("rowptr/colidx/vals must be contiguous CUDA int64/int32/float32 tensors")
+            raise TypeError("rowptr/colidx/vals must be contiguous int64/int32/float32 tensors on one GPU")
         nnz, T, E = colidx.numel(), R.nrows, R.ncols
         if rowptr.numel() != T + 1 or vals.numel() != nnz:
             raise ValueError("rowptr must have nrows + 1 entries, and every column index a value")
@@ -329,22 +329,22 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     """
     if stream is not None:
         return _elsewhere(adapters, stream, x, A, B, S, base, out, wait=wait)
-    dt = _dtype(x, "x")
+    dt, dtype, dev, index = _dtype(x, "x"), x.dtype, x.device, x.get_device()
     (La, r, K), (L, N, rb) = A.shape, B.shape
     if La != L or r != rb:
         raise ValueError(f"A must be L x r x K and B L x N x r, got {tuple(A.shape)} and {tuple(B.shape)}")
-    _same(A, x, "A")
-    _same(B, x, "B")
-    rowptr, colidx, vals, dev, T = S.rowptr, S.colidx, S.vals, x.device, S.nrows
+    if not A.dtype == B.dtype == dtype or not A.get_device() == B.get_device() == index:
+        raise TypeError("A and B must have x's type and device")
+    rowptr, colidx, vals, T, rows = S.rowptr, S.colidx, S.vals, S.nrows, x.shape
     if rowptr.dtype != torch.int64 or colidx.dtype != torch.int32 or vals.dtype != torch.float32 or \
             not (rowptr.is_contiguous() and colidx.is_contiguous() and vals.is_contiguous()) or \
-            not rowptr.device == colidx.device == vals.device == dev:
+            not rowptr.get_device() == colidx.get_device() == vals.get_device() == index:
         raise TypeError("S must hold contiguous int64/int32/float32 tensors on x's device")
     nnz = colidx.numel()
     if S.ncols != L or rowptr.numel() != T + 1 or vals.numel() != nnz:
-        raise ValueError(f"S must be {x.shape[0]} x {L} in CSR")
-    if x.dim() != 2 or x.shape[0] != T or x.shape[1] != K:
-        raise ValueError(f"x must be {T} rows of {K} values, got {tuple(x.shape)}")
+        raise ValueError(f"S must be {rows[0]} x {L} in CSR")
+    if len(rows) != 2 or rows[0] != T or rows[1] != K:
+        raise ValueError(f"x must be {T} rows of {K} values, got {tuple(rows)}")
     x, ldx, _, need = _operand(x)
     A, lda, apart, more = _operand(A)
     B, ldb, apartB, most = _operand(B)
@@ -353,12 +353,13 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     need = 16 + nnz * rank * 16 + (need + more + most if T * rank > 8192 else 0)
     ldbase = ldy = N
     if base is not None:
-        _same(base, x, "base")
+        if base.dtype != dtype or base.get_device() != index:
+            raise TypeError("base must have x's type and device")
         base, ldbase = _matrix(base, "base", T)
         if base.shape[1] != N:
             raise ValueError(f"base must be {T} x {N}")
     if out is None:
-        out = torch.empty((T, N), dtype=x.dtype, device=dev)
+        out = torch.empty((T, N), dtype=dtype, device=dev)
     else:
         _same(out, x, "out")
         same, ldy = _matrix(out, "out", T)
@@ -370,7 +371,7 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     call = _abi.ADAPTERS_CALL.pack(T, L, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), K, r, N,
                                    x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), ldb, apartB,
                                    0 if base is None else base.data_ptr(), ldbase, out.data_ptr(), ldy, dt)
-    _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(dev.index))
+    _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(index))
     if wait:
         torch.cuda.current_stream(dev).synchronize()
         if T * rank > 8192 and N > 0 and scratch[:4].view(torch.int32).item():
