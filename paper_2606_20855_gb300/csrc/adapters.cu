@@ -487,6 +487,7 @@ constexpr int kStepSplit = 4;
 template <bool half, bool vec>
 __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapters_call c, uint2* __restrict__ h, int rpad) {
   __shared__ float2 part[kAdWarps];
+  may_start_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int K = static_cast<int>(c.K), r = static_cast<int>(c.r), pairs = rpad / 2;
   int begin, end;
@@ -543,15 +544,22 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
 }
 
 // A thread per value of y: its row of B against v h, which every thread of the CTA reads.  Bound by latencies: 48 tokens of rank 16,
-// 4096 values, 6.3 MB of B: 5 us.
+// 4096 values, 6.3 MB of B: 5 us, of which what does not need h passes while the inner products run (four
+// tokens of 512 values, both kernels: 6.8 us without, 5.1 us with that).
 template <bool half>
-__global__ void __launch_bounds__(kAdThreads) expand_step_kernel(const ws_adapters_call c, const uint2* __restrict__ h, int rpad, bool vecB) {
+__global__ void __launch_bounds__(kAdThreads) expand_step_kernel(const ws_adapters_call c, const uint2* h, int rpad, bool vecB) {
   const int64_t n = static_cast<int64_t>(blockIdx.x) * kAdThreads + threadIdx.x, t = blockIdx.y;
   if (n >= c.N) return;
+  if (c.nnz == 0) wait_for_last();  // as in the tiles: another call may write base
   const int r = static_cast<int>(c.r);
   int begin, end;
   entry_range(c.rowptr, t, c.nnz, &begin, &end);
   float acc = c.base ? value16<half>(static_cast<const uint16_t*>(c.base)[t * c.ldbase + n]) : 0.0f;
+  if (begin < end) {
+    const int a = c.colidx[begin];
+    if (met(c, a)) asm volatile("prefetch.global.L1 [%0];" ::"l"(static_cast<const uint16_t*>(c.B) + a * c.strideB + n * c.ldb));
+  }
+  wait_for_last();  // the inner products
   for (int e = begin; e < end; ++e) {
     const int a = c.colidx[e];
     if (!met(c, a)) continue;
@@ -584,7 +592,9 @@ ws_status_t launch_step(const ws_adapters_call& c, uint2* h, cudaStream_t s) {
   const auto shrink = vec ? shrink_step_kernel<half, true> : shrink_step_kernel<half, false>;
   if (c.nnz > 0)
     shrink<<<dim3(T, static_cast<unsigned>(rpad / 2 / (kAdWarps / kStepSplit))), kAdThreads, 0, s>>>(c, h, rpad);
-  expand_step_kernel<half><<<dim3(static_cast<unsigned>((c.N + kAdThreads - 1) / kAdThreads), T), kAdThreads, 0, s>>>(c, h, rpad, vecB);
+  const dim3 grid(static_cast<unsigned>((c.N + kAdThreads - 1) / kAdThreads), T);
+  const cudaError_t e = launch_early(expand_step_kernel<half>, grid, kAdThreads, 0, s, 1, c, h, rpad, vecB);
+  if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
   return WS_OK;
 }
 

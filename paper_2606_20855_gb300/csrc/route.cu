@@ -64,9 +64,10 @@ __device__ __forceinline__ float key_value(uint32_t key) {
 // second k rounds: 30 us.
 template <typename T, int V>
 __global__ void __launch_bounds__(32 * kRouteWarps)
-    topk_route_kernel(const T* __restrict__ logits, int64_t rows, int cols, int64_t ld, bool vec, int k,
-                      bool normalize, int64_t* __restrict__ rowptr, int32_t* __restrict__ colidx,
-                      float* __restrict__ vals) {
+    topk_route_kernel(const T* logits, int64_t rows, int cols, int64_t ld, bool vec, int k, bool normalize, int64_t* rowptr,
+                      int32_t* colidx, float* vals) {
+  may_start_next();
+  wait_for_last();
   __shared__ uint2 cand[kRouteWarps][32];
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t row = static_cast<int64_t>(blockIdx.x) * kRouteWarps + warp;
@@ -179,9 +180,10 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
 // 65,537 rows of 256 (k = 8, float, 67 MB written): 17 us, the rate of a fill.
 template <typename T, int V>
 __global__ void __launch_bounds__(32 * kRouteWarps)
-    topk_route_backward_kernel(const T* __restrict__ logits, int64_t rows, int cols, int64_t ld, bool vec, int k,
-                               bool normalize, const int32_t* __restrict__ colidx, const float* __restrict__ vals,
-                               const float* __restrict__ gvals, T* __restrict__ glogits, int64_t ldg, bool vecg) {
+    topk_route_backward_kernel(const T* logits, int64_t rows, int cols, int64_t ld, bool vec, int k, bool normalize,
+                               const int32_t* colidx, const float* vals, const float* gvals, T* glogits, int64_t ldg, bool vecg) {
+  may_start_next();
+  wait_for_last();
   constexpr int N = V * sizeof(T) >= 16 ? 16 / sizeof(T) : V;
   __shared__ __align__(16) float lines[kRouteWarps][32 * V];
   const int lane = threadIdx.x & 31;
@@ -271,9 +273,8 @@ void launch_topk_route(const void* logits, int64_t rows, int cols, int64_t ld, w
     using T = decltype(t);
     for_values(cols, [&](auto v) {
       constexpr int V = decltype(v)::value;
-      topk_route_kernel<T, V><<<grid, 32 * kRouteWarps, 0, s>>>(static_cast<const T*>(logits), rows, cols, ld,
-                                                                packs(logits, ld, V, sizeof(T)), k, normalize, rowptr,
-                                                                colidx, vals);
+      launch_early(topk_route_kernel<T, V>, dim3(grid), 32 * kRouteWarps, 0, s, 1, static_cast<const T*>(logits), rows, cols, ld,
+                   packs(logits, ld, V, sizeof(T)), k, normalize, rowptr, colidx, vals);
     });
   });
 }
@@ -286,9 +287,9 @@ void launch_topk_route_backward(const void* logits, int64_t rows, int cols, int6
     using T = decltype(t);
     for_values(cols, [&](auto v) {
       constexpr int V = decltype(v)::value;
-      topk_route_backward_kernel<T, V><<<grid, 32 * kRouteWarps, 0, s>>>(
-          static_cast<const T*>(logits), rows, cols, ld, packs(logits, ld, V, sizeof(T)), k, normalize, colidx, vals,
-          gvals, static_cast<T*>(glogits), ldg, packs(glogits, ldg, V, sizeof(T)));
+      launch_early(topk_route_backward_kernel<T, V>, dim3(grid), 32 * kRouteWarps, 0, s, 1, static_cast<const T*>(logits), rows, cols, ld,
+                   packs(logits, ld, V, sizeof(T)), k, normalize, colidx, vals, gvals, static_cast<T*>(glogits), ldg,
+                   packs(glogits, ldg, V, sizeof(T)));
     });
   });
 }

@@ -173,7 +173,7 @@ class Routing:
         # one array: offsets, the status word, the scratch (at a multiple of 16 bytes); rows, entries and slots
         words = (E + 3) // 2 * 2
         self._lead = lead = words + scratch // 8
-        self._buf = torch.empty(lead + (3 * nnz + 1) // 2, dtype=torch.int64, device=self.device)
+        self._buf = torch.empty(2 * lead + 3 * nnz, dtype=torch.int32, device=self.device)
         at = self._buf.data_ptr()
         ints = at + 8 * lead
         self._c = _abi.WsRouting(T, E, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), at, ints,
@@ -181,24 +181,24 @@ class Routing:
         self._r = ctypes.byref(self._c)
         _abi.ws_routing_build(self._r, at + 8 * words, scratch, raw)
 
+    def _part(self, first: int, count: int) -> torch.Tensor:
+        return self._buf.as_strided((count,), (1,), first)  # the cheapest view on the host
+
     @property
     def offsets(self) -> torch.Tensor:
-        return self._buf[:self.R.ncols + 1]
-
-    def _part(self, i: int) -> torch.Tensor:
-        return self._buf[self._lead:].view(torch.int32)[i * self.nnz:(i + 1) * self.nnz]
+        return self._part(0, 2 * self.R.ncols + 2).view(torch.int64)
 
     @property
     def rows(self) -> torch.Tensor:
-        return self._part(0)
+        return self._part(2 * self._lead, self.nnz)
 
     @property
     def entries(self) -> torch.Tensor:
-        return self._part(1)
+        return self._part(2 * self._lead + self.nnz, self.nnz)
 
     @property
     def slots(self) -> torch.Tensor:
-        return self._part(2)
+        return self._part(2 * self._lead + 2 * self.nnz, self.nnz)
 
     def _rows_of(self, t: torch.Tensor, rows: int, name: str):
         """(t, its row stride, the length of its rows, their type), t being `rows` rows on the plan's device."""
@@ -314,7 +314,7 @@ class Routing:
             return _elsewhere(self.wait, stream)
         self._queue()
         torch.cuda.current_stream(self.device).synchronize()
-        if int(self._buf[self.R.ncols + 1]) & 0xFFFFFFFF:
+        if int(self._buf[2 * (self.R.ncols + 1)]):
             raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
 
 
