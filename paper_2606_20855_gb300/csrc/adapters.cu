@@ -303,7 +303,7 @@ __device__ __noinline__ float added(const ws_adapters_call& c, const float* h, i
 template <bool half>
 __global__ void __launch_bounds__(kExpandThreads, 2)
     expand_tile_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_base,
-                       const __grid_constant__ CUtensorMap map_y, const ws_adapters_call c, const float* __restrict__ h,
+                       const __grid_constant__ CUtensorMap map_y, const ws_adapters_call c, const float* h,
                        int rpad, int split, bool copies, int* status) {
   extern __shared__ uint8_t raw[];
   __shared__ __align__(8) uint64_t base_bar, b_bar, m_bar;
@@ -340,7 +340,6 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   const uint32_t tmem = tmem_slot;
   const uint32_t idesc = instr_desc(half, false, false, kTok, kExpandN);
 
-  wait_for_last();  // the inner products
   int done = 0;        // products of 32 ranks
   bool mixed = false;  // some token does not have some adapter of the tile
   for (;;) {
@@ -359,6 +358,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
         bar_expect(smem_u32(&b_bar), kExpandB);
         tma_3d(sb, &map_b, r0, n0, a, smem_u32(&b_bar));
       }
+      if (done == 0) wait_for_last();  // the inner products
       // v h of 128 tokens, four ranks a thread and turn, neighbouring threads along a token's ranks; all loads in flight at once
       const int log_quads = ranks == kExpandRanks ? 3 : 2;
       constexpr int kTurns = kTok * (kExpandRanks / 4) / kExpandThreads;
@@ -402,6 +402,7 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
     }
     if (mine) w.next(c);
   }
+  if (done == 0) wait_for_last();  // the kernel ends after the one before
   // Without the copy engine (rows that do not start at multiples of 16 bytes) the warps move base and y along their rows.
   const auto place = [&](int row, int col) { return sy + (col >> 6) * kExpandY + row * 128 + ((((col & 63) >> 3) ^ (row & 7)) << 4) + 2 * (col & 7); };
   const int columns = min(kExpandN, N - n0);
@@ -423,42 +424,49 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   if (!dead) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-    for (int j = side * (kExpandN / 2); j < (side + 1) * (kExpandN / 2); j += 16) {
-      const int left = N - n0 - j;
-      if (left <= 0) break;
-      float f[16] = {};
-      __syncwarp();
-      if (done > 0) tmem_load16(tmem + j + (static_cast<uint32_t>((warp & 3) * 32) << 16), f);
-      if (mixed && there) {
-        // A token without an adapter got zero times its values: nothing, unless those are infinite or NaN.
-        for (int i = 0; i < 16; ++i)
-          if (i < left && !(fabsf(f[i]) <= 3.4e38f)) f[i] = added<half>(c, h, rpad, split, t, n0 + j + i);
+    for (int q = 2 * side; q < 2 * side + 2 && q < pieces; ++q) {  // 64 columns, stored as soon as they are there
+#pragma unroll 1
+      for (int j = 64 * q; j < 64 * q + 64; j += 16) {
+        const int left = N - n0 - j;
+        if (left <= 0) break;
+        float f[16] = {};
+        __syncwarp();
+        if (done > 0) tmem_load16(tmem + j + (static_cast<uint32_t>((warp & 3) * 32) << 16), f);
+        if (mixed && there) {
+          // A token without an adapter got zero times its values: nothing, unless those are infinite or NaN.
+          for (int i = 0; i < 16; ++i)
+            if (i < left && !(fabsf(f[i]) <= 3.4e38f)) f[i] = added<half>(c, h, rpad, split, t, n0 + j + i);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint32_t at = place(m, j + 8 * s);
+          uint32_t b[4] = {};
+          if (c.base)
+            asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at) : "memory");
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            b[i] = pair16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i],
+                                value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1]);
+          asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
+        }
       }
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const uint32_t at = place(m, j + 8 * s);
-        uint32_t b[4] = {};
-        if (c.base)
-          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at) : "memory");
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          b[i] = pair16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i],
-                              value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1]);
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
+      if (copies) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        asm volatile("bar.sync %0, %1;" ::"r"(1 + side), "r"(kTok) : "memory");  // the side's threads
+        if (m == 0) {
+          tma_store_2d(&map_y, sy + q * kExpandY, n0 + 64 * q, static_cast<int>(t0));
+          asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+        }
       }
     }
+    if (copies && m == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
   }
-  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
   __syncwarp();
   __syncthreads();
   if (threadIdx.x == 0 && dead) {  // no copy and no product may be in flight when the CTA leaves
     atomicOr(status, 1);
     if (done > 0) bar_wait_short(smem_u32(&b_bar), (done - 1) & 1), bar_wait_short(smem_u32(&m_bar), (done - 1) & 1);
     if (copies && c.base) bar_wait_short(smem_u32(&base_bar), 0);
-  } else if (threadIdx.x == 0 && copies) {
-    for (int i = 0; i < pieces; ++i) tma_store_2d(&map_y, sy + i * kExpandY, n0 + 64 * i, static_cast<int>(t0));
-    asm volatile("cp.async.bulk.commit_group;" ::: "memory");
-    asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
   }
   if (!copies && !dead) {
     uint16_t* dst = static_cast<uint16_t*>(c.y) + t0 * c.ldy + n0;
