@@ -50,7 +50,7 @@ struct GroupedParams {
   int64_t ldo;   // values between rows of the result
   int64_t group_stride;  // kRowsSum: values between gW[e]
   bool half;
-  int vec;       // rows of the result start at multiples of so many bytes: 16, 8, 4 or 2
+  int vec;       // rows of the result start at multiples of so many bytes: 16 (the copy engine may store them), 8, 4 or 2
   int* status;
 };
 
@@ -71,6 +71,10 @@ struct Tile {
 template <int kRows>
 constexpr int kThreadsOf = kRows == kRowsSum ? 224 : 192;
 
+// Pieces of shared memory through which a storing warp's results go.
+template <int kRows>
+constexpr int kPieces = kRows == kRowsN ? 0 : kRows == kRowsM ? 1 : 2;
+
 // Rows of a group in a tile, unless they are summed over.
 template <int BN, int kRows>
 constexpr int kRowTileOf = kRows == kRowsM ? kTileM : BN;
@@ -81,7 +85,7 @@ struct Shape {
   static constexpr int kStageBytes = kBytesA + kBytesB;
   static constexpr int kStages = (196 * 1024) / kStageBytes > 10 ? 10 : (196 * 1024) / kStageBytes;
   static constexpr int kAccCols = 2 * BN < 32 ? 32 : 2 * BN;  // a power of two
-  static constexpr size_t kSmem = static_cast<size_t>(kStages) * kStageBytes + (kRows == kRowsN ? 0 : 4 * kTurnBytes) + 1024;
+  static constexpr size_t kSmem = static_cast<size_t>(kStages) * kStageBytes + 4 * kPieces<kRows> * kTurnBytes + 1024;
 };
 
 // Tile t of the sequence that all roles of all CTAs share.  first[e]: row tiles of the groups before e.  kPair: t is two
@@ -132,17 +136,17 @@ __device__ __forceinline__ bool tile_at(const GroupedParams& p, const int* first
   return true;
 }
 
-// Stores 64 values (from column 0 of dst on, `left` of them inside the result) of a warp's 32 rows; on(row): the row is stored.
-// They go through shared memory, a row of 128 bytes a lane, its 16-byte pieces placed by the row's last three bits, so that lanes
-// that write rows and lanes that read along them meet no bank twice.  A lane's own row would be 32 rows a store; turned, a store
-// covers four rows of 128 bytes (or, where rows are not 16-byte aligned, one row).  64 experts' gradients of 1024 x 2048 from 40
-// rows each, 268 MB written: 138 us with the values converted one by one, 91 us two at a time; a fill of the same memory takes 72
-// us.  Eight warps that store instead of four, each half of the columns: 96 us.
-template <typename On>
-__device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t turn, uint16_t* dst, const float (&f)[64], int left, On on) {
+// Results leave a warp by 32 rows of 64 values, through 4 KB of shared memory: a row of 128 bytes a lane, its 16-byte pieces placed
+// by the row's last three bits (the copy engine's 128-byte swizzle), so that lanes that write rows and lanes that read along them
+// meet no bank twice.  From there the copy engine stores all 32 rows at once, where they start at multiples of 16 bytes and all are
+// stored, while the warp turns to the next 64 columns in the other of two such pieces; else the warp stores along rows.  64 experts'
+// gradients of 1024 x 2048 from 40 rows each, 268 MB written (40 us at the copy rate): 55 us, stored along rows 91 us (138 us with the
+// values converted one by one, 96 us with eight warps, each half of the columns).  Where the experts' rows are the result's, one piece has
+// to do, as the row tiles of all experts are counted in shared memory too.
+__device__ __forceinline__ void put_rows(uint32_t turn, bool half, const float (&f)[64]) {
   const int lane = threadIdx.x & 31;
   uint32_t all[32];
-  if (p.half) {
+  if (half) {
 #pragma unroll
     for (int i = 0; i < 32; ++i) all[i] = pair16<true>(f[2 * i], f[2 * i + 1]);
   } else {
@@ -156,6 +160,12 @@ __device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t tu
                  "r"(w[2]), "r"(w[3])
                  : "memory");
   }
+}
+
+// Stores what put_rows left (from column 0 of dst on, `left` columns of them inside the result); on(row): the row is stored.
+template <typename On>
+__device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t turn, uint16_t* dst, int left, On on) {
+  const int lane = threadIdx.x & 31;
   __syncwarp();
   // B bytes a lane: 16, 8, 4 or 2, as the rows of the result start
   const auto along = [&](auto bytes) {
@@ -210,7 +220,7 @@ __device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t tu
 template <int BN, int kRows, bool kWMN, bool kPair>
 __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
     grouped_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                   const GroupedParams p) {
+                   const __grid_constant__ CUtensorMap map_out, const GroupedParams p) {
   using S = Shape<BN, kRows, kPair>;
   constexpr bool kAMN = kRows == kRowsSum || (kRows == kRowsN && kWMN);
   constexpr bool kBMN = kRows == kRowsSum || (kRows == kRowsM && kWMN);
@@ -425,6 +435,7 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
     bool ok = true;
     Tile t;
     uint16_t* const result = static_cast<uint16_t*>(p.out);
+    int turns = 0;  // the piece that is next
     for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
       if (t.steps > 0) {
         ok = bar_wait_warp(smem_u32(&acc_full[acc]), acc_phase, &dead);
@@ -448,9 +459,10 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
           }
         }
       } else {
-        const uint32_t turn = base + S::kStages * S::kStageBytes + quarter * kTurnBytes;
+        const uint32_t turn0 = base + S::kStages * S::kStageBytes + kPieces<kRows> * quarter * kTurnBytes;
         const int columns = kRows == kRowsM ? p.features : p.width;
         const int lines = (kRows == kRowsM ? t.rows : p.features - t.m0) - quarter * 32;  // rows of the warp that are stored
+        const bool engine = p.vec == 16 && (kRows == kRowsSum || lines >= 32);
         uint16_t* const to = kRows == kRowsM ? result + (static_cast<int64_t>(t.row0) + quarter * 32) * p.ldo + t.n0
                                              : result + t.group * p.group_stride + (static_cast<int64_t>(t.m0) + quarter * 32) * p.ldo + t.n0;
 #pragma unroll 1
@@ -459,7 +471,23 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
           if (left <= 0 || lines <= 0) break;
           float f[64] = {};
           if (t.steps > 0) tmem_load64(addr + c, f);
-          store_turned(p, turn, to + c, f, left, [&](int row) { return row < lines; });
+          // the piece is free: at most the other one's store still reads
+          if (lane == 0) asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(kPieces<kRows> - 1) : "memory");
+          __syncwarp();
+          const uint32_t turn = turn0 + turns * kTurnBytes;
+          if (++turns == kPieces<kRows>) turns = 0;
+          put_rows(turn, p.half, f);
+          if (engine) {
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              if constexpr (kRows == kRowsSum) tma_store_3d(&map_out, turn, t.n0 + c, t.m0 + quarter * 32, t.group);
+              else tma_store_2d(&map_out, turn, t.n0 + c, t.row0 + quarter * 32);
+              asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
+          } else {
+            store_turned(p, turn, to + c, left, [&](int row) { return row < lines; });
+          }
         }
       }
       if (t.steps > 0) {
@@ -472,6 +500,7 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
         if (++acc == 2) acc = 0, acc_phase ^= 1;
       }
     }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
   }
   __syncwarp();
   __syncthreads();
@@ -584,7 +613,7 @@ cudaError_t launch_thin(const GroupedRows& g, cudaStream_t s) {
 // ---------------------------------------------------------------- host
 
 template <int BN, int kRows, bool kWMN, bool kPair = false>
-cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const GroupedParams& p, int64_t tiles, int num_sms,
+cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const CUtensorMap& out, const GroupedParams& p, int64_t tiles, int num_sms,
                    cudaStream_t s) {
   using S = Shape<BN, kRows, kPair>;
   const auto kernel = grouped_kernel<BN, kRows, kWMN, kPair>;
@@ -593,7 +622,7 @@ cudaError_t launch(const CUtensorMap& a, const CUtensorMap& b, const GroupedPara
   if (e != cudaSuccess) return e;
   const int64_t teams = kPair ? num_sms / 2 : num_sms;
   const unsigned grid = static_cast<unsigned>((tiles < teams ? tiles : teams) * (kPair ? 2 : 1));
-  return launch_early(kernel, dim3(grid), kThreadsOf<kRows>, S::kSmem, s, kPair ? 2 : 1, a, b, p);
+  return launch_early(kernel, dim3(grid), kThreadsOf<kRows>, S::kSmem, s, kPair ? 2 : 1, a, b, out, p);
 }
 
 int64_t up(int64_t x, int64_t y) { return (x + y - 1) / y; }
@@ -614,7 +643,8 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
   p.half = g.half;
   p.vec = row_alignment(reinterpret_cast<uintptr_t>(g.out) | static_cast<uint64_t>(g.ldo * 2));
   p.status = g.r->status;
-  CUtensorMap x, w;
+  CUtensorMap x, w, out{};
+  if (p.vec == 16 && !encode(&out, g.out, g.half, features, g.r->nnz, g.ldo, 0, 0, 32)) p.vec = 8;
   const int64_t met = g.r->nnz < g.r->ncols ? g.r->nnz : g.r->ncols;  // groups that can have rows
   const double mean = static_cast<double>(g.r->nnz) / static_cast<double>(g.r->ncols);
   const auto run = [&](auto bn, auto side, auto pair) {
@@ -626,7 +656,7 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
                encode(&w, g.w, g.half, g.K, g.N, g.ldw, g.r->ncols, g.group_stride, kWMN ? 64 : kPair ? kFeat / 2 : kFeat);
     if (!*encoded) return cudaSuccess;
     const int64_t tiles = (g.r->nnz / (kPair ? 2 * kRowTile : kRowTile) + met) * up(features, kFeat);
-    return launch<BN, kRows, kWMN, kPair>(kRows == kRowsM ? x : w, kRows == kRowsM ? w : x, p, tiles, num_sms, s);
+    return launch<BN, kRows, kWMN, kPair>(kRows == kRowsM ? x : w, kRows == kRowsM ? w : x, out, p, tiles, num_sms, s);
   };
   using std::integral_constant;
   // Few rows an expert: W's features fill the 128 lanes and the rows are the short side.
@@ -675,7 +705,8 @@ ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_
   p.half = g.half;
   p.vec = row_alignment(reinterpret_cast<uintptr_t>(g.out) | static_cast<uint64_t>(g.ldo * 2) | static_cast<uint64_t>(g.group_stride * 2));
   p.status = g.r->status;
-  CUtensorMap a, b;
+  CUtensorMap a, b, out{};
+  if (p.vec == 16 && !encode(&out, g.out, g.half, g.K, g.N, g.ldo, g.r->ncols, g.group_stride, 32)) p.vec = 8;
   if (!encode(&a, gys, g.half, g.N, g.r->nnz, ldgys, 0, 0, 64) || !encode(&b, g.x, g.half, g.K, g.r->nnz, g.ldx, 0, 0, 64))
     return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
   const int64_t wide = g.r->ncols * up(g.N, kTileM) * up(g.K, 256);
@@ -683,10 +714,10 @@ ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_
   const bool paired = static_cast<double>(g.r->nnz) >= kPairRows * static_cast<double>(g.r->ncols) && pairs >= num_sms / 2 &&
                       up(g.N, kTileM) % 2 == 0;
   const cudaError_t e = paired
-                            ? launch<256, kRowsSum, false, true>(a, b, p, pairs, num_sms, s)
+                            ? launch<256, kRowsSum, false, true>(a, b, out, p, pairs, num_sms, s)
                         : wide >= num_sms
-                            ? launch<256, kRowsSum, false>(a, b, p, wide, num_sms, s)
-                            : launch<128, kRowsSum, false>(a, b, p, g.r->ncols * up(g.N, kTileM) * up(g.K, 128), num_sms, s);
+                            ? launch<256, kRowsSum, false>(a, b, out, p, wide, num_sms, s)
+                            : launch<128, kRowsSum, false>(a, b, out, p, g.r->ncols * up(g.N, kTileM) * up(g.K, 128), num_sms, s);
   return e == cudaSuccess ? WS_OK : routing_fail(WS_ERR_CUDA, "grouped product: %s", cudaGetErrorString(e));
 }
 

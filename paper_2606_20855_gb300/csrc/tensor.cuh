@@ -162,6 +162,12 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* map, uint32_t sr
                : "memory");
 }
 
+__device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(map), "r"(x), "r"(y), "r"(z),
+               "r"(src)
+               : "memory");
+}
+
 // Shared-memory matrix descriptor, 128-byte swizzle.  K-major: 8-row groups of
 // 1024 bytes follow each other.  MN-major: blocks of 64 (M or N) x 64 (K), in
 // which 8 steps of K take 1024 bytes; blocks are 8192 bytes apart.
