@@ -177,7 +177,8 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
 
 // A warp per row: the softmax again (not kept from the choice: a row of logits is read faster than weights of all columns are
 // stored), the chosen columns put over it in shared memory, every value of the row stored once, in packs.  Bound by the store:
-// 65,537 rows of 256 (k = 8, float, 67 MB written): 17 us, the rate of a fill.
+// 65,537 rows of 256 (k = 8, float, 67 MB written, 10 us at the copy rate): 13.5 us; 17 us with a lane's values stored side by side
+// (half sectors), and as long with four rows a warp.
 template <typename T, int V>
 __global__ void __launch_bounds__(32 * kRouteWarps)
     topk_route_backward_kernel(const T* logits, int64_t rows, int cols, int64_t ld, bool vec, int k, bool normalize,
@@ -226,16 +227,17 @@ __global__ void __launch_bounds__(32 * kRouteWarps)
   if (static_cast<unsigned>(col) < static_cast<unsigned>(cols)) line[col] = v * (g - a);
   __syncwarp();
   T* dst = glogits + row * ldg;
-  if (vecg && lane * V + V <= cols) {
+  if (vecg) {  // neighbouring lanes store neighbouring packs
 #pragma unroll
-    for (int i = 0; i < V; i += N) {
+    for (int c = 0; c < V / N; ++c) {
+      const int at = (32 * c + lane) * N;
       float part[N];
 #pragma unroll
-      for (int j = 0; j < N; ++j) part[j] = line[lane * V + i + j];
-      *reinterpret_cast<Pack<T, N>*>(dst + lane * V + i) = pack<T, N>(part);
+      for (int j = 0; j < N; ++j) part[j] = line[at + j];
+      if (at + N <= cols) *reinterpret_cast<Pack<T, N>*>(dst + at) = pack<T, N>(part);
+      else
+        for (int j = at; j < cols; ++j) dst[j] = from_f32<T>(line[j]);
     }
-  } else if (vecg) {
-    for (int i = lane * V; i < cols; ++i) dst[i] = from_f32<T>(line[i]);  // the row's last lane, and none after it
   } else {
     for (int i = lane; i < cols; i += 32) dst[i] = from_f32<T>(line[i]);
   }
