@@ -209,13 +209,24 @@ __device__ __forceinline__ void store_turned(const GroupedParams& p, uint32_t tu
   __syncwarp();
 }
 
+// Where rows are summed, a tile's last stage is fetched first and multiplied kAhead stages later than that place in the ring, so that its
+// rows behind the group's last are cleared by then.  32 experts' gradients of 2048 x 2048 from about 1024 rows each: 177 us, 199 us in
+// order (three stages later 178 us; 164-167 us where no stage is partly filled).
+constexpr int kAhead = 2;
+template <int kRows>
+__device__ __forceinline__ bool tail_first(const Tile& t) {
+  return kRows == kRowsSum && t.rows % kTileK != 0 && t.steps > kAhead;
+}
+// How far from its turn's place in the ring the stage of turn i lies.
+__device__ __forceinline__ int ring_shift(bool tail_is_first, int i) { return !tail_is_first || i > kAhead ? 0 : i == kAhead ? -kAhead : 1; }
+
 // a: the M side's operand (kRowsM: the experts' rows, kRowsN: W, kRowsSum: gys), b: the N side's.
 // kWMN: W's contraction index runs along its rows (MN-major).
 // kPair: two CTAs, whose tiles lie one below the other, multiply as one (256 x 256): each holds its 128 rows of the M side and half of
 // the N side, so that a stage takes 32 KB of shared memory and of the way from L2 instead of 48, and six stages fit where four did.
 // Rank 0 issues the products and counts both CTAs' bytes at its barriers (rank 1 counting its own and telling rank 0 cost a microsecond a
 // stage).  8198 rows of eight experts, 2048 -> 8192: 170 us, 1620 TFLOP/s (about 200 us in a loop, at the power limit); 32768 rows of 32
-// experts, 2048 x 2048: 166 us, 165 us for the rows' gradient and 193 us for the matrices' (about 615 us in a loop).  Before the steps
+// experts, 2048 x 2048: 166 us, 165 us for the rows' gradient and 177 us for the matrices' (about 615 us in a loop).  Before the steps
 // that followed, the loops took 206 and 653 us with pairs, 214 and 665 us without.
 template <int BN, int kRows, bool kWMN, bool kPair>
 __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
@@ -284,7 +295,9 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
       bool ok = true, ready = false;  // ready: the stage is known to be empty
       Tile t;
       for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
-        for (int k = 0; k < t.steps; ++k) {
+        const bool swapped = tail_first<kRows>(t);
+        for (int turn = 0; turn < t.steps; ++turn) {
+          const int k = !swapped ? turn : turn == 0 ? t.steps - 1 : turn - 1;
           if (!ready && !bar_wait(smem_u32(&empty_bar[stage]), phase ^ 1, &dead)) {
             ok = false;
             break;
@@ -364,31 +377,42 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
         if (t.steps == 0) continue;
         ok = bar_wait<kPair>(smem_u32(&acc_empty[acc]), acc_phase ^ 1, &dead);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (int k = 0; ok && k < t.steps; ++k) {
-          const uint32_t sa = base + stage * S::kStageBytes, sb = sa + kBytesA;
+        const bool swapped = tail_first<kRows>(t);
+        if (swapped) ready = false;  // the stage that was asked for is the last one's
+        for (int turn = 0; ok && turn < t.steps; ++turn) {
           const int next = stage + 1 == S::kStages ? 0 : stage + 1;
           const uint32_t next_phase = next == 0 ? phase ^ 1 : phase;
-          const int rows = kRows == kRowsSum ? t.rows - k * kTileK : kTileK;  // in the stage, or more
-          if (kRows == kRowsSum && rows < kTileK) {
-            ok = bar_wait<kPair>(smem_u32(&clear_bar[stage]), cleared >> stage & 1, &dead);
-            cleared ^= 1u << stage;
+          const auto shifted = [&](int from, uint32_t from_phase, int by, uint32_t* its_phase) {
+            const int at = from + by;
+            *its_phase = at >= S::kStages || at < 0 ? from_phase ^ 1 : from_phase;
+            return at >= S::kStages ? at - S::kStages : at < 0 ? at + S::kStages : at;
+          };
+          uint32_t use_phase, ask_phase;
+          const int use = shifted(stage, phase, ring_shift(swapped, turn), &use_phase);
+          const int ask = shifted(next, next_phase, turn + 1 < t.steps ? ring_shift(swapped, turn + 1) : 0, &ask_phase);
+          const bool tail = swapped ? turn == kAhead : kRows == kRowsSum && t.rows - turn * kTileK < kTileK;
+          const int rows = tail ? t.rows % kTileK : kTileK;  // in the stage
+          const uint32_t sa = base + use * S::kStageBytes, sb = sa + kBytesA;
+          if (kRows == kRowsSum && tail) {
+            ok = bar_wait<kPair>(smem_u32(&clear_bar[use]), cleared >> use & 1, &dead);
+            cleared ^= 1u << use;
           } else if (!ready) {
-            ok = bar_wait(smem_u32(&full_bar[stage]), phase, &dead);
+            ok = bar_wait(smem_u32(&full_bar[use]), use_phase, &dead);
           }
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          ready = bar_ask(smem_u32(&full_bar[next]), next_phase);
+          ready = bar_ask(smem_u32(&full_bar[ask]), ask_phase);
           const uint64_t da = smem_desc(sa, kAMN), db = smem_desc(sb, kBMN);
 #pragma unroll
           for (int j = 0; j < kTileK / 16; ++j) {
             if (kRows == kRowsSum && 16 * j >= rows) break;
             const uint64_t a = da + j * (kAMN ? 2048 >> 4 : 32 >> 4), b = db + j * (kBMN ? 2048 >> 4 : 32 >> 4);
-            if constexpr (kPair) mma_f16_pair(tmem + acc * BN, a, b, idesc, k > 0 || j > 0);
-            else mma_f16(tmem + acc * BN, a, b, idesc, k > 0 || j > 0);
+            if constexpr (kPair) mma_f16_pair(tmem + acc * BN, a, b, idesc, turn > 0 || j > 0);
+            else mma_f16(tmem + acc * BN, a, b, idesc, turn > 0 || j > 0);
           }
-          if constexpr (kPair) mma_commit_pair(smem_u32(&empty_bar[stage]));
-          else mma_commit(smem_u32(&empty_bar[stage]));
-          if (k == t.steps - 1) {
+          if constexpr (kPair) mma_commit_pair(smem_u32(&empty_bar[use]));
+          else mma_commit(smem_u32(&empty_bar[use]));
+          if (turn == t.steps - 1) {
             if constexpr (kPair) mma_commit_pair(smem_u32(&acc_full[acc]));
             else mma_commit(smem_u32(&acc_full[acc]));
           }
@@ -410,10 +434,11 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
     bool ok = true;
     Tile t;
     for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
+      const int64_t at_stage = tail_first<kRows>(t) ? steps : steps + t.steps - 1;
       steps += t.steps;
       const int rows = t.rows - (t.steps - 1) * kTileK;
       if (t.steps == 0 || rows == kTileK) continue;
-      const int stage = static_cast<int>((steps - 1) % S::kStages);
+      const int stage = static_cast<int>(at_stage % S::kStages);
       ok = bar_wait_warp(smem_u32(&tail_bar[stage]), cleared >> stage & 1, &dead);
       if (!ok) break;
       const uint32_t at = base + stage * S::kStageBytes;
