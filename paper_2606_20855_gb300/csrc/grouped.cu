@@ -225,8 +225,8 @@ __device__ __forceinline__ int ring_shift(bool tail_is_first, int i) { return !t
 // kPair: two CTAs, whose tiles lie one below the other, multiply as one (256 x 256): each holds its 128 rows of the M side and half of
 // the N side, so that a stage takes 32 KB of shared memory and of the way from L2 instead of 48, and six stages fit where four did.
 // Rank 0 issues the products and counts both CTAs' bytes at its barriers (rank 1 counting its own and telling rank 0 cost a microsecond a
-// stage).  8198 rows of eight experts, 2048 -> 8192: 170 us, 1620 TFLOP/s (about 200 us in a loop, at the power limit); 32768 rows of 32
-// experts, 2048 x 2048: 166 us, 165 us for the rows' gradient and 177 us for the matrices' (about 615 us in a loop).  Before the steps
+// stage).  8198 rows of eight experts, 2048 -> 8192: 169 us, 1630 TFLOP/s (about 200 us in a loop, at the power limit); 32768 rows of 32
+// experts, 2048 x 2048: 167 us, 167 us for the rows' gradient and 179 us for the matrices' (about 620 us in a loop).  Before the steps
 // that followed, the loops took 206 and 653 us with pairs, 214 and 665 us without.
 template <int BN, int kRows, bool kWMN, bool kPair>
 __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
