@@ -371,7 +371,9 @@ ws_status_t ws_rowptr_scan_static(int64_t* rowptr, int64_t nrows, ws_stream_t st
  * the number of dense rows <= INT32_MAX, rows of at most 2^24 values.
  * Entries whose column is not in [0, ncols) take no part: they have slot -1 and
  * gradient 0, and the slots they leave over come last and hold zero rows.
- * rowptr is read within [0, nnz] whatever it holds.
+ * rowptr is read within [0, nnz] whatever it holds: where it decreases results
+ * are unspecified, but nothing outside the arrays is read or written, and
+ * offsets never exceed nnz.
  *
  * ws_topk_route -- R from logits (rows x cols, float, bfloat16 or half): row i
  * holds the k largest logits of row i (ties to the lowest column), by

@@ -89,6 +89,10 @@ __device__ __forceinline__ void mark_rows(const ws_routing& r, WarpRows& w, int 
   }
 }
 
+// Where entries are counted from: a + b, at most the number of entries.  Row pointers that decrease make warps whose ranges overlap,
+// which count entries more than once; slots from nnz on are then nobody's, and offsets end at nnz.
+__device__ __forceinline__ int slots_before(const ws_routing& r, int64_t a, int64_t b) { return static_cast<int>(min(a + b, r.nnz)); }
+
 // Slots of the warp's rows; pre[warp * cols + e] plus first[e] is the slot of the warp's first entry of column e.  staged: what
 // goes to the slots' arrays is kept there (row and entry, 16 bits each) instead.
 __device__ __forceinline__ void place_rows(const ws_routing& r, WarpRows& w, int cols, const uint32_t* mask,
@@ -104,8 +108,11 @@ __device__ __forceinline__ void place_rows(const ws_routing& r, WarpRows& w, int
       const int col = w.col[i];
       int slot = -1;
       if (static_cast<unsigned>(col) < static_cast<unsigned>(cols)) {
-        slot = first[col] + pre[warp * cols + col] + __popc(mask[warp * cols + col] & ((1u << w.row[i]) - 1u));
-        if (staged) {
+        const uint32_t at = static_cast<uint32_t>(first[col]) + pre[warp * cols + col] +
+                            __popc(mask[warp * cols + col] & ((1u << w.row[i]) - 1u));
+        if (at < static_cast<uint32_t>(r.nnz)) slot = static_cast<int>(at);
+        if (slot < 0) {  // counted more than once
+        } else if (staged) {
           staged[slot] = static_cast<uint32_t>(w.first + w.row[i]) << 16 | static_cast<uint32_t>(e);
         } else {
           r.rows[slot] = static_cast<int32_t>(w.first + w.row[i]);
@@ -126,19 +133,19 @@ __device__ __forceinline__ void clear_words(uint32_t* p, int words) {
   }
 }
 
-// total[e] (shared) becomes the first slot of column e; returns the number of placed entries.
-__device__ __forceinline__ int scan_columns(int cols, int* total, int* scratch) {
-  int sum = 0;
+// total[e] (shared; at most one a row) becomes the first slot of column e; returns the number of placed entries.
+__device__ __forceinline__ int scan_columns(const ws_routing& r, int cols, int* total, int64_t* scratch) {
+  int64_t sum = 0;
   for (int e0 = 0; e0 < cols; e0 += blockDim.x) {
     const int e = e0 + threadIdx.x;
-    const int n = e < cols ? total[e] : 0;
-    int all = 0;
-    const int before = block_exclusive_scan(n, scratch, &all);
-    if (e < cols) total[e] = sum + before;
+    const int64_t n = e < cols ? total[e] : 0;
+    int64_t all = 0;
+    const int64_t before = block_exclusive_scan(n, scratch, &all);
+    if (e < cols) total[e] = slots_before(r, sum, before);
     sum += all;
   }
   __syncthreads();
-  return sum;
+  return slots_before(r, sum, 0);
 }
 
 // Offsets of all columns, and -1 in the slots that entries of no column leave over.
@@ -171,7 +178,7 @@ size_t build_smem(int cols, int W) { return static_cast<size_t>(cols) * (W * 4 +
 __global__ void __launch_bounds__(32 * kSmallWarps) routing_small_kernel(ws_routing r, int cols, bool stage) {
   const int warps = blockDim.x >> 5;
   extern __shared__ __align__(16) int sm[];
-  __shared__ int scratch[32];
+  __shared__ int64_t scratch[32];
   may_start_next();
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
   int* first = sm + warps * cols;
@@ -184,7 +191,7 @@ __global__ void __launch_bounds__(32 * kSmallWarps) routing_small_kernel(ws_rout
   __syncthreads();
   for (int e = threadIdx.x; e < cols; e += blockDim.x) first[e] = count_column(mask, pre, cols, e, warps);
   __syncthreads();
-  const int placed = scan_columns(cols, first, scratch);
+  const int placed = scan_columns(r, cols, first, scratch);
   write_offsets(r, cols, first, placed);
   uint32_t* const staged = stage ? reinterpret_cast<uint32_t*>(pre + ((warps * cols + 1) & ~1)) : nullptr;
   place_rows(r, w, cols, mask, pre, first, staged);
@@ -230,7 +237,7 @@ template <int W>
 __global__ void __launch_bounds__(32 * W) routing_place_kernel(ws_routing r, int cols, int64_t chunk,
                                                                const int32_t* counts) {
   extern __shared__ __align__(16) int sm[];
-  __shared__ int scratch[32];
+  __shared__ int64_t scratch[32];
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
   int* next = sm + W * cols;            // first slot of the tile in every column
   int* before = next + cols;            // entries of the chunks before this one
@@ -264,18 +271,18 @@ __global__ void __launch_bounds__(32 * W) routing_place_kernel(ws_routing r, int
       }
   }
   __syncthreads();
-  const int placed = scan_columns(cols, next, scratch);
+  const int placed = scan_columns(r, cols, next, scratch);
   if (blockIdx.x == 0) write_offsets(r, cols, next, placed);
   __syncthreads();
   for (int e = threadIdx.x; e < cols; e += blockDim.x) {
-    next[e] += before[e];
+    next[e] = slots_before(r, next[e], before[e]);
     before[e] = count_column(mask, pre, cols, e, W);
   }
   __syncthreads();
   place_rows(r, w, cols, mask, pre, next);
   for (int64_t row0 = begin + 32 * W; row0 < end; row0 += 32 * W) {
     __syncthreads();
-    for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] += before[e];
+    for (int e = threadIdx.x; e < cols; e += blockDim.x) next[e] = slots_before(r, next[e], before[e]);
     w.start(r, row0 + (threadIdx.x & ~31u));
     clear_words(mask, W * cols);
     __syncthreads();
