@@ -442,7 +442,7 @@ ws_status_t ws_routing_combine_backward(const ws_routing* r, const void* gy, int
  *   matmul            ys[s] = W[e] xs[s]                     xs: nnz x K, ys: nnz x N
  *   matmul_backward   gxs[s] = W[e]^T gys[s]                 gys: nnz x N, gxs: nnz x K; NULL: not wanted, W is not read
  *                     gW[e] = sum over s of gys[s] xs[s]^T   zero for columns without entries; NULL: not wanted, xs is not read
- * Rows behind the placed entries are not written (ys, gxs).  N, K <= 2^24.
+ * Rows behind the placed entries are zero (ys, gxs).  N, K <= 2^24.
  * An input whose address or strides are not multiples of 16 bytes is first
  * copied to `scratch` (16-byte aligned), which has to have room for 16 bytes for every 8 values, or part of
  * them, of its rows; scratch may be NULL where all inputs are aligned.

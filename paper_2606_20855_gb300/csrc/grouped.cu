@@ -15,6 +15,8 @@
 // whose contraction index runs along its rows (W in `rows`, both in `weights`)
 // is given to the tensor cores as "MN-major", never transposed by a copy.
 //
+// Rows of the result behind the placed entries (there are some only if entries
+// have no column) are zero, as in the rows that are moved.
 // A tile of rows may reach past its expert's last row: such rows are computed
 // and not stored.  In `weights` they would be summed, so the last stage is
 // multiplied as far as it has rows, in steps of 16, and the rows past the end in the last
@@ -461,6 +463,9 @@ __global__ void __launch_bounds__(kThreadsOf<kRows>, 1)
     Tile t;
     uint16_t* const result = static_cast<uint16_t*>(p.out);
     int turns = 0;  // the piece that is next
+    if constexpr (kRows != kRowsSum)  // rows behind the placed entries
+      for (int64_t s = p.offsets[p.groups] + 4 * static_cast<int64_t>(blockIdx.x) + quarter; s < p.nnz; s += 4 * static_cast<int64_t>(gridDim.x))
+        for (int c = lane; c < p.features; c += 32) result[s * p.ldo + c] = 0;
     for (int64_t i = team; ok && tile_at<BN, kRows, kPair>(p, first, i, rank, &t); i += teams) {
       if (t.steps > 0) {
         ok = bar_wait_warp(smem_u32(&acc_full[acc]), acc_phase, &dead);
@@ -549,7 +554,7 @@ constexpr int kThinRows = 8, kThinFeatures = 32;
 
 template <bool half>
 __global__ void __launch_bounds__(kThinThreads, 3)
-    thin_kernel(const int64_t* offsets, int groups, const uint16_t* x, int64_t ldx,
+    thin_kernel(const int64_t* offsets, int groups, int64_t nnz, const uint16_t* x, int64_t ldx,
                 const uint16_t* W, int64_t ldw, int64_t group_stride, uint16_t* y, int64_t ldy,
                 int N, int K) {
   __shared__ float red[kThinWarps][kThinFeatures][kThinRows + 1];
@@ -558,6 +563,12 @@ __global__ void __launch_bounds__(kThinThreads, 3)
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, q = lane & 3;
   if (threadIdx.x == 0) found[0] = -1;
   wait_for_last();
+  const int64_t placed = offsets[groups];
+  const int f0 = blockIdx.x * kThinFeatures;
+  const auto zero_rest = [&] {  // rows behind the placed entries
+    for (int64_t s = placed + static_cast<int64_t>(blockIdx.y) * kThinWarps + warp; s < nnz; s += static_cast<int64_t>(gridDim.y) * kThinWarps)
+      if (f0 + lane < N) y[s * ldy + f0 + lane] = 0;
+  };
   int sum = 0;
   const int want = blockIdx.y;
   for (int e0 = 0; e0 < groups && sum <= want; e0 += kThinThreads) {
@@ -576,8 +587,10 @@ __global__ void __launch_bounds__(kThinThreads, 3)
   }
   __syncthreads();
   const int e = found[0], row0 = found[1], rows = found[2];
-  if (e < 0) return;
-  const int f0 = blockIdx.x * kThinFeatures;
+  if (e < 0) {
+    zero_rest();
+    return;
+  }
   const uint16_t* wrow[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) wrow[i] = W + e * group_stride + min(f0 + 8 * i + g, N - 1) * ldw;
@@ -623,6 +636,7 @@ __global__ void __launch_bounds__(kThinThreads, 3)
     for (int w = 0; w < kThinWarps; ++w) s += red[w][f][row];
     y[(static_cast<int64_t>(row0) + row) * ldy + f0 + f] = bits16<half>(s);
   }
+  zero_rest();
 }
 
 cudaError_t launch_thin(const GroupedRows& g, cudaStream_t s) {
@@ -630,8 +644,8 @@ cudaError_t launch_thin(const GroupedRows& g, cudaStream_t s) {
   const dim3 grid(static_cast<unsigned>((g.N + kThinFeatures - 1) / kThinFeatures),
                   static_cast<unsigned>(g.r->nnz / kThinRows + met));
   const auto kernel = g.half ? thin_kernel<true> : thin_kernel<false>;
-  return launch_early(kernel, grid, kThinThreads, 0, s, 1, g.r->offsets, static_cast<int>(g.r->ncols), static_cast<const uint16_t*>(g.x),
-                      g.ldx, static_cast<const uint16_t*>(g.w), g.ldw, g.group_stride, static_cast<uint16_t*>(g.out), g.ldo,
+  return launch_early(kernel, grid, kThinThreads, 0, s, 1, g.r->offsets, static_cast<int>(g.r->ncols), g.r->nnz,
+                      static_cast<const uint16_t*>(g.x), g.ldx, static_cast<const uint16_t*>(g.w), g.ldw, g.group_stride, static_cast<uint16_t*>(g.out), g.ldo,
                       static_cast<int>(g.N), static_cast<int>(g.K));
 }
 

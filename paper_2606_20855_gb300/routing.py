@@ -277,7 +277,7 @@ class Routing:
 
     def matmul(self, xs: torch.Tensor, W: torch.Tensor, stream=None) -> torch.Tensor:
         """ys[s] = W[e] xs[s] for the rows s of every column e: xs nnz x K in slot order, W E x N x K, bfloat16 or
-        float16; products and sums in 32 bits, rounded once.  Rows behind the placed entries are left unwritten."""
+        float16; products and sums in 32 bits, rounded once.  Rows behind the placed entries are zero."""
         if stream is not None:
             return _elsewhere(self.matmul, stream, xs, W)
         dt, N, K = self._product(xs, W)
