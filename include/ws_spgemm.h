@@ -369,8 +369,9 @@ ws_status_t ws_rowptr_scan_static(int64_t* rowptr, int64_t nrows, ws_stream_t st
  * before anything is queued.  Dense matrices are row-major with unit stride
  * within a row and `ld` values from row to row.  ncols <= 1024, nrows, nnz and
  * the number of dense rows <= INT32_MAX, rows of at most 2^24 values.
- * Entries whose column is not in [0, ncols) take no part: they have slot -1 and
- * gradient 0, and the slots they leave over come last and hold zero rows.
+ * Entries whose column is not in [0, ncols), and those before rowptr[0] and from
+ * rowptr[nrows] on, take no part: they have slot -1 and gradient 0, and the
+ * slots they leave over come last and hold zero rows.
  * rowptr is read within [0, nnz] whatever it holds: where it decreases results
  * are unspecified, but nothing outside the arrays is read or written, and
  * offsets never exceed nnz.

@@ -148,7 +148,17 @@ __device__ __forceinline__ int scan_columns(const ws_routing& r, int cols, int* 
   return slots_before(r, sum, 0);
 }
 
-// Offsets of all columns, and -1 in the slots that entries of no column leave over.
+// Entries of no row, where arrays are longer than the row pointer says: f(entry) for each.
+template <typename F>
+__device__ __forceinline__ void for_rowless(const ws_routing& r, F f) {
+  int begin, end, unused;
+  entry_range(r.rowptr, 0, r.nnz, &begin, &unused);
+  entry_range(r.rowptr, r.nrows - 1, r.nnz, &unused, &end);
+  for (int64_t e = threadIdx.x; e < begin; e += blockDim.x) f(e);
+  for (int64_t e = end + static_cast<int64_t>(threadIdx.x); e < r.nnz; e += blockDim.x) f(e);
+}
+
+// Offsets of all columns, and -1 in the slots that entries of no column leave over and for the entries of no row.
 __device__ __forceinline__ void write_offsets(const ws_routing& r, int cols, const int* first, int placed) {
   for (int e = threadIdx.x; e < cols; e += blockDim.x) r.offsets[e] = first[e];
   if (threadIdx.x == 0) {
@@ -156,6 +166,7 @@ __device__ __forceinline__ void write_offsets(const ws_routing& r, int cols, con
     *r.status = 0;
   }
   for (int64_t i = placed + static_cast<int64_t>(threadIdx.x); i < r.nnz; i += blockDim.x) r.rows[i] = r.entries[i] = -1;
+  if (placed < r.nnz) for_rowless(r, [&](int64_t e) { r.slots[e] = -1; });
 }
 
 // Entries of column e in the warps' rows; pre[w * cols + e] receives those of the warps before w.
@@ -431,6 +442,7 @@ __global__ void __launch_bounds__(kDotThreads)
   const int64_t row = blockIdx.x;
   zero_rest<Pack<T, M>>(r, reinterpret_cast<char*>(gys), ldgys * static_cast<int64_t>(sizeof(T)), width / M, row,
                         gridDim.x, threadIdx.x, kDotThreads);
+  if (row == 0 && r.offsets[r.ncols] < r.nnz) for_rowless(r, [&](int64_t e) { gvals[e] = 0.0f; });
   int begin, end;
   entry_range(r.rowptr, row, r.nnz, &begin, &end);
   const T* g = gy + row * ldgy;

@@ -146,7 +146,8 @@ class Routing:
 
     ``offsets`` (int64 [E + 1]) is the first slot of every column, ``rows`` and ``entries`` (int32 [nnz]) are the row
     and the entry of R in every slot, ``slots`` (int32 [nnz]) is the slot of every entry.  Entries whose column is out
-    of range have slot -1 and take no part; the slots they leave over come last, hold -1 and stand for zero rows.
+    of range, or that no row holds (before rowptr[0], from rowptr[T] on), have slot -1 and
+    take no part; the slots they leave over come last, hold -1 and stand for zero rows.
     The object uses R's arrays as they are at every call: ``combine`` reads R's values then.
     """
 

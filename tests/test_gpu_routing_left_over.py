@@ -42,3 +42,42 @@ def test_products_write_rows_behind_the_placed_entries(counts, left_over, N, K):
             value = float(torch.tensor(value).bfloat16())
             assert bool((t[:placed, :width] == value).all()) and bool((t[placed:Z, :width] == 0).all())
             assert bool(t[Z:].isnan().all()) and bool(t[:, width:].isnan().all())
+
+
+@pytest.mark.parametrize("T,E,k", [(5, 7, 3), (700, 40, 4), (5000, 64, 2)])
+@pytest.mark.parametrize("before,behind", [(0, 1), (0, 900), (300, 0), (17, 41)])
+def test_entries_of_no_row(T, E, k, before, behind):
+    """Arrays longer than the row pointer says, as a program has them that drops entries without reading their number back."""
+    import ctypes
+    from paper_2606_20855_gb300 import DeviceCSR, Routing, _abi
+    g = torch.Generator().manual_seed(T)
+    col = torch.rand((T, E), generator=g).argsort(1)[:, :k].sort(1).values.flatten().to(torch.int32)
+    nnz, Z, H = T * k, before + T * k + behind, 40
+    wide = torch.cat([torch.zeros(before, dtype=torch.int32), col, torch.full((behind,), E - 1, dtype=torch.int32)]).cuda()
+    v = torch.rand(Z, generator=g).cuda()
+    rowptr = torch.arange(T + 1, device="cuda") * k
+    want = Routing(DeviceCSR(T, E, rowptr, col.cuda(), v[before:before + nnz].contiguous()))
+
+    def filled(n, value, dt):
+        return torch.full((n,), value, dtype=dt, device="cuda")
+
+    rowptr = rowptr + before
+    offsets, status = filled(E + 1, 7, torch.int64), filled(1, 7, torch.int32)
+    rows, entries, slots = (filled(Z, 7, torch.int32) for _ in range(3))
+    r = _abi.WsRouting(T, E, Z, rowptr.data_ptr(), wide.data_ptr(), v.data_ptr(), offsets.data_ptr(), rows.data_ptr(), entries.data_ptr(),
+                       slots.data_ptr(), status.data_ptr())
+    need, stream = _abi.ws_routing_scratch(T, E), torch.cuda.current_stream().cuda_stream
+    room = torch.empty(max(need, 16), dtype=torch.uint8, device="cuda")
+    p = ctypes.byref(r)
+    _abi.ws_routing_build(p, room.data_ptr(), need, stream)
+    assert torch.equal(offsets, want.offsets) and torch.equal(rows[:nnz], want.rows) and torch.equal(entries[:nnz], want.entries + before)
+    assert bool((rows[nnz:] == -1).all()) and bool((entries[nnz:] == -1).all())
+    assert torch.equal(slots[before:before + nnz], want.slots)
+    assert bool((slots[:before] == -1).all()) and bool((slots[before + nnz:] == -1).all())
+
+    gy, ys = (torch.randn((n, H), generator=g).cuda() for n in (T, Z))
+    gys, gvals = torch.full((Z, H), math.nan, device="cuda"), filled(Z, math.nan, torch.float32)
+    _abi.ws_routing_combine_backward(p, gy.data_ptr(), H, ys.data_ptr(), H, gys.data_ptr(), H, gvals.data_ptr(), H, _abi.WS_F32, stream)
+    a, b = want.combine_backward(gy, ys[:nnz])
+    assert torch.equal(gys[:nnz], a) and torch.equal(gvals[before:before + nnz], b)
+    assert bool((gys[nnz:] == 0).all()) and bool((gvals[:before] == 0).all()) and bool((gvals[before + nnz:] == 0).all())
