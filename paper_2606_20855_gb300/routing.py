@@ -148,7 +148,8 @@ class Routing:
     and the entry of R in every slot, ``slots`` (int32 [nnz]) is the slot of every entry.  Entries whose column is out
     of range, or that no row holds (before rowptr[0], from rowptr[T] on), have slot -1 and
     take no part; the slots they leave over come last, hold -1 and stand for zero rows.
-    The object uses R's arrays as they are at every call: ``combine`` reads R's values then.
+    The plan is that of R's shape, row pointer and columns when it is built, and keeps those arrays.  ``combine`` and its
+    gradient read R's values as they are at the call, of the tensor that ``R.vals`` is then.
     """
 
     def __init__(self, R: DeviceCSR, validate: bool = False, stream=None):
@@ -162,10 +163,12 @@ class Routing:
                 not rowptr.get_device() == colidx.get_device() == vals.get_device() or \
                 not (rowptr.is_contiguous() and colidx.is_contiguous() and vals.is_contiguous()):
             raise TypeError("rowptr/colidx/vals must be contiguous int64/int32/float32 tensors on one GPU")
-        nnz, T, E = colidx.numel(), R.nrows, R.ncols
+        self._nrows, self._ncols = T, E = R.nrows, R.ncols
+        nnz = colidx.numel()
         if rowptr.numel() != T + 1 or vals.numel() != nnz:
             raise ValueError("rowptr must have nrows + 1 entries, and every column index a value")
         self.R, self.nnz, self.device = R, nnz, rowptr.device
+        self._arrays, self._vals = (rowptr, colidx), vals  # whose addresses the calls get
         self._index = self.device.index
         self._stream = raw = _raw_stream(self._index)
         if validate:
@@ -187,7 +190,7 @@ class Routing:
 
     @property
     def offsets(self) -> torch.Tensor:
-        return self._part(0, 2 * self.R.ncols + 2).view(torch.int64)
+        return self._part(0, 2 * self._ncols + 2).view(torch.int64)
 
     @property
     def rows(self) -> torch.Tensor:
@@ -217,15 +220,26 @@ class Routing:
         raw = _raw_stream(self._index)
         if raw != self._stream:
             s = torch.cuda.current_stream(self.device)
-            for u in (self._buf, self.R.rowptr, self.R.colidx, self.R.vals):
+            for u in (self._buf, *self._arrays, self._vals):
                 u.record_stream(s)
         return raw
+
+    def _read_values(self) -> None:
+        """R's values for a call that reads them: the tensor may be another one than at the last call."""
+        vals = self.R.vals
+        if vals is not self._vals:
+            if vals.dtype != torch.float32 or vals.get_device() != self._index or not vals.is_contiguous():
+                raise TypeError("R's values must be a contiguous float32 tensor on the routing matrix's device")
+            if vals.numel() != self.nnz:
+                raise ValueError(f"R must have {self.nnz} values, got {vals.numel()}")
+            self._vals, self._c.vals = vals, vals.data_ptr()
+            vals.record_stream(torch.cuda.current_stream(self.device))
 
     def dispatch(self, x: torch.Tensor, stream=None) -> torch.Tensor:
         """xs[slot] = x[row]: the rows of x (T x H) in slot order (nnz x H)."""
         if stream is not None:
             return _elsewhere(self.dispatch, stream, x)
-        x, ld, H, dt = self._rows_of(x, self.R.nrows, "x")
+        x, ld, H, dt = self._rows_of(x, self._nrows, "x")
         out = torch.empty((self.nnz, H), dtype=x.dtype, device=self.device)
         _abi.ws_routing_dispatch(self._r, x.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue())
         return out
@@ -235,7 +249,7 @@ class Routing:
         if stream is not None:
             return _elsewhere(self.dispatch_backward, stream, grad_xs)
         g, ld, H, dt = self._rows_of(grad_xs, self.nnz, "grad_xs")
-        out = torch.empty((self.R.nrows, H), dtype=g.dtype, device=self.device)
+        out = torch.empty((self._nrows, H), dtype=g.dtype, device=self.device)
         _abi.ws_routing_dispatch_backward(self._r, g.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue())
         return out
 
@@ -244,7 +258,8 @@ class Routing:
         if stream is not None:
             return _elsewhere(self.combine, stream, ys)
         ys, ld, H, dt = self._rows_of(ys, self.nnz, "ys")
-        out = torch.empty((self.R.nrows, H), dtype=ys.dtype, device=self.device)
+        self._read_values()
+        out = torch.empty((self._nrows, H), dtype=ys.dtype, device=self.device)
         _abi.ws_routing_combine(self._r, ys.data_ptr(), ld, out.data_ptr(), H, H, dt, self._queue())
         return out
 
@@ -253,11 +268,12 @@ class Routing:
         if stream is not None:
             return _elsewhere(self.combine_backward, stream, grad_y, ys)
         ys, ld, H, dt = self._rows_of(ys, self.nnz, "ys")
-        g, ldg, same, dtg = self._rows_of(grad_y, self.R.nrows, "grad_y")
+        g, ldg, same, dtg = self._rows_of(grad_y, self._nrows, "grad_y")
         if dtg != dt:
             raise TypeError("grad_y must have the other matrix's type and device")
         if same != H:
             raise ValueError("grad_y and ys differ in the length of their rows")
+        self._read_values()
         out = torch.empty((self.nnz, H), dtype=ys.dtype, device=self.device)
         gvals = torch.empty(self.nnz, dtype=torch.float32, device=self.device)
         _abi.ws_routing_combine_backward(self._r, g.data_ptr(), ldg, ys.data_ptr(), ld, out.data_ptr(), H,
@@ -267,8 +283,8 @@ class Routing:
     def _product(self, xs: torch.Tensor, W: torch.Tensor):
         """(type, N, K) of a product."""
         dt, stack, rows = _dtype(xs, "xs"), W.shape, xs.shape
-        if len(stack) != 3 or stack[0] != self.R.ncols:
-            raise ValueError(f"W must be {self.R.ncols} matrices, got {tuple(stack)}")
+        if len(stack) != 3 or stack[0] != self._ncols:
+            raise ValueError(f"W must be {self._ncols} matrices, got {tuple(stack)}")
         if W.dtype != xs.dtype or not W.get_device() == xs.get_device() == self._index:
             raise TypeError("W and xs must have one type and be on the routing matrix's device")
         _, N, K = stack
@@ -295,7 +311,7 @@ class Routing:
         column without entries), in their types."""
         if stream is not None:
             return _elsewhere(self.matmul_backward, stream, grad_ys, xs, W)
-        (dt, N, K), E = self._product(xs, W), self.R.ncols
+        (dt, N, K), E = self._product(xs, W), self._ncols
         _same(grad_ys, xs, "grad_ys")
         if grad_ys.dim() != 2 or grad_ys.shape[0] != self.nnz or grad_ys.shape[1] != N:
             raise ValueError(f"grad_ys must be {self.nnz} rows of {N} values, got {tuple(grad_ys.shape)}")
@@ -315,7 +331,7 @@ class Routing:
             return _elsewhere(self.wait, stream)
         self._queue()
         torch.cuda.current_stream(self.device).synchronize()
-        if int(self._buf[2 * (self.R.ncols + 1)]):
+        if int(self._buf[2 * (self._ncols + 1)]):
             raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
 
 
