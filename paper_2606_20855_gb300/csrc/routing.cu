@@ -181,7 +181,12 @@ __device__ __forceinline__ int count_column(const uint32_t* mask, uint16_t* pre,
 }
 
 // Shared memory: mask [W][cols], two int arrays [cols], pre [W][cols].
-size_t build_smem(int cols, int W) { return static_cast<size_t>(cols) * (W * 4 + 8 + W * 2); }
+constexpr size_t build_smem(int cols, int W) { return static_cast<size_t>(cols) * (W * 4 + 8 + W * 2); }
+
+// The most that a plan in a single launch takes.  A kernel's limit of dynamic shared memory is set to a constant: it is the kernel's,
+// whichever thread launches it, and a smaller plan of one thread may not lower it under another's.
+constexpr size_t kMostSmall = 200 * 1024;
+static_assert(build_smem(kRouteMaxCols, kSmallWarps) <= kMostSmall);
 
 // As many warps as the rows need.  stage: rows and entries are put in the order of their slots in shared memory first, because one SM
 // stores the 32 places of a warp one after the other.  us without | with: 1001 rows of eight entries over 64 columns 14.0 | 8.6
@@ -565,15 +570,15 @@ int64_t routing_chunks(int64_t nrows, int64_t ncols, int num_sms) {
 void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cudaStream_t s) {
   const int cols = static_cast<int>(r.ncols);
   const int64_t chunks = routing_chunks(r.nrows, cols, num_sms);
-  const auto allow = [&](const void* kernel, size_t smem) {
-    if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
+  const auto allow = [&](const void* kernel, size_t smem, size_t most) {
+    if (smem > 48 * 1024) cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(most));
   };
   if (chunks == 1) {
     const int warps = r.nrows <= 128 ? 4 : static_cast<int>((r.nrows + 31) / 32);  // four at least, for the columns
     const size_t own = build_smem(cols, warps), all = ((own + 3) & ~size_t{3}) + static_cast<size_t>(r.nnz) * 4;
-    const bool stage = r.nnz <= 65536 && all <= 200 * 1024;
+    const bool stage = r.nnz <= 65536 && all <= kMostSmall;
     const size_t smem = stage ? all : own;
-    allow(reinterpret_cast<const void*>(routing_small_kernel), smem);
+    allow(reinterpret_cast<const void*>(routing_small_kernel), smem, kMostSmall);
     routing_small_kernel<<<1, 32 * warps, smem, s>>>(r, cols, stage);
     return;
   }
@@ -581,8 +586,8 @@ void launch_routing_build(const ws_routing& r, int32_t* counts, int num_sms, cud
     constexpr int W = decltype(warps)::value;
     const size_t smem = build_smem(cols, W);
     const int64_t chunk = up(up(r.nrows, 32 * W), chunks) * 32 * W;
-    allow(reinterpret_cast<const void*>(routing_count_kernel<W>), smem);
-    allow(reinterpret_cast<const void*>(routing_place_kernel<W>), smem);
+    allow(reinterpret_cast<const void*>(routing_count_kernel<W>), smem, build_smem(kRouteMaxCols, W));
+    allow(reinterpret_cast<const void*>(routing_place_kernel<W>), smem, build_smem(kRouteMaxCols, W));
     routing_count_kernel<W><<<static_cast<unsigned>(chunks), 32 * W, smem, s>>>(r, cols, chunk, counts);
     launch_early(routing_place_kernel<W>, dim3(static_cast<unsigned>(chunks)), 32 * W, smem, s, 1, r, cols, chunk, counts);
   };
