@@ -7,7 +7,7 @@
 // Two kernels: inner products h = A[a] x[t] for every entry of S, then
 // y = base + B[a] (v h).  Both are bound by memory (x, base and y, and the met
 // adapters, once each; 2 rank multiply-adds per value), so h stays small: sums
-// are 32-bit, and where v h meets B on the tensor cores it is a pair of 16-bit values, its rounding and the
+// are 32-bit, and where v h meets B on the tensor cores (many tokens) it is a pair of 16-bit values, its rounding and the
 // rounding of what that left over, 16 (bfloat16) or 22 (half) significant bits.
 // One 16-bit value would add an error as large as the result's own rounding.
 // A half pair holds |v h| up to 65504.
@@ -494,7 +494,7 @@ constexpr int kStepSplit = 4;
 
 // vec: the rows of x and A start at multiples of 16 bytes.
 template <bool half, bool vec>
-__global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapters_call c, uint2* __restrict__ h, int rpad) {
+__global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapters_call c, float2* __restrict__ h, int rpad) {
   __shared__ float2 part[kAdWarps];
   may_start_next();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -536,7 +536,6 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
         for (int u = 0; u < U; ++u) add(xv[u], av[u], bv[u]);
       }
       for (; k < K; k += kStep) add(load8(x, k, K, vec), load8(A0, k, K, vec), load8(A1, k, K, vec));
-      if (2 * p + 1 >= r) s1 = 0.0f;
     }
     s0 = warp_sum(s0);
     s1 = warp_sum(s1);
@@ -546,7 +545,7 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
 #pragma unroll
       for (int i = 1; i < kStepSplit; ++i) s0 += part[warp + i].x, s1 += part[warp + i].y;
       const float v = c.vals[e];
-      h[static_cast<int64_t>(e) * pairs + p] = 2 * p < r ? split_pair<half>(v * s0, v * s1) : make_uint2(0, 0);
+      h[static_cast<int64_t>(e) * pairs + p] = make_float2(2 * p < r ? v * s0 : 0.0f, 2 * p + 1 < r ? v * s1 : 0.0f);
     }
     __syncthreads();
   }
@@ -556,7 +555,7 @@ __global__ void __launch_bounds__(kAdThreads) shrink_step_kernel(const ws_adapte
 // 4096 values, 6.3 MB of B: 5 us, of which what does not need h passes while the inner products run (four
 // tokens of 512 values, both kernels: 6.8 us without, 5.1 us with that).
 template <bool half>
-__global__ void __launch_bounds__(kAdThreads) expand_step_kernel(const ws_adapters_call c, const uint2* h, int rpad, bool vecB) {
+__global__ void __launch_bounds__(kAdThreads) expand_step_kernel(const ws_adapters_call c, const float2* h, int rpad, bool vecB) {
   const int64_t n = static_cast<int64_t>(blockIdx.x) * kAdThreads + threadIdx.x, t = blockIdx.y;
   if (n >= c.N) return;
   if (c.nnz == 0) wait_for_last();  // as in the tiles: another call may write base
@@ -573,26 +572,22 @@ __global__ void __launch_bounds__(kAdThreads) expand_step_kernel(const ws_adapte
     const int a = c.colidx[e];
     if (!met(c, a)) continue;
     const uint16_t* row = static_cast<const uint16_t*>(c.B) + a * c.strideB + n * c.ldb;
-    const uint4* hv = reinterpret_cast<const uint4*>(h + static_cast<int64_t>(e) * (rpad / 2));
+    const float4* hv = reinterpret_cast<const float4*>(h + static_cast<int64_t>(e) * (rpad / 2));
 #pragma unroll 4
     for (int k = 0; k < r; k += 4) {
       const uint2 b = load4(row, k, r, vecB);
-      const uint4 p = hv[k / 4];
-      const uint32_t hi[2] = {p.x, p.z}, lo[2] = {p.y, p.w}, bw[2] = {b.x, b.y};
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        acc = fmaf(value16<half>(static_cast<uint16_t>(hi[i])) + value16<half>(static_cast<uint16_t>(lo[i])),
-                   value16<half>(static_cast<uint16_t>(bw[i])), acc);
-        acc = fmaf(value16<half>(static_cast<uint16_t>(hi[i] >> 16)) + value16<half>(static_cast<uint16_t>(lo[i] >> 16)),
-                   value16<half>(static_cast<uint16_t>(bw[i] >> 16)), acc);
-      }
+      const float4 p = hv[k / 4];
+      acc = fmaf(p.x, value16<half>(static_cast<uint16_t>(b.x)), acc);
+      acc = fmaf(p.y, value16<half>(static_cast<uint16_t>(b.x >> 16)), acc);
+      acc = fmaf(p.z, value16<half>(static_cast<uint16_t>(b.y)), acc);
+      acc = fmaf(p.w, value16<half>(static_cast<uint16_t>(b.y >> 16)), acc);
     }
   }
   static_cast<uint16_t*>(c.y)[t * c.ldy + n] = bits16<half>(acc);
 }
 
 template <bool half>
-ws_status_t launch_step(const ws_adapters_call& c, uint2* h, cudaStream_t s) {
+ws_status_t launch_step(const ws_adapters_call& c, float2* h, cudaStream_t s) {
   const int rpad = adapters_rank(c.r);
   const bool vecB = c.r % 4 == 0 && reinterpret_cast<uintptr_t>(c.B) % 8 == 0 && c.ldb % 4 == 0 && c.strideB % 4 == 0;
   const unsigned T = static_cast<unsigned>(c.nrows);
@@ -652,7 +647,7 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
 ws_status_t launch_adapters(const ws_adapters_call& c, void* scratch, int num_sms, cudaStream_t s) {
   char* h = static_cast<char*>(scratch) + 16;  // behind the status word
   if (!adapters_step(c.nrows, c.r)) return launch_prompt(c, reinterpret_cast<float*>(h), static_cast<int*>(scratch), num_sms, s);
-  return c.dtype == WS_F16 ? launch_step<true>(c, reinterpret_cast<uint2*>(h), s) : launch_step<false>(c, reinterpret_cast<uint2*>(h), s);
+  return c.dtype == WS_F16 ? launch_step<true>(c, reinterpret_cast<float2*>(h), s) : launch_step<false>(c, reinterpret_cast<float2*>(h), s);
 }
 
 }  // namespace wsk
