@@ -8,9 +8,13 @@
 // y = base + B[a] (v h).  Both are bound by memory (x, base and y, and the met
 // adapters, once each; 2 rank multiply-adds per value), so h stays small: sums
 // are 32-bit, and where v h meets B on the tensor cores (many tokens) it is a pair of 16-bit values, its rounding and the
-// rounding of what that left over, 16 (bfloat16) or 22 (half) significant bits.
+// rounding of what that left over.
 // One 16-bit value would add an error as large as the result's own rounding.
-// A half pair holds |v h| up to 65504.
+// A pair of bfloat16 holds 16 significant bits over the range of floats.  Halves end at 65504 and 2^-24, so a token's v h are
+// multiplied by a power of two, which its sums are divided by: the one that brings the largest of the token's first 32 ranks to
+// 2^10 .. 2^11.  The pair then is off by at most 2^-23 of a value, plus 2^-35 of the largest one.  Further ranks and
+// adapters of the token are multiplied by the same power; if that leaves the largest of 32 of them outside 1 .. 2^15, where
+// the second bound would be above 2^-25 of it, or it overflows, the token's values are computed one by one in 32 bits.
 //
 // Few tokens ("step"): every token is on its own, its inner products split over warps, then
 // a thread per value of y: everything in flight at once, no
@@ -39,6 +43,22 @@ __device__ __forceinline__ uint2 split_pair(float a, float b) {
   const uint16_t la = bits16<half>(ra == ra && fabsf(ra) <= 3.4e38f ? ra : 0.0f);
   const uint16_t lb = bits16<half>(rb == rb && fabsf(rb) <= 3.4e38f ? rb : 0.0f);
   return make_uint2(ha | static_cast<uint32_t>(hb) << 16, la | static_cast<uint32_t>(lb) << 16);
+}
+
+// Of the largest |v h| of 32 ranks of a token, when halves are to hold them: the power of two that the token has, or gets now
+// (0: none yet), and whether that does not fit these ranks.  Below 2^-60 they are less than any half, whatever B holds.
+struct HalfScale {
+  float power;
+  bool unfit;
+};
+__device__ __forceinline__ HalfScale half_scale(float power, float largest) {
+  if (!(largest > 8.7e-19f && largest <= 3.4e38f)) return {power, false};
+  if (power == 0.0f) {  // 2^(10 - e) for a largest of 2^e and more
+    const int e = static_cast<int>(__float_as_uint(largest) >> 23) - 127;
+    power = __uint_as_float(static_cast<uint32_t>(10 - e + 127) << 23);
+  }
+  const float z = largest * power;
+  return {power, !(z >= 1.0f && z <= 32768.0f)};
 }
 
 // Ranks k .. k + 3 of a row of B, zero past its end.
@@ -311,7 +331,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   __shared__ uint32_t tmem_slot;
   __shared__ volatile int dead;
   __shared__ int mins[kExpandThreads / 32], entry[kTok];
-  __shared__ float value[kTok];
+  __shared__ float value[kTok], power[half ? kTok : 1];  // power: of two, for v h of the token (0: none yet)
+  __shared__ bool alone[half ? kTok : 1];                // the token's values are computed one by one
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, m = threadIdx.x & (kTok - 1), side = threadIdx.x / kTok;
   const uint32_t sa = (smem_u32(raw) + 1023u) & ~1023u, sy = sa + kExpandA, sb = sy + 4 * kExpandY;
   const int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTok, t = t0 + m;
@@ -333,6 +354,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
     }
   }
   if (warp == 0) tmem_alloc<kExpandN>(smem_u32(&tmem_slot));
+  if constexpr (half)
+    if (side == 0) power[m] = 0.0f, alone[m] = false;
   Walk w;
   w.start(c, t);
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -373,15 +396,41 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
                                                                                4 * (at & ((1 << log_quads) - 1)))
                                            : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
       }
+      float4 vh[kTurns];
+      float had[kTurns], largest[kTurns];
+#pragma unroll
+      for (int i = 0; i < kTurns; ++i) {
+        const int row = (threadIdx.x + kExpandThreads * i) >> log_quads;
+        float4 f = part[i][0];
+#pragma unroll
+        for (int k = 1; k < kMaxSplit; ++k) f.x += part[i][k].x, f.y += part[i][k].y, f.z += part[i][k].z, f.w += part[i][k].w;
+        const float s = row < kTok ? value[row] : 0.0f;
+        vh[i] = make_float4(s * f.x, s * f.y, s * f.z, s * f.w);
+        if constexpr (half) {
+          had[i] = row < kTok ? power[row] : 0.0f;
+          largest[i] = fmaxf(fmaxf(fabsf(vh[i].x), fabsf(vh[i].y)), fmaxf(fabsf(vh[i].z), fabsf(vh[i].w)));
+        }
+      }
+      if constexpr (half) {  // of all ranks of a token, which neighbouring lanes hold
+        for (int o = 1; o < 1 << log_quads; o <<= 1)
+#pragma unroll
+          for (int i = 0; i < kTurns; ++i) largest[i] = fmaxf(largest[i], __shfl_xor_sync(0xffffffffu, largest[i], o));
+        __syncwarp();  // all of them have read its power
+      }
 #pragma unroll
       for (int i = 0; i < kTurns; ++i) {
         const int at = threadIdx.x + kExpandThreads * i, row = at >> log_quads, quad = at & ((1 << log_quads) - 1);
         if (row >= kTok) break;
-        float4 f = part[i][0];
-#pragma unroll
-        for (int k = 1; k < kMaxSplit; ++k) f.x += part[i][k].x, f.y += part[i][k].y, f.z += part[i][k].z, f.w += part[i][k].w;
-        const float s = value[row];
-        const uint2 a01 = split_pair<half>(s * f.x, s * f.y), a23 = split_pair<half>(s * f.z, s * f.w);
+        float4 f = vh[i];
+        if constexpr (half) {
+          const HalfScale now = half_scale(had[i], largest[i]);
+          if (quad == 0) {
+            power[row] = now.power;
+            if (now.unfit) alone[row] = true;
+          }
+          if (now.power != 0.0f) f = make_float4(now.power * f.x, now.power * f.y, now.power * f.z, now.power * f.w);
+        }
+        const uint2 a01 = split_pair<half>(f.x, f.y), a23 = split_pair<half>(f.z, f.w);
         const uint32_t to = sa + row * 128 + 8 * (quad & 1), hi = to + (((quad >> 1) ^ (row & 7)) << 4),
                        lo = to + (((4 + (quad >> 1)) ^ (row & 7)) << 4);
         asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(hi), "r"(a01.x), "r"(a23.x) : "memory");
@@ -424,6 +473,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
   __syncthreads();
   if (!dead) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const bool by_itself = half && alone[half ? m : 0];
+    const float times = half && !by_itself && power[half ? m : 0] != 0.0f ? power[half ? m : 0] : 1.0f, back = 1.0f / times;  // exact
 #pragma unroll 1
     for (int q = 2 * side; q < 2 * side + 2 && q < pieces; ++q) {  // 64 columns, stored as soon as they are there
 #pragma unroll 1
@@ -433,10 +484,10 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
         float f[16] = {};
         __syncwarp();
         if (done > 0) tmem_load16(tmem + j + (static_cast<uint32_t>((warp & 3) * 32) << 16), f);
-        if (mixed && there) {
+        if ((mixed || by_itself) && there) {
           // A token without an adapter got zero times its values: nothing, unless those are infinite or NaN.
           for (int i = 0; i < 16; ++i)
-            if (i < left && !(fabsf(f[i]) <= 3.4e38f)) f[i] = added<half>(c, h, rpad, split, t, n0 + j + i);
+            if (i < left && (by_itself || !(fabsf(f[i]) <= 3.4e38f))) f[i] = times * added<half>(c, h, rpad, split, t, n0 + j + i);
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
@@ -446,8 +497,8 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
             asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]) : "r"(at) : "memory");
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            b[i] = pair16<half>(value16<half>(static_cast<uint16_t>(b[i])) + f[8 * s + 2 * i],
-                                value16<half>(static_cast<uint16_t>(b[i] >> 16)) + f[8 * s + 2 * i + 1]);
+            b[i] = pair16<half>(fmaf(f[8 * s + 2 * i], back, value16<half>(static_cast<uint16_t>(b[i]))),
+                                fmaf(f[8 * s + 2 * i + 1], back, value16<half>(static_cast<uint16_t>(b[i] >> 16))));
           asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(b[0]), "r"(b[1]), "r"(b[2]), "r"(b[3]) : "memory");
         }
       }

@@ -69,3 +69,68 @@ def test_few_tokens(T, L, r, K, N, dt, how, size):
     bound = U[dt] * want.abs() + (K + 2 * r + 8) * 2.0 ** -23 * mass + STEP[dt]
     bad = ~((got.double() - want).abs() <= bound)
     assert not bool(bad.any()), (int(bad.sum()), got[bad][:4], want[bad][:4])
+
+
+# Many tokens: v h is kept as a pair of 16-bit values, off by 2^-16 of it (bfloat16); in half by 2^-23 of it and, where the largest of
+# 32 ranks of a token is brought to 1 or more, by 2^-25 of that largest one.
+def _pairs(x, A, B, on, vals, dt):
+    if dt == torch.bfloat16:
+        return None
+    extra = torch.zeros((x.shape[0], B.shape[1]), dtype=torch.float64, device="cuda")
+    for a in range(on.shape[1]):
+        t = on[:, a]
+        vh = (vals[t, a].float().double()[:, None] * (x[t].double() @ A[a].double().T)).abs()
+        for r0 in range(0, A.shape[1], 32):
+            largest = vh[:, r0:r0 + 32].max(1, keepdim=True).values
+            extra[t] += 2.0 ** -25 * largest * B[a][:, r0:r0 + 32].double().abs().sum(1)[None, :]
+    return extra
+
+
+def _check_tiles(x, A, B, on, vals, base):
+    from paper_2606_20855_gb300 import adapters
+    dt, K, r = x.dtype, x.shape[1], A.shape[1]
+    got = adapters(x, A, B, _csr(on, vals), base, wait=True)
+    want, mass = _exact(x, A, B, on, vals, base)
+    bound = U[dt] * want.abs() + (K + 2 * r + 8) * 2.0 ** -23 * mass + STEP[dt]
+    extra = _pairs(x, A, B, on, vals, dt)
+    bound += 2.0 ** -16 * mass if extra is None else extra + 2.0 ** -23 * mass
+    bad = ~((got.double() - want).abs() <= bound)
+    if dt == torch.float16:  # from 65520 on a half is infinite
+        bad &= ~(torch.isinf(got) & (want.abs() + bound >= 65520) & (got.sign() == want.sign()))
+    assert not bool(bad.any()), (int(bad.sum()), bad.nonzero()[:4].tolist(), got[bad][:4], want[bad][:4])
+
+
+@pytest.mark.parametrize("size", [1e6, 2e5, 1.0, 1e-3, 1e-6, 1e-9])
+@pytest.mark.parametrize("how", ["one", "runs", "several"])
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("T,L,r,K,N", [(700, 5, 16, 64, 48), (300, 4, 40, 200, 300), (530, 3, 64, 72, 257), (600, 6, 13, 1000, 100)])
+def test_many_tokens(T, L, r, K, N, dt, how, size):
+    _check_tiles(*_case(T, L, r, K, N, dt, size, how))
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("r", [16, 48])
+def test_values_far_apart(dt, r):
+    """Adapters of one token, tokens of one tile and ranks of one adapter whose sizes differ by many powers of ten."""
+    T, L, K, N = 600, 5, 96, 130
+    x, A, B, on, vals, base = _case(T, L, r, K, N, dt, 1.0, "several")
+    g = torch.Generator(device="cuda").manual_seed(7)
+    vals = 10.0 ** (torch.rand((T, L), generator=g, device="cuda") * 10 - 7)
+    _check_tiles(x, A, B, on, vals, base)
+    ranks = 10.0 ** (torch.rand((1, r, 1), generator=g, device="cuda") * 7 - 5)
+    _check_tiles(x, (A.float() * ranks).to(dt), B, on, vals, base)
+    vals[::3] = 0.0  # entries that add nothing
+    _check_tiles(x, A, B, on, vals, base)
+
+
+@pytest.mark.parametrize("size", [1.0, 2e5, 1e-6])
+def test_a_token_does_not_depend_on_its_tile(size):
+    """Equal bits, whether all tokens of a tile share an adapter or every other one has another or none."""
+    from paper_2606_20855_gb300 import adapters
+    x, A, B, on, vals, base = _case(640, 4, 16, 128, 96, torch.float16, size, "one")
+    all_one = adapters(x, A, B, _csr(on, vals), base)
+    mixed = on.clone()
+    mixed[1::4], mixed[2::4, 1], mixed[2::4, 3] = False, False, True
+    some = adapters(x, A, B, _csr(mixed, vals), base)
+    same = (mixed == on).all(1)
+    assert bool(torch.isfinite(all_one).all()) and torch.equal(some[same], all_one[same])
