@@ -250,6 +250,11 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
           float f[16];
           tmem_load16(tmem + acc * kRankBlock + at * n + j + (static_cast<uint32_t>(quarter * 32) << 16), f);
           if (mine) {
+            if (r0 + j + 16 > c.r) {  // past the rank: zero, also where x is infinite (times a zero that the copy filled in)
+#pragma unroll
+              for (int e = 0; e < 16; ++e)
+                if (r0 + j + e >= c.r) f[e] = 0.0f;
+            }
             float4* dst = reinterpret_cast<float4*>(h + static_cast<int64_t>(behind.at) * rpad + r0 + j);
 #pragma unroll
             for (int e = 0; e < 4; ++e) dst[e] = make_float4(f[4 * e], f[4 * e + 1], f[4 * e + 2], f[4 * e + 3]);

@@ -134,3 +134,22 @@ def test_a_token_does_not_depend_on_its_tile(size):
     some = adapters(x, A, B, _csr(mixed, vals), base)
     same = (mixed == on).all(1)
     assert bool(torch.isfinite(all_one).all()) and torch.equal(some[same], all_one[same])
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("r", [1, 15, 16, 40])
+@pytest.mark.parametrize("T", [9, 700])
+def test_infinite_sums_keep_their_sign(T, r, dt):
+    """Positive matrices and one infinite value in x: infinity, not NaN, whatever the rank is padded to."""
+    from paper_2606_20855_gb300 import adapters
+    K, N = 72, 50
+    x, A, B = _randn((T, K), dt, 1), _randn((2, r, K), dt, 2).abs() + 0.5, _randn((2, N, r), dt, 3).abs() + 0.5
+    x[5, 3], x[8, 70] = float("inf"), -float("inf")
+    on = torch.zeros((T, 2), dtype=torch.bool, device="cuda")
+    on[:, 0], on[:, 1] = torch.arange(T, device="cuda") % 3 != 0, torch.arange(T, device="cuda") % 3 == 0
+    on[5], on[8] = torch.tensor([False, True], device="cuda"), torch.tensor([False, True], device="cuda")
+    y = adapters(x, A, B, _csr(on, torch.ones((T, 2), device="cuda")), None)
+    assert bool((y[5] == float("inf")).all()) and bool((y[8] == -float("inf")).all())
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[5], rest[8] = False, False
+    assert bool(torch.isfinite(y[rest]).all())
