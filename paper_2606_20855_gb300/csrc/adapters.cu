@@ -666,14 +666,19 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
   if (!encoder()) return routing_fail(WS_ERR_CUDA, "cuTensorMapEncodeTiled is not available");
   cudaError_t e = cudaMemsetAsync(status, 0, sizeof(int), s);
   if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
-  CUtensorMap x{}, a{}, b{}, base{}, y{};
+  CUtensorMap x{}, a{}, b{};
+  // a grid's y has 65535 CTAs at most: rows of 2^24 values take two launches of the sums
+  constexpr int64_t kMost = int64_t{65535} * kExpandN;
+  const auto describe_b = [&](const void* from, int64_t rows) {
+    return c.nnz == 0 || encode(&b, from, half, c.r, rows, c.ldb, c.ncols, c.strideB, kExpandN, kExpandRanks);
+  };
   if (c.nnz > 0) {
     // parts of K until every SM has a CTA
     const int64_t steps = (c.K + 63) / 64;
     while (split < kMaxSplit && 2 * split <= steps && tiles * split < static_cast<unsigned>(num_sms) / 2) split *= 2;
     if (!encode(&x, c.x, half, c.K, c.nrows, c.ldx, 0, 0, kTok) ||
         !encode(&a, c.A, half, c.K, c.r, c.lda, c.ncols, c.strideA, rpad < kRankBlock ? rpad : kRankBlock) ||
-        !encode(&b, c.B, half, c.r, c.N, c.ldb, c.ncols, c.strideB, kExpandN, kExpandRanks))
+        !describe_b(c.B, c.N < kMost ? c.N : kMost))
       return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
     e = cudaFuncSetAttribute(reinterpret_cast<const void*>(shrink_tile_kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
                              static_cast<int>(kShrinkSmem));
@@ -681,20 +686,28 @@ ws_status_t launch_prompt(const ws_adapters_call& c, float* h, int* status, int 
     const dim3 grid(tiles, static_cast<unsigned>(split), static_cast<unsigned>((rpad + kRankBlock - 1) / kRankBlock));
     shrink_tile_kernel<<<grid, kShrinkThreads, kShrinkSmem, s>>>(x, a, c, h, rpad, status);
   }
-  // base and y by the copy engine where their rows start at multiples of 16 bytes, else by loads and stores
-  const auto rows16 = [](const void* p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; };
-  bool copies = (!c.base || rows16(c.base, c.ldbase)) && rows16(c.y, c.ldy);
-  if (copies && !(encode(&y, c.y, half, c.N, c.nrows, c.ldy, 0, 0, kTok) &&
-                  (!c.base || encode(&base, c.base, half, c.N, c.nrows, c.ldbase, 0, 0, kTok))))
-    copies = false;
   const auto kernel = half ? expand_tile_kernel<true> : expand_tile_kernel<false>;
   e = cudaFuncSetAttribute(reinterpret_cast<const void*>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
                            static_cast<int>(kExpandSmem));
   if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
-  const dim3 grid(tiles, static_cast<unsigned>((c.N + kExpandN - 1) / kExpandN));
-  const cudaError_t launched = launch_early(kernel, grid, kExpandThreads, kExpandSmem, s, 1, b, base, y, c,
-                                            static_cast<const float*>(h), rpad, split, copies, status);
-  if (launched != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(launched));
+  for (int64_t n = 0; n < c.N; n += kMost) {
+    ws_adapters_call p = c;
+    p.N = c.N - n < kMost ? c.N - n : kMost;
+    if (n > 0 && c.nnz > 0) p.B = static_cast<const uint16_t*>(c.B) + n * c.ldb;
+    if (c.base) p.base = static_cast<const uint16_t*>(c.base) + n;
+    p.y = static_cast<uint16_t*>(c.y) + n;
+    if (n > 0 && !describe_b(p.B, p.N)) return routing_fail(WS_ERR_INVALID_ARG, "a matrix cannot be described to the copy engine");
+    CUtensorMap base{}, y{};
+    // base and y by the copy engine where their rows start at multiples of 16 bytes, else by loads and stores
+    const auto rows16 = [](const void* q, int64_t ld) { return reinterpret_cast<uintptr_t>(q) % 16 == 0 && ld % 8 == 0; };
+    bool copies = (!c.base || rows16(p.base, c.ldbase)) && rows16(p.y, c.ldy);
+    if (copies && !(encode(&y, p.y, half, p.N, c.nrows, c.ldy, 0, 0, kTok) &&
+                    (!c.base || encode(&base, p.base, half, p.N, c.nrows, c.ldbase, 0, 0, kTok))))
+      copies = false;
+    const dim3 grid(tiles, static_cast<unsigned>((p.N + kExpandN - 1) / kExpandN));
+    e = launch_early(kernel, grid, kExpandThreads, kExpandSmem, s, 1, b, base, y, p, static_cast<const float*>(h), rpad, split, copies, status);
+    if (e != cudaSuccess) return routing_fail(WS_ERR_CUDA, "adapters: %s", cudaGetErrorString(e));
+  }
   return WS_OK;
 }
 

@@ -193,8 +193,9 @@ inline int adapters_rank(int64_t r) { return static_cast<int>((r + 15) / 16 * 16
 // Whether tokens go one by one.  That reads A and B for every token (from L2), 2 rank (K + N) bytes each; a tile of 128 tokens
 // reads x once for every few adapters it meets.  K = N = 4096, bfloat16, us one by one | as tiles of one adapter | as tiles in
 // which every token has another adapter: 512 tokens of rank 16 31 | 22 | 225, 256 of rank 64 about 100 | 31 | 659, 1024 of rank
-// 16 about 58 | 22 | 225.
-inline bool adapters_step(int64_t nrows, int64_t r) { return nrows * adapters_rank(r) <= 8192; }
+// 16 about 58 | 22 | 225.  Rank 0 (base alone) goes by tokens as rank 16 does: one by one is a launch with a row of CTAs a token, of
+// which there may be 65535.
+inline bool adapters_step(int64_t nrows, int64_t r) { return nrows * (r > 0 ? adapters_rank(r) : 16) <= 8192; }
 // scratch: a status word (16 bytes), then up to four parts of h.
 ws_status_t launch_adapters(const ws_adapters_call& c, void* scratch, int num_sms, cudaStream_t s);
 
