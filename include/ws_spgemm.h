@@ -466,7 +466,8 @@ ws_status_t ws_routing_matmul_backward(const ws_routing* r, const void* gys, int
  * (bfloat16: 16 significant bits; half: off by 2^-23 of them and at most 2^-25 of
  * the largest of 32 ranks of the token, over the range of floats), the result is
  * summed in 32 bits and rounded once.  "Many tokens": nrows times r, rounded up
- * to a multiple of 16, is above 8192.  base may be NULL (zero) and may be y itself.
+ * to a multiple of 16, is above 8192.  base may be NULL (zero) and may be y itself;
+ * y may overlap no other input.
  * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned, and for
  * many tokens 16 bytes more for every 8 values, or part of them, of the rows of
  * each of x, A and B whose address or strides are not multiples of 16 bytes.  For

@@ -341,8 +341,8 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     projection they share (``base``, its result; None for zero).
 
     x: T x K, A: L x r x K, B: L x N x r, base: T x N, bfloat16 or float16; S: T x L in CSR, float32 values, rows empty
-    for tokens without an adapter.  ``out`` may be ``base``: the adapters' part is then added in place.  ``wait``: waits for the
-    result and raises if a kernel gave up a wait.
+    for tokens without an adapter.  ``out`` may be ``base``: the adapters' part is then added in place; it may overlap no
+    other input.  ``wait``: waits for the result and raises if a kernel gave up a wait.
     """
     if stream is not None:
         return _elsewhere(adapters, stream, x, A, B, S, base, out, wait=wait)
@@ -384,6 +384,11 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
             raise ValueError(f"out must be {T} x {N} with unit stride within its rows")
         if base is not None and (out.data_ptr(), ldy) != (base.data_ptr(), ldbase) and _overlap(out, base):
             raise ValueError("out must be base itself or lie apart from it")
+        first, end = _span(out)
+        for t, name in ((x, "x"), (A, "A"), (B, "B"), (rowptr, "S"), (colidx, "S"), (vals, "S")):
+            a, b = _span(t)
+            if a < end and first < b and _overlap(out, t):  # it is written while they are read
+                raise ValueError(f"out must lie apart from {name}")
     scratch = torch.empty(need, dtype=torch.uint8, device=dev)
     call = _abi.ADAPTERS_CALL.pack(T, L, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), K, r, N,
                                    x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), ldb, apartB,
@@ -396,11 +401,32 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     return out
 
 
+def _span(t: torch.Tensor):
+    """First address of a tensor and the one behind its last."""
+    at = t.data_ptr()
+    if t.is_contiguous():
+        return at, at + t.nbytes
+    return at, at + (sum((n - 1) * s for n, s in zip(t.shape, t.stride())) + 1) * t.element_size()
+
+
 def _overlap(a: torch.Tensor, b: torch.Tensor) -> bool:
-    """Whether the address ranges of two matrices meet."""
-    def span(t):
-        if t.numel() == 0:
-            return t.data_ptr(), t.data_ptr()
-        return t.data_ptr(), t.data_ptr() + ((t.shape[0] - 1) * t.stride(0) + t.shape[1]) * t.element_size()
-    (a0, a1), (b0, b1) = span(a), span(b)
-    return a0 < b1 and b0 < a1
+    """Whether two tensors, of unit stride within a row, may share memory: their address ranges meet, and neither's rows
+    all lie between the other's (as column blocks of one matrix do)."""
+    if a.numel() == 0 or b.numel() == 0:
+        return False
+
+    def row(t):  # bytes of a row
+        return (t.shape[-1] - 1) * t.stride(-1) * t.element_size() + t.element_size()
+
+    def steps(t):  # bytes from row to row and from matrix to matrix
+        return [t.stride(i) * t.element_size() for i in range(t.dim() - 1) if t.shape[i] > 1]
+
+    def between(inner, outer):
+        if outer.dim() != 2 or outer.shape[0] < 2:
+            return False
+        ld = outer.stride(0) * outer.element_size()
+        at = (inner.data_ptr() - outer.data_ptr()) % ld
+        return at >= row(outer) and at + row(inner) <= ld and all(s % ld == 0 for s in steps(inner))
+
+    (a0, a1), (b0, b1) = _span(a), _span(b)
+    return a0 < b1 and b0 < a1 and not between(a, b) and not between(b, a)
