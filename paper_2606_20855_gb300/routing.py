@@ -25,6 +25,14 @@ from .spgemm import DeviceCSR
 
 _ROW_DTYPES = {torch.float32: _abi.WS_F32, torch.bfloat16: _abi.WS_BF16, torch.float16: _abi.WS_F16}
 _raw_stream = torch._C._cuda_getCurrentRawStream  # of a device, without building the object
+_current_device = torch._C._cuda_getDevice
+
+
+def _queue_of(index: int) -> int:
+    """The current stream of the tensors' device, which has to be the current device: the library launches there."""
+    if _current_device() != index:
+        raise ValueError(f"tensors on device {index}, but device {_current_device()} is current")
+    return _raw_stream(index)
 
 
 def _elsewhere(f, stream, *args, **kwargs):
@@ -108,7 +116,7 @@ def topk_route(logits: torch.Tensor, k: int, normalize: bool = True, stream=None
     colidx = torch.empty(T * k, dtype=torch.int32, device=dev)
     vals = torch.empty(T * k, dtype=torch.float32, device=dev)
     _abi.ws_topk_route(x.data_ptr(), T, E, ld, dt, k, normalize, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(),
-                       _raw_stream(dev.index))
+                       _queue_of(dev.index))
     return DeviceCSR(T, E, rowptr, colidx, vals)
 
 
@@ -132,7 +140,7 @@ def topk_route_backward(logits: torch.Tensor, R: DeviceCSR, grad_vals: torch.Ten
     g, vals, cols = grad_vals.contiguous(), vals.contiguous(), R.colidx.contiguous()
     out = torch.empty((T, E), dtype=x.dtype, device=x.device)
     _abi.ws_topk_route_backward(x.data_ptr(), T, E, ld, dt, k, normalize, cols.data_ptr(), vals.data_ptr(),
-                                g.data_ptr(), out.data_ptr(), E, _raw_stream(x.device.index))
+                                g.data_ptr(), out.data_ptr(), E, _queue_of(x.device.index))
     return out
 
 
@@ -170,7 +178,7 @@ class Routing:
         self.R, self.nnz, self.device = R, nnz, rowptr.device
         self._arrays, self._vals = (rowptr, colidx), vals  # whose addresses the calls get
         self._index = self.device.index
-        self._stream = raw = _raw_stream(self._index)
+        self._stream = raw = _queue_of(self._index)
         if validate:
             _abi.ws_csr_destroy(R._handle(True, raw))
         scratch = _scratch(T, E, self._index)
@@ -217,7 +225,7 @@ class Routing:
 
     def _queue(self) -> int:
         """The current stream, for a call; the plan's arrays stay allocated until it is done with them."""
-        raw = _raw_stream(self._index)
+        raw = _queue_of(self._index)
         if raw != self._stream:
             s = torch.cuda.current_stream(self.device)
             for u in (self._buf, *self._arrays, self._vals):
@@ -393,7 +401,7 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     call = _abi.ADAPTERS_CALL.pack(T, L, nnz, rowptr.data_ptr(), colidx.data_ptr(), vals.data_ptr(), K, r, N,
                                    x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), ldb, apartB,
                                    0 if base is None else base.data_ptr(), ldbase, out.data_ptr(), ldy, dt)
-    _abi.ws_adapters(call, scratch.data_ptr(), need, _raw_stream(index))
+    _abi.ws_adapters(call, scratch.data_ptr(), need, _queue_of(index))
     if wait:
         torch.cuda.current_stream(dev).synchronize()
         if T * rank > 8192 and N > 0 and scratch[:4].view(torch.int32).item():
