@@ -412,7 +412,8 @@ typedef struct ws_routing {
 /*
  * ws_routing_build -- fills offsets, rows, entries and slots: the entries of R
  * sorted by column, rows in order within a column.  `scratch` holds
- * ws_routing_scratch(nrows, ncols) bytes, 16-byte aligned (0 for few rows: NULL then).
+ * ws_routing_scratch(nrows, ncols) bytes, 16-byte aligned (0 for few rows: NULL
+ * then; -1 if the device cannot be asked, with the reason in ws_last_error).
  */
 int64_t ws_routing_scratch(int64_t nrows, int64_t ncols);
 ws_status_t ws_routing_build(const ws_routing* r, void* scratch, int64_t scratch_bytes, ws_stream_t stream);

@@ -249,7 +249,10 @@ def ws_topk_route_backward(logits: int, rows: int, cols: int, ld: int, dtype: in
 
 
 def ws_routing_scratch(nrows: int, ncols: int) -> int:
-    return load().ws_routing_scratch(nrows, ncols)
+    size = load().ws_routing_scratch(nrows, ncols)
+    if size < 0:
+        _check("ws_routing_scratch", 7)  # WS_ERR_CUDA
+    return size
 
 
 def ws_routing_build(r, scratch: int, scratch_bytes: int, stream: int) -> None:

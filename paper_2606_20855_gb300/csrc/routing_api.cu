@@ -183,7 +183,8 @@ ws_status_t ws_topk_route_backward(const void* logits, int64_t rows, int64_t col
 
 int64_t ws_routing_scratch(int64_t nrows, int64_t ncols) {
   int sms = 0;
-  if (nrows < 0 || ncols < 0 || sm_count(&sms) != WS_OK) return 0;
+  if (nrows < 0 || ncols < 0) return 0;
+  if (sm_count(&sms) != WS_OK) return -1;
   const int64_t chunks = routing_chunks(nrows, ncols, sms);
   return chunks == 1 ? 0 : chunks * ((ncols + 3) & ~int64_t{3}) * static_cast<int64_t>(sizeof(int32_t));
 }
