@@ -466,9 +466,8 @@ ws_status_t ws_routing_matmul_backward(const ws_routing* r, const void* gys, int
  * 32 bits, for many tokens kept, times the value, as pairs of 16-bit values
  * (bfloat16: 16 significant bits; half: off by 2^-23 of them and at most 2^-25 of
  * the largest of 32 ranks of the token, over the range of floats), the result is
- * summed in 32 bits and rounded once.  "Many tokens": nrows times r, rounded up
- * to a multiple of 16, is above 8192.  base may be NULL (zero) and may be y itself;
- * y may overlap no other input.
+ * summed in 32 bits and rounded once.  "Many tokens": ws_adapters_many(nrows, r)
+ * is not 0.  base may be NULL (zero) and may be y itself; y may overlap no other input.
  * `scratch` holds ws_adapters_scratch(nnz, r) bytes, 16-byte aligned, and for
  * many tokens 16 bytes more for every 8 values, or part of them, of the rows of
  * each of x, A and B whose address or strides are not multiples of 16 bytes.  For
@@ -495,6 +494,7 @@ typedef struct ws_adapters_call {
 } ws_adapters_call;
 
 int64_t ws_adapters_scratch(int64_t nnz, int64_t r);
+int ws_adapters_many(int64_t nrows, int64_t r);
 ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scratch_bytes, ws_stream_t stream);
 
 #ifdef __cplusplus

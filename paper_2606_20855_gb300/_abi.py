@@ -65,6 +65,7 @@ SIGNATURES = [
     ("ws_routing_matmul_backward", _i32, [_p, _p, _i64, _p, _i64, _p, _i64, _i64, _i64, _i64, _p, _i64, _p, _i64, _i64,
                                           _i32, _p, _i64, _p]),
     ("ws_adapters_scratch", _i64, [_i64, _i64]),
+    ("ws_adapters_many", _i32, [_i64, _i64]),
     ("ws_adapters", _i32, [ctypes.c_char_p, _p, _i64, _p]),
 ]
 
@@ -308,6 +309,10 @@ def ws_routing_matmul_backward(r, gys: int, ldgys: int, xs: int, ldxs: int, W: i
 
 def ws_adapters_scratch(nnz: int, r: int) -> int:
     return load().ws_adapters_scratch(nnz, r)
+
+
+def ws_adapters_many(nrows: int, r: int) -> bool:
+    return bool(load().ws_adapters_many(nrows, r))
 
 
 def ws_adapters(call: bytes, scratch: int, scratch_bytes: int, stream: int) -> None:

@@ -302,6 +302,8 @@ int64_t ws_adapters_scratch(int64_t nnz, int64_t r) {
   return 16 + (nnz <= 0 || r <= 0 ? 0 : nnz * adapters_rank(r) * 4 * static_cast<int64_t>(sizeof(float)));
 }
 
+int ws_adapters_many(int64_t nrows, int64_t r) { return nrows >= 0 && r >= 0 && !adapters_step(nrows, r); }
+
 ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scratch_bytes, ws_stream_t stream) {
   if (!call) return routing_fail(WS_ERR_INVALID_ARG, "NULL arguments");
   const ws_adapters_call& c = *call;

@@ -149,6 +149,16 @@ def _scratch(nrows: int, ncols: int, device: int) -> int:
     return _abi.ws_routing_scratch(nrows, ncols)
 
 
+@functools.lru_cache(maxsize=1024)
+def _adapters_scratch(nnz: int, r: int) -> int:
+    return _abi.ws_adapters_scratch(nnz, r)
+
+
+@functools.lru_cache(maxsize=1024)
+def _adapters_many(nrows: int, r: int) -> bool:
+    return _abi.ws_adapters_many(nrows, r)
+
+
 class Routing:
     """A routing matrix with its transpose: the entries of R sorted by column, rows in order within a column.
 
@@ -373,9 +383,8 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     x, ldx, _, need = _operand(x)
     A, lda, apart, more = _operand(A)
     B, ldb, apartB, most = _operand(B)
-    # ws_adapters_scratch, and copies for many tokens
-    rank = (r + 15) // 16 * 16
-    need = 16 + nnz * rank * 16 + (need + more + most if T * rank > 8192 else 0)
+    many = _adapters_many(T, r)
+    need = _adapters_scratch(nnz, r) + (need + more + most if many else 0)
     ldbase = ldy = N
     if base is not None:
         if base.dtype != dtype or base.get_device() != index:
@@ -404,7 +413,7 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     _abi.ws_adapters(call, scratch.data_ptr(), need, _queue_of(index))
     if wait:
         torch.cuda.current_stream(dev).synchronize()
-        if T * rank > 8192 and N > 0 and scratch[:4].view(torch.int32).item():
+        if many and N > 0 and scratch[:4].view(torch.int32).item():
             raise _abi.WsError("adapters", 8, "a kernel gave up a wait")
     return out
 
