@@ -18,8 +18,6 @@ def __getattr__(name):
     if name not in __all__:
         raise AttributeError(name)
     import importlib
-    here = globals()
-    for module, names in (("spgemm", [n for n in __all__ if n not in _ROUTING]), ("routing", _ROUTING)):
-        m = importlib.import_module(f"{__name__}.{module}")
-        here.update({n: getattr(m, n) for n in names})  # the function spgemm over the submodule of that name
-    return here[name]
+    m = importlib.import_module(f"{__name__}.{'routing' if name in _ROUTING else 'spgemm'}")
+    globals()[name] = found = m if name == "spgemm" else getattr(m, name)  # that module, called, is its function of the same name
+    return found

@@ -11,6 +11,8 @@ computed entirely by libws_spgemm.so through the four ABI calls:
 """
 from __future__ import annotations
 
+import sys
+import types
 from dataclasses import dataclass
 
 import numpy as np
@@ -318,3 +320,14 @@ def spgemm(A: DeviceCSR, B: DeviceCSR, validate: bool = False, stream=None) -> D
         C = op.numeric(stream=stream)
         op.wait(stream)
     return C
+
+
+class _CallableModule(types.ModuleType):
+    """This module, which the package's name ``spgemm`` means however it is imported: a call of it is one of the function
+    ``spgemm``."""
+
+    def __call__(self, *args, **kwargs):
+        return spgemm(*args, **kwargs)
+
+
+sys.modules[__name__].__class__ = _CallableModule
