@@ -443,7 +443,10 @@ __global__ void __launch_bounds__(kExpandThreads, 2)
       }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       if (!__syncthreads_and(mine || !there)) mixed = true;
-      if (dead) break;
+      if (dead) {  // this turn's copy may be in flight; it is not among those that are waited for on the way out
+        if (threadIdx.x == 0) bar_wait_short(smem_u32(&b_bar), done & 1);
+        break;
+      }
       if (threadIdx.x == 0 && bar_wait(smem_u32(&b_bar), done & 1, &dead)) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         const uint64_t da = smem_desc(sa, false), db = smem_desc64(sb);
