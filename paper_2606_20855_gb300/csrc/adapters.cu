@@ -274,10 +274,11 @@ __global__ void __launch_bounds__(kShrinkThreads, 1)
     if (items < kList || dead) break;
   }
   if (dead) {  // no copy and no product may be in flight when the CTA leaves
-    if (warp == 0 && lane == 0)
+    // by the lanes that copied and multiplied
+    if (warp == 0 && elect_one())
       for (int f = max(0, filled - kShrinkStages); f < filled; ++f)
         bar_wait_short(smem_u32(&full_bar[f % kShrinkStages]), static_cast<uint32_t>(f / kShrinkStages) & 1);
-    if (warp == 1 && lane == 0) {
+    if (warp == 1 && elect_one()) {
       mma_commit(smem_u32(&last_bar));
       bar_wait_short(smem_u32(&last_bar), 0);
       atomicOr(status, 1);

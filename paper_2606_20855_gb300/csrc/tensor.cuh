@@ -13,8 +13,8 @@ namespace wsk {
 
 constexpr unsigned long long kWaitLimitNs = 2000000000ull;
 
-// One lane of a warp, all of whose lanes are here: the compiler then knows that a single thread runs what follows, and does not
-// wrap each copy and matrix instruction in a loop over lanes.
+// One lane of a warp, all of whose lanes are here, the same one at every call: the compiler then knows that a single thread runs
+// what follows, and does not wrap each copy and matrix instruction in a loop over lanes.
 __device__ __forceinline__ bool elect_one() {
   uint32_t on;
   asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(on));
