@@ -44,22 +44,23 @@ class Layer:
 
     def forward(self, x):
         w = self.weights()
-        logits = Routing(one_expert(x.shape[0])).matmul(x, w["router"][None])
+        every = Routing(one_expert(x.shape[0]))
+        logits = every.matmul(x, w["router"][None])
         R = topk_route(logits, K)
         plan = Routing(R)
         xs = plan.dispatch(x)
         up = plan.matmul(xs, w["up"])
         act = torch.relu(up)
         ys = plan.matmul(act, w["down"])
-        return plan.combine(ys), (w, logits, R, plan, x, xs, up, act, ys)
+        return plan.combine(ys), (w, logits, R, plan, x, xs, up, act, ys, every)
 
     def backward(self, grad_y, kept):
-        w, logits, R, plan, x, xs, up, act, ys = kept
+        w, logits, R, plan, x, xs, up, act, ys, every = kept
         grad_ys, grad_vals = plan.combine_backward(grad_y, ys)
         grad_act, grad_down = plan.matmul_backward(grad_ys, act, w["down"])
         grad_xs, grad_up = plan.matmul_backward(grad_act * (up > 0), xs, w["up"])
         grad_logits = topk_route_backward(logits, R, grad_vals)
-        grad_x, grad_router = Routing(one_expert(x.shape[0])).matmul_backward(grad_logits, x, w["router"][None])
+        grad_x, grad_router = every.matmul_backward(grad_logits, x, w["router"][None])
         return grad_x + plan.dispatch_backward(grad_xs), {"router": grad_router[0], "up": grad_up, "down": grad_down}
 
 
@@ -72,8 +73,12 @@ def train(layer: Layer, steps: int) -> list[float]:
     for _ in range(steps):
         y, kept = layer.forward(x)
         off = y.float() - goal
-        losses.append(float(off.square().mean()))
         _, grads = layer.backward((off * (2 / off.numel())).to(torch.bfloat16), kept)
+        # read back together: the loss, and whether a product's kernel gave up a wait (its result would be incomplete)
+        loss, gave_up = torch.stack([off.square().mean(), (kept[3].status | kept[-1].status).float()[0]]).tolist()
+        if gave_up:
+            raise RuntimeError("a product's kernel gave up a wait")
+        losses.append(loss)
         for name, grad in grads.items():
             layer.master[name] -= 20.0 * grad.float()
     return losses
@@ -89,9 +94,12 @@ def serve(layer: Layer, requests: int = 5, rank: int = 16) -> float:
     B = (torch.randn((requests, H, rank), generator=g, device="cuda") * rank ** -0.5).to(torch.bfloat16)
     S = DeviceCSR(requests, requests, torch.arange(requests + 1, device="cuda"),
                   torch.arange(requests, dtype=torch.int32, device="cuda"), torch.full((requests,), 0.5, device="cuda"))
-    y, (w, logits, R, *_) = layer.forward(x)
-    base = Routing(one_expert(requests)).matmul(y, proj)
-    out = adapters(y, A, B, S, base, out=base)
+    y, (w, logits, R, *rest) = layer.forward(x)
+    shared = Routing(one_expert(requests))
+    base = shared.matmul(y, proj)
+    out = adapters(y, A, B, S, base, out=base, wait=True)
+    for plan in (rest[0], rest[-1], shared):
+        plan.wait()
 
     cols, vals = R.colidx.view(-1, K).long(), R.vals.view(-1, K)
     want = torch.zeros((requests, H), device="cuda")

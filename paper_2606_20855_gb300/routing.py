@@ -38,7 +38,7 @@ def _queue_of(index: int) -> int:
 def _elsewhere(f, stream, *args, **kwargs):
     """f on ``stream``: results are allocated and work is queued there; inputs that came from another stream stay
     allocated until it is done with them."""
-    for t in args:
+    for t in (*args, *kwargs.values()):
         for u in (t.rowptr, t.colidx, t.vals) if isinstance(t, DeviceCSR) else (t,):
             if isinstance(u, torch.Tensor):
                 u.record_stream(stream)
@@ -168,6 +168,10 @@ class Routing:
     take no part; the slots they leave over come last, hold -1 and stand for zero rows.
     The plan is that of R's shape, row pointer and columns when it is built, and keeps those arrays.  ``combine`` and its
     gradient read R's values as they are at the call, of the tensor that ``R.vals`` is then.
+
+    The products' kernels wait for one another with a limit of two seconds.  One that gives up a wait leaves its result
+    incomplete and says so only in ``status`` (int32 [1], nonzero then, cleared when the plan is built): read it where
+    results are read, or call ``wait``, which waits for the stream and raises.
     """
 
     def __init__(self, R: DeviceCSR, validate: bool = False, stream=None):
@@ -221,6 +225,10 @@ class Routing:
     @property
     def slots(self) -> torch.Tensor:
         return self._part(2 * self._lead + 2 * self.nnz, self.nnz)
+
+    @property
+    def status(self) -> torch.Tensor:
+        return self._part(2 * (self._ncols + 1), 1)
 
     def _rows_of(self, t: torch.Tensor, rows: int, name: str):
         """(t, its row stride, the length of its rows, their type), t being `rows` rows on the plan's device."""
@@ -349,21 +357,26 @@ class Routing:
             return _elsewhere(self.wait, stream)
         self._queue()
         torch.cuda.current_stream(self.device).synchronize()
-        if int(self._buf[2 * (self._ncols + 1)]):
+        if int(self.status):
             raise _abi.WsError("Routing.wait", 8, "a product's kernel gave up a wait")
 
 
 def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, base: torch.Tensor | None = None,
-             out: torch.Tensor | None = None, stream=None, wait: bool = False) -> torch.Tensor:
+             out: torch.Tensor | None = None, stream=None, wait: bool = False,
+             status: torch.Tensor | None = None) -> torch.Tensor:
     """y[t] = base[t] + sum over row t of S of value * B[a] (A[a] x[t]): low-rank adapters of many requests beside the
     projection they share (``base``, its result; None for zero).
 
     x: T x K, A: L x r x K, B: L x N x r, base: T x N, bfloat16 or float16; S: T x L in CSR, float32 values, rows empty
     for tokens without an adapter.  ``out`` may be ``base``: the adapters' part is then added in place; it may overlap no
-    other input.  ``wait``: waits for the result and raises if a kernel gave up a wait.
+    other input.
+
+    The kernels for many tokens wait for one another with a limit of two seconds.  One that gives up a wait leaves y
+    incomplete.  ``status`` (int32, one value, of the caller's) is then made nonzero, and left as it is otherwise, so that one
+    serves many calls; ``wait`` waits for the result and raises.
     """
     if stream is not None:
-        return _elsewhere(adapters, stream, x, A, B, S, base, out, wait=wait)
+        return _elsewhere(adapters, stream, x, A, B, S, base, out, wait=wait, status=status)
     dt, dtype, dev, index = _dtype(x, "x"), x.dtype, x.device, x.get_device()
     (La, r, K), (L, N, rb) = A.shape, B.shape
     if La != L or r != rb:
@@ -383,7 +396,9 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
     x, ldx, _, need = _operand(x)
     A, lda, apart, more = _operand(A)
     B, ldb, apartB, most = _operand(B)
-    many = _adapters_many(T, r)
+    if status is not None and (status.dtype != torch.int32 or status.numel() != 1 or status.get_device() != index):
+        raise TypeError("status must be one int32 value on x's device")
+    many = _adapters_many(T, r) and N > 0
     need = _adapters_scratch(nnz, r) + (need + more + most if many else 0)
     ldbase = ldy = N
     if base is not None:
@@ -411,9 +426,11 @@ def adapters(x: torch.Tensor, A: torch.Tensor, B: torch.Tensor, S: DeviceCSR, ba
                                    x.data_ptr(), ldx, A.data_ptr(), lda, apart, B.data_ptr(), ldb, apartB,
                                    0 if base is None else base.data_ptr(), ldbase, out.data_ptr(), ldy, dt)
     _abi.ws_adapters(call, scratch.data_ptr(), need, _queue_of(index))
+    if many and status is not None:
+        status.bitwise_or_(scratch[:4].view(torch.int32).view(status.shape))
     if wait:
         torch.cuda.current_stream(dev).synchronize()
-        if many and N > 0 and scratch[:4].view(torch.int32).item():
+        if many and scratch[:4].view(torch.int32).item():
             raise _abi.WsError("adapters", 8, "a kernel gave up a wait")
     return out
 
