@@ -133,14 +133,16 @@ __device__ __forceinline__ void clear_words(uint32_t* p, int words) {
   }
 }
 
-// total[e] (shared; at most one a row) becomes the first slot of column e; returns the number of placed entries.
-__device__ __forceinline__ int scan_columns(const ws_routing& r, int cols, int* total, int64_t* scratch) {
-  int64_t sum = 0;
+// total[e] (shared; at most one a row) becomes the first slot of column e; returns the number of placed entries.  V holds rows times
+// columns: what is marked may be more than the entries are.
+template <typename V>
+__device__ __forceinline__ int scan_columns(const ws_routing& r, int cols, int* total, V* scratch) {
+  V sum = 0;
   for (int e0 = 0; e0 < cols; e0 += blockDim.x) {
     const int e = e0 + threadIdx.x;
-    const int64_t n = e < cols ? total[e] : 0;
-    int64_t all = 0;
-    const int64_t before = block_exclusive_scan(n, scratch, &all);
+    const V n = e < cols ? total[e] : 0;
+    V all = 0;
+    const V before = block_exclusive_scan(n, scratch, &all);
     if (e < cols) total[e] = slots_before(r, sum, before);
     sum += all;
   }
@@ -194,7 +196,7 @@ static_assert(build_smem(kRouteMaxCols, kSmallWarps) <= kMostSmall);
 __global__ void __launch_bounds__(32 * kSmallWarps) routing_small_kernel(ws_routing r, int cols, bool stage) {
   const int warps = blockDim.x >> 5;
   extern __shared__ __align__(16) int sm[];
-  __shared__ int64_t scratch[32];
+  __shared__ int scratch[32];
   may_start_next();
   uint32_t* mask = reinterpret_cast<uint32_t*>(sm);
   int* first = sm + warps * cols;
