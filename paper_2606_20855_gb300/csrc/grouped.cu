@@ -34,6 +34,7 @@ constexpr int kTileM = 128;   // rows of the M side: lanes of tensor memory
 constexpr int kTileK = 64;    // 128 bytes: the swizzle's span
 constexpr int kBytesA = kTileM * kTileK * 2;
 constexpr int kTurnBytes = 32 * 128;
+constexpr double kFewRows = 4;     // mean rows an expert up to which W's features fill the lanes, or warps read W by themselves
 constexpr double kPairRows = 512;  // rows an expert from which on its row tiles go in pairs
 
 // Where the rows of the experts are in the product D (M x N tile).
@@ -698,14 +699,23 @@ cudaError_t launch_rows(const GroupedRows& g, int num_sms, cudaStream_t s, bool*
     return launch<BN, kRows, kWMN, kPair>(kRows == kRowsM ? x : w, kRows == kRowsM ? w : x, out, p, tiles, num_sms, s);
   };
   using std::integral_constant;
-  // Few rows an expert: W's features fill the 128 lanes and the rows are the short side.
-  // Forward: pieces of 16 rows and 32 features also where they all are at work at once (24 rows of three experts, K = 1520, N =
+  // Few rows an expert: W's features fill the 128 lanes and the rows are the short side.  us of the product and of the rows' gradient in
+  // pieces of eight (product) or tiles of 16 rows | in tiles of 64, rows at random: 64 experts, K = 2048, N = 1024, mean 0.4 10.6, 10.5 |
+  // 16.0, 14.7, mean 1 31.1, 30.7 | 34.6, 30.5, mean 4 43.0, 44.2 | 45.8, 42.8, mean 8 48.7, 44.3 | 46.6, 43.5, mean 12 59, 46 | 47, 44;
+  // eight experts, N = 8192, mean 3 33.9, 35.0 | 41.8, 32.9, mean 8 48.1, 42.6 | 46.0, 41.2; 128 experts, K = 1024, N = 2048, mean 0.2
+  // 12.2, 16.9 | 18.7, 20.2, mean 2 75.4, 71.4 | 71.3, 69.6, mean 12 142, 86 | 84, 82.
+  // Forward: pieces of eight rows and 32 features also where they all are at work at once (24 rows of three experts, K = 1520, N =
   // 304: 14 us in tiles of 128 features, 8 us so).
+  // The mean is over all columns: how many rows each has is known on the device only, so demand on few of many experts takes the
+  // kernel of few rows.
   if constexpr (kWMN) {
-    if (mean <= 12) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>(), std::false_type());
+    if (mean <= kFewRows) return run(integral_constant<int, 16>(), integral_constant<int, kRowsN>(), std::false_type());
   } else {
-    if (mean <= 12 || (g.r->nnz / kThinRows + met) * up(features, kThinFeatures) <= 2 * num_sms) return launch_thin(g, s);
+    if (mean <= kFewRows || (g.r->nnz / kThinRows + met) * up(features, kThinFeatures) <= 2 * num_sms) return launch_thin(g, s);
   }
+  // Tiles of 64 rows | of 128, the rows on the lanes: 64 experts as above, mean 24 48, 45 | 49, 48, mean 48 49.5, 46.5 | 49.9, 49.2, mean
+  // 64 50.2, 47.3 | 49.9, 48.5, mean 96 59, 61 | 52, 51; 16 experts, K = 4096, N = 2048, mean 24 45.4, 45.8 | 48.7, 44.9, mean 48 46.6,
+  // 46.8 | 49.2, 45.9, mean 96 62, 56 | 50, 46.
   if (mean <= 48) return run(integral_constant<int, 64>(), integral_constant<int, kRowsN>(), std::false_type());
   // Pairs of row tiles where experts have enough of them that the odd one left over costs less than pairs gain.  2048 -> 4096, TFLOP/s
   // in pairs | one by one: 256 rows an expert 1060 | 1073, 512 1327 | 1277, 1024 1490 | 1364, 4096 1692 | 1536; with gradients 256
