@@ -323,10 +323,11 @@ __device__ __noinline__ float added(const ws_adapters_call& c, const float* h, i
 
 // 256 values of 128 tokens: base arrives while the products run; the sums go through the same piece of shared memory to y.  Two
 // CTAs share an SM, so that one's latencies (row pointer, column, h and B, product, store) pass under the other's
-// work.  8192 tokens, 2048 halves: 17 us without adapters (base to y, 67 MB; 10 us at the copy rate), 20 us with rank 16, 24 us with
-// rank 32; on the warp-level instruction 31 us, with a CTA that keeps v h for two columns 34 us, with a thread for each token's
+// work.  8192 tokens of 12 requests, 2048 values: 14 us without adapters (base to y, 67 MB; 10 us at the copy rate), 24 us
+// (bfloat16) and 25.6 us (half, whose power of two is sought) with rank 16, 25.7 and 27.4 us with rank 32.  In half, before that power:
+// 24 us with rank 32; on the warp-level instruction 31 us, with a CTA that keeps v h for two columns 34 us, with a thread for each token's
 // v h 25-28 us (its loads touch 32 rows at a time).  128 columns a CTA: inner products and sums take 51.7 us with three CTAs an SM and
-// 60.2 with four, where this takes 44.4, because each CTA goes through h again.
+// 60.2 with four, where this took 44.4, because each CTA goes through h again.
 template <bool half>
 __global__ void __launch_bounds__(kExpandThreads, 2)
     expand_tile_kernel(const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_base,

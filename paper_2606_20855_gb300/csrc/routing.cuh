@@ -191,9 +191,11 @@ ws_status_t launch_grouped_weights(const GroupedRows& g, const void* gys, int64_
 // Ranks kept for an entry of S: h is padded with zeros.
 inline int adapters_rank(int64_t r) { return static_cast<int>((r + 15) / 16 * 16); }
 // Whether tokens go one by one.  That reads A and B for every token (from L2), 2 rank (K + N) bytes each; a tile of 128 tokens
-// reads x once for every few adapters it meets.  K = N = 4096, bfloat16, us one by one | as tiles of one adapter | as tiles in
-// which every token has another adapter: 512 tokens of rank 16 31 | 22 | 225, 256 of rank 64 about 100 | 31 | 659, 1024 of rank
-// 16 about 58 | 22 | 225.  Rank 0 (base alone) goes by tokens as rank 16 does: one by one is a launch with a row of CTAs a token, of
+// reads x once for every few adapters it meets.  K = N = 4096, bfloat16, us of the kernels where all tokens share an adapter, where
+// each has its own, one by one | in tiles: 512 tokens of rank 16 26, 37 | 16.5, 411, 256 of rank 32 31, 40 | 16.5, 554, 128 of
+// rank 64 47, 57 | 21, 993, 1024 of rank 16 48, 70 | 17.5, 458, 256 of rank 64 84, 100 | 21, 1025.  How many adapters the tokens
+// have is known on the device only: above the limit many tokens that each have their own take six to ten times as long as they
+// would one by one, below it tokens that share one take up to 2.3 times as long as in tiles.  Rank 0 (base alone) goes by tokens as rank 16 does: one by one is a launch with a row of CTAs a token, of
 // which there may be 65535.
 inline bool adapters_step(int64_t nrows, int64_t r) { return nrows * (r > 0 ? adapters_rank(r) : 16) <= 8192; }
 // scratch: a status word (16 bytes), then up to four parts of h.
