@@ -153,3 +153,19 @@ def test_infinite_sums_keep_their_sign(T, r, dt):
     rest = torch.ones(T, dtype=torch.bool, device="cuda")
     rest[5], rest[8] = False, False
     assert bool(torch.isfinite(y[rest]).all())
+
+
+@pytest.mark.parametrize("dt", TYPES)
+@pytest.mark.parametrize("r", [1, 15, 16, 40])
+@pytest.mark.parametrize("T", [9, 700])
+def test_infinite_sums_keep_their_sign_where_all_share_an_adapter(T, r, dt):
+    """The same in tiles whose tokens have one adapter, none of which is computed by itself."""
+    from paper_2606_20855_gb300 import adapters
+    K, N = 72, 50
+    x, A, B = _randn((T, K), dt, 1), _randn((1, r, K), dt, 2).abs() + 0.5, _randn((1, N, r), dt, 3).abs() + 0.5
+    x[5, 3], x[8, 70] = float("inf"), -float("inf")
+    y = adapters(x, A, B, _csr(torch.ones((T, 1), dtype=torch.bool, device="cuda"), torch.ones((T, 1), device="cuda")), None)
+    assert bool((y[5] == float("inf")).all()) and bool((y[8] == -float("inf")).all())
+    rest = torch.ones(T, dtype=torch.bool, device="cuda")
+    rest[5], rest[8] = False, False
+    assert bool(torch.isfinite(y[rest]).all())
