@@ -463,7 +463,8 @@ ws_status_t ws_routing_matmul_backward(const ws_routing* r, const void* gys, int
  *   gated    h[s]  = act(gate) * up,         gate = Wg[e] xs[s] + bg[e],  up = Wu[e] xs[s] + bu[e]   Wg[e], Wu[e]: F x K
  * bfloat16 or half, biases (one row an expert) and residual (rows in slot order) in the same type.  bias, bg, bu, residual may be NULL
  * (none).  z, or gate and up, receive the sums rounded to that type, for the backward calls; NULL: not wanted.
- * act: silu = z / (1 + exp(-z)), gelu = z (1 + erf(z / sqrt 2)) / 2, gelu_tanh its form with tanh, the derivative of relu at 0 is 0.
+ * act: WS_ACT_NONE is z itself, a gated block's gate too; silu = z / (1 + exp(-z)), gelu = z (1 + erf(z / sqrt 2)) / 2, gelu_tanh its form
+ * with tanh, the derivative of relu at 0 is 0.
  * At infinities values and derivatives are the limits.
  * Backward, from gys or gh and the kept sums:
  *   linear   gz = gys act'(z);  gxs[s] = W[e]^T gz[s],  gW[e] = sum of gz[s] xs[s]^T,  gbias[e] = sum of gz[s]   (residual: gys)

@@ -25,7 +25,6 @@ constexpr int kAtOnce = 2;  // rows that a warp has in flight
 struct SlopeParams {
   const int64_t* offsets;
   int groups;
-  int64_t nnz;
   int width, padded;          // columns; those of a row of `out` (16-byte rows; behind the width zeros)
   const uint16_t *g, *z, *up;
   int64_t ldg, ldz, ldup;
@@ -84,6 +83,7 @@ __global__ void __launch_bounds__(kSlopeThreads, kBoth && kSums ? 3 : 0) slope_k
   }
   may_start_next();
   with_act(p.act, [&](auto act) {
+  constexpr bool kSame = !kBoth && decltype(act)::value == WS_ACT_NONE;  // the sums' gradient is the result's
   for (int64_t tile = blockIdx.y; tile < tiles; tile += gridDim.y) {
     int64_t row0 = tile * p.tile, rows = placed - row0;
     if constexpr (kSums) {
@@ -106,7 +106,7 @@ __global__ void __launch_bounds__(kSlopeThreads, kBoth && kSums ? 3 : 0) slope_k
         for (int j = 0; j < kAtOnce; ++j) {
           const int64_t row = row0 + min(static_cast<int64_t>(r0 + j * kWarps), rows - 1);
           wg[j] = load8(p.g + row * p.ldg, col, p.width, p.vecg);
-          if constexpr (decltype(act)::value != WS_ACT_NONE) wz[j] = load8(p.z + row * p.ldz, col, p.width, p.vecz);
+          if constexpr (!kSame) wz[j] = load8(p.z + row * p.ldz, col, p.width, p.vecz);
           if constexpr (kBoth) wu[j] = load8(p.up + row * p.ldup, col, p.width, p.vecup);
         }
 #pragma unroll
@@ -116,7 +116,7 @@ __global__ void __launch_bounds__(kSlopeThreads, kBoth && kSums ? 3 : 0) slope_k
           [[maybe_unused]] float g[8], z[8], up[8], dz[8], du[8];
           unpack8<half>(wg[j], g);
           if constexpr (kBoth) unpack8<half>(wu[j], up);
-          if constexpr (decltype(act)::value == WS_ACT_NONE) {  // the sums' gradient is the result's
+          if constexpr (kSame) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) dz[i] = g[i];
           } else {
@@ -241,21 +241,21 @@ ws_status_t launch_two_products(const GroupedRows& g, const void* second, int64_
 }
 
 ws_status_t launch_slopes(const SlopeRows& r, int num_sms, cudaStream_t s) {
+  const int64_t nnz = r.r->nnz;
   SlopeParams p{};
   p.offsets = r.r->offsets;
   p.groups = static_cast<int>(r.r->ncols);
-  p.nnz = r.r->nnz;
   p.width = static_cast<int>(r.width);
   p.padded = static_cast<int>(r.padded);
-  p.g = static_cast<const uint16_t*>(r.g), p.ldg = r.ldg, p.vecg = rows16(r.g, r.ldg, p.nnz);
-  p.z = static_cast<const uint16_t*>(r.z), p.ldz = r.ldz, p.vecz = rows16(r.z, r.ldz, p.nnz);
-  p.up = static_cast<const uint16_t*>(r.up), p.ldup = r.ldup, p.vecup = rows16(r.up, r.ldup, p.nnz);
+  p.g = static_cast<const uint16_t*>(r.g), p.ldg = r.ldg, p.vecg = rows16(r.g, r.ldg, nnz);
+  p.z = static_cast<const uint16_t*>(r.z), p.ldz = r.ldz, p.vecz = rows16(r.z, r.ldz, nnz);
+  p.up = static_cast<const uint16_t*>(r.up), p.ldup = r.ldup, p.vecup = rows16(r.up, r.ldup, nnz);
   p.out = static_cast<uint16_t*>(r.out);
   p.sums = r.sums;
   p.act = r.z ? r.act : WS_ACT_NONE;
   const bool both = r.up != nullptr, sums = r.sums != nullptr;
-  p.tile = slope_rows(p.nnz, p.padded, sums);
-  const int64_t tiles = sums ? slope_tiles(p.nnz, p.groups, p.padded) : up(p.nnz, p.tile);
+  p.tile = slope_rows(nnz, p.padded, sums);
+  const int64_t tiles = sums ? slope_tiles(nnz, p.groups, p.padded) : up(nnz, p.tile);
   cudaError_t e = both ? (sums ? launch_slope<true, true>(p, r.half, tiles, num_sms, s) : launch_slope<true, false>(p, r.half, tiles, num_sms, s))
                        : (sums ? launch_slope<false, true>(p, r.half, tiles, num_sms, s) : launch_slope<false, false>(p, r.half, tiles, num_sms, s));
   if (e == cudaSuccess && sums) {
