@@ -6,8 +6,11 @@
 // Phi, the normal distribution, by the rational approximation 7.1.26 of Abramowitz and Stegun's Handbook of Mathematical
 // Functions, off by 7.5e-8: q = 1 - Phi(|z|) = exp(-z^2 / 2) t (a1 + t (a2 + ...)) / 2 with t = 1 / (1 + p |z| / sqrt 2), so that gelu is
 // max(z, 0) - |z| q and its derivative 1/2 + sign(z) (1/2 - q + |z| phi(z)).  2^x and 1 / x are the approximate instructions (off by
-// 2^-22), as results are rounded to 16 bits.  Below -80 values are those at -80, above 80 derivatives those at 80 (equal to
-// 32 bits but for silu and gelu of values that no 16-bit type tells from 0): the limits, not inf * 0, at infinities.  NaN stays NaN.
+// 2^-22), as results are rounded to 16 bits.  Infinities have the limits, not inf * 0: what an exponential is multiplied by stops at kActEdge.
+// 1 + exp(-v) is held times kScale, so that its reciprocal is normal where v is down to -92; below -93 the reciprocal is 0.  So bfloat16,
+// which has the exponents of 32 bits, gets the values down to its smallest normal number, and 0 or what lies between below that; of the
+// derivatives, sums of such factors times up to 250, what is below 2^-124 may be 0, and of the logistic function's above 82 what is below 2^-119.
+// NaN stays NaN, but relu's derivative is 0 there.
 #pragma once
 
 #include "pairs.cuh"
@@ -15,10 +18,11 @@
 
 namespace wsk {
 
-constexpr float kActEdge = 80.0f;
+constexpr float kActEdge = 93.0f;       // 2^127 < exp(93) kScale < 2^128: finite, with a reciprocal below 2^-126, which is 0
+constexpr float kScale = 0.0078125f;    // 2^-7
 constexpr float kLog2E = 1.4426950408889634f;
 
-// For |z| up to 80: -q / (e t), e = exp(-z^2 / 2) and t.
+// For |z| up to kActEdge: -q / (e t), e = exp(-z^2 / 2) and t.
 __device__ __forceinline__ Two normal_tail(Two a, Two* e, Two* t) {
   *t = inverse(fma2(a, two(0.23164190f), two(1.0f)));  // 0.3275911 / sqrt 2
   *e = two_to(mul2(mul2(a, a), two(-0.5f * kLog2E)));
@@ -27,17 +31,17 @@ __device__ __forceinline__ Two normal_tail(Two a, Two* e, Two* t) {
   q = fma2(*t, q, two(0.142248368f));
   return fma2(*t, q, two(-0.127414796f));
 }
-// exp(-v): of z, or of gelu_tanh's 2 w, at least -80 and, where above is false, not above 80.
+// exp(-v) kScale, v being z or gelu_tanh's 2 w: z at least -kActEdge, v too, and not above kActEdge where `above` is false.
 template <int kAct>
 __device__ __forceinline__ Two falling(Two z, bool above) {
   if constexpr (kAct == WS_ACT_GELU_TANH) {
-    const Two v = mul2(z, fma2(mul2(z, z), two(-1.5957691216057308f * 0.044715f * kLog2E), two(-1.5957691216057308f * kLog2E)));
-    return two_to(each(v, [&](float x) {
-      x = at_most(x, kActEdge * kLog2E);
-      return above ? x : at_least(x, -kActEdge * kLog2E);
+    const Two x = fma2(z, fma2(mul2(z, z), two(-1.5957691216057308f * 0.044715f * kLog2E), two(-1.5957691216057308f * kLog2E)), two(-7.0f));
+    return two_to(each(x, [&](float y) {
+      y = at_most(y, kActEdge * kLog2E - 7.0f);
+      return above ? y : at_least(y, -kActEdge * kLog2E - 7.0f);
     }));
   }
-  return two_to(mul2(z, two(-kLog2E)));
+  return two_to(fma2(z, two(-kLog2E), two(-7.0f)));
 }
 
 // f(z) of two values, in their place.
@@ -56,7 +60,7 @@ __device__ __forceinline__ void act_values(float* a, float* b) {
     return;
   }
   const Two low = two(at_least(*a, -kActEdge), at_least(*b, -kActEdge));
-  const Two s = inverse(add2(falling<kAct>(low, true), two(1.0f)));
+  const Two s = mul2(inverse(add2(falling<kAct>(low, true), two(kScale))), two(kScale));
   split(kAct == WS_ACT_SIGMOID ? s : mul2(low, s), a, b);
 }
 template <int kAct>
@@ -85,7 +89,7 @@ __device__ __forceinline__ void act_slopes(float* a, float* b, float* va, float*
   } else {
     const Two low = two(at_least(*a, -kActEdge), at_least(*b, -kActEdge));
     const Two x = each(low, [](float z) { return at_most(z, kActEdge); });
-    const Two e = falling<kAct>(x, false), s = inverse(add2(e, two(1.0f))), slope = mul2(s, mul2(e, s));
+    const Two e = falling<kAct>(x, false), q = inverse(add2(e, two(kScale))), s = mul2(q, two(kScale)), slope = mul2(s, mul2(e, q));
     if constexpr (kAct == WS_ACT_SIGMOID) {
       split(s, va, vb);
       split(slope, a, b);
