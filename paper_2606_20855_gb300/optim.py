@@ -11,6 +11,7 @@ import ctypes
 import struct
 
 import torch
+from torch.autograd.graph import increment_version
 
 from . import _abi
 from .routing import _ROW_DTYPES, _queue_of, _span
@@ -32,6 +33,9 @@ class AdamW:
     then, as roots below 2^-63 count as 0.
     state: that of another optimizer, used and updated as it is, not copied: the dict that ``state`` is.  Its entries are lists of
     a tensor for every parameter, "m" and "v", or "m", "r", "m_scale" and "r_scale", and "step", int64 [1], steps done.
+
+    A step counts as an operation in place on the parameters and copies that it updates: a backward pass that needs their old values is an
+    error, as with any operation of torch (but not where a captured step is replayed).
 
     No two steps of one optimizer, or of two that share tensors, may run at the same time.
     """
@@ -101,6 +105,7 @@ class AdamW:
         self._at_table, self._at_step, self._at_done = ctypes.addressof(self._table), state["step"].data_ptr(), self._done.data_ptr()
         self._pointers, self._pack = (ctypes.c_void_p * count)(), struct.Struct(f"={count}Q")
         self._at_pointers = ctypes.addressof(self._pointers)
+        self._written = [t for t in (*params, *copies) if t is not None]  # what a backward pass may need as it was
 
     def _one(self, t: torch.Tensor | None, dtype, name: str) -> int:
         if t is None:
@@ -128,7 +133,7 @@ class AdamW:
         if not any([g is None for g in grads]) and [g.numel() for g in grads] == self._sizes and \
                 all([g.is_contiguous() for g in grads]):  # the usual: all of them, as they are
             kinds, places = {g.dtype for g in grads}, {g.get_device() for g in grads}
-            at = [g.data_ptr() for g in grads]
+            at, written = [g.data_ptr() for g in grads], self._written
         else:
             held = [g if g is None or g.is_contiguous() else g.contiguous() for g in grads]
             kinds, places = {g.dtype for g in held if g is not None}, {g.get_device() for g in held if g is not None}
@@ -136,6 +141,7 @@ class AdamW:
             for i, (g, n) in enumerate(zip(held, self._sizes)):
                 if g is not None and g.numel() != n:
                     raise ValueError(f"gradient {i} must have the parameter's {n} values, got {tuple(g.shape)}")
+            written = [t for g, p, c in zip(grads, self.params, self.copies) if g is not None for t in (p, c) if t is not None]
         if len(kinds) > 1 or not kinds <= _ROW_DTYPES.keys():
             raise TypeError(f"gradients must be float32, bfloat16 or float16, all the same, got {kinds}")
         if places - {self._index}:
@@ -149,6 +155,7 @@ class AdamW:
                                     self._one(scale, torch.float32, "scale"), self._one(skip, torch.int32, "skip"), lr, *self.betas,
                                     self.eps, self.seed, self.bits, _ROW_DTYPES[kind] if kind is not None else _abi.WS_F32, self._copy_type)
         _abi.ws_adamw(call, raw)
+        increment_version(written)  # 1 us of the host for ten tensors
 
     def _record(self, raw: int) -> None:
         """The tensors stay allocated until the current stream, a new one, is done with them."""
