@@ -2,17 +2,15 @@
 // multiply-adds of sm_100 and later take a pair in one instruction (gelu: 10 a value, 30 with erff one by one).
 //
 // sigmoid(z) = 1 / (1 + exp(-z)), silu = z sigmoid(z), gelu = z Phi(z), gelu_tanh = z sigmoid(2 w) for w = sqrt(2 / pi) (z + 0.044715 z^3).
-// Phi, the normal distribution, by the part above |z|: q = 1 - Phi(|z|) = exp(-z^2 / 2) t (c1 + t (c2 + ... + t c6)) with t = 1 / (1 + p |z|), the
-// form of 7.1.26 in Abramowitz and Stegun's Handbook of Mathematical Functions with a term more.  Coefficients are fitted (least largest
-// error by linear programming over |z| up to 13.5) to be off by 1.0e-7, and beyond |z| = 2.7, where that is more, by 3.1e-5 of q: with
-// those of 7.1.26 gelu is 0.36% off at -6 and 1% at -8.  gelu is max(z, 0) - |z| q; its derivative is r = q - |z| phi(z) below 0 and
-// 1 - r above, so that nothing cancels in the tail.  2^x and 1 / x are the approximate instructions (off by 2^-22), as results are rounded
-// to 16 bits.
-// Infinities have the limits, not inf * 0: what an exponential is multiplied by stops at kActEdge.  1 + exp(-v) is held times kScale, so that its
-// reciprocal is normal where v is down to -92; below -93 the reciprocal is 0.  So bfloat16, which has the exponents of 32 bits, gets the
-// values down to its smallest normal number, and 0 or what lies between below that; of the derivatives, sums of such factors times up to 250,
-// what is below 2^-124 may be 0 (gelu: 2^-122), and of the logistic function's above 82 what is below 2^-119.  NaN stays NaN, but relu's
-// derivative is 0 there.
+// Phi, the normal distribution, by the part above |z|: q = 1 - Phi(|z|) = exp(-z^2 / 2) t (c1 + t (c2 + ... + t c6)) with t = 1 / (a + b |z|), the
+// form of 7.1.26 in Abramowitz and Stegun's Handbook of Mathematical Functions with a term more, scaled so that -c6 is 1 (a pair of registers
+// for one constant more spilled: 40,000 rows, 64 -> 4096, silu 124 -> 143 us).  Coefficients are fitted (least largest error by linear
+// programming over |z| up to 13.5) to be off by 1.0e-7, and beyond |z| = 2.7, where that is more, by 3.1e-5 of q: with those of 7.1.26
+// gelu is 0.36% off at -6 and 1% at -8.  gelu is max(z, 0) - |z| q; its derivative is r = q - |z| phi(z) below 0 and 1 - r above, so
+// that nothing cancels in the tail.  2^x and 1 / x are the approximate instructions (off by 2^-22), as results are rounded to 16 bits.
+// Infinities have the limits, not inf * 0: what an exponential is multiplied by stops at kActEdge, from where on its reciprocal is 0.  Factors
+// below 2^-126 are 0, where bfloat16 has the exponents of 32 bits: values below 2^-119 (silu is z times such a factor) and derivatives
+// below 2^-118 may be 0.  NaN stays NaN, but relu's derivative is 0 there.
 #pragma once
 
 #include "pairs.cuh"
@@ -20,31 +18,30 @@
 
 namespace wsk {
 
-constexpr float kActEdge = 93.0f;       // 2^127 < exp(93) kScale < 2^128: finite, with a reciprocal below 2^-126, which is 0
-constexpr float kScale = 0.0078125f;    // 2^-7
+constexpr float kActEdge = 88.4f;  // exp(88.4) is between 2^127 and 2^128: finite, its reciprocal below 2^-126
 constexpr float kLog2E = 1.4426950408889634f;
 
 // For |z| up to kActEdge: -q / (e t), e = exp(-z^2 / 2) and t.
 __device__ __forceinline__ Two normal_tail(Two a, Two* e, Two* t) {
-  *t = inverse(fma2(a, two(0.2943481f), two(1.0f)));
+  *t = inverse(fma2(a, two(0.444193947f), two(1.509077f)));
   *e = two_to(mul2(mul2(a, a), two(-0.5f * kLog2E)));
-  Two q = fma2(*t, two(0.084670398f), two(-0.256180699f));
-  q = fma2(*t, q, two(0.059818978f));
-  q = fma2(*t, q, two(-0.163315557f));
-  q = fma2(*t, q, two(-0.106777966f));
-  return fma2(*t, q, two(-0.118215053f));
+  Two q = add2(*t, two(-2.00494935f));
+  q = fma2(*t, q, two(0.310230568f));
+  q = fma2(*t, q, two(-0.561256981f));
+  q = fma2(*t, q, two(-0.243166892f));
+  return fma2(*t, q, two(-0.178395617f));
 }
-// exp(-v) kScale, v being z or gelu_tanh's 2 w: z at least -kActEdge, v too, and not above kActEdge where `above` is false.
+// exp(-v), v being z or gelu_tanh's 2 w: z at least -kActEdge, v too, and not above kActEdge where `above` is false.
 template <int kAct>
 __device__ __forceinline__ Two falling(Two z, bool above) {
   if constexpr (kAct == WS_ACT_GELU_TANH) {
-    const Two x = fma2(z, fma2(mul2(z, z), two(-1.5957691216057308f * 0.044715f * kLog2E), two(-1.5957691216057308f * kLog2E)), two(-7.0f));
-    return two_to(each(x, [&](float y) {
-      y = at_most(y, kActEdge * kLog2E - 7.0f);
-      return above ? y : at_least(y, -kActEdge * kLog2E - 7.0f);
+    const Two v = mul2(z, fma2(mul2(z, z), two(-1.5957691216057308f * 0.044715f * kLog2E), two(-1.5957691216057308f * kLog2E)));
+    return two_to(each(v, [&](float x) {
+      x = at_most(x, kActEdge * kLog2E);
+      return above ? x : at_least(x, -kActEdge * kLog2E);
     }));
   }
-  return two_to(fma2(z, two(-kLog2E), two(-7.0f)));
+  return two_to(mul2(z, two(-kLog2E)));
 }
 
 // f(z) of two values, in their place.
@@ -63,7 +60,7 @@ __device__ __forceinline__ void act_values(float* a, float* b) {
     return;
   }
   const Two low = two(at_least(*a, -kActEdge), at_least(*b, -kActEdge));
-  const Two s = mul2(inverse(add2(falling<kAct>(low, true), two(kScale))), two(kScale));
+  const Two s = inverse(add2(falling<kAct>(low, true), two(1.0f)));
   split(kAct == WS_ACT_SIGMOID ? s : mul2(low, s), a, b);
 }
 template <int kAct>
@@ -92,7 +89,7 @@ __device__ __forceinline__ void act_slopes(float* a, float* b, float* va, float*
   } else {
     const Two low = two(at_least(*a, -kActEdge), at_least(*b, -kActEdge));
     const Two x = each(low, [](float z) { return at_most(z, kActEdge); });
-    const Two e = falling<kAct>(x, false), q = inverse(add2(e, two(kScale))), s = mul2(q, two(kScale)), slope = mul2(s, mul2(e, q));
+    const Two e = falling<kAct>(x, false), s = inverse(add2(e, two(1.0f))), slope = mul2(s, mul2(e, s));
     if constexpr (kAct == WS_ACT_SIGMOID) {
       split(s, va, vb);
       split(slope, a, b);
