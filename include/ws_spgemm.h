@@ -465,7 +465,7 @@ ws_status_t ws_routing_matmul_backward(const ws_routing* r, const void* gys, int
  * (none).  z, or gate and up, receive the sums rounded to that type, for the backward calls; NULL: not wanted.
  * act: WS_ACT_NONE is z itself, a gated block's gate too; silu = z / (1 + exp(-z)), gelu = z (1 + erf(z / sqrt 2)) / 2, gelu_tanh its form
  * with tanh, the derivative of relu at 0 is 0.
- * At infinities values and derivatives are the limits.
+ * At infinities values and derivatives are the limits; values below 2^-119 and derivatives below 2^-118 may be 0.
  * Backward, from gys or gh and the kept sums:
  *   linear   gz = gys act'(z);  gxs[s] = W[e]^T gz[s],  gW[e] = sum of gz[s] xs[s]^T,  gbias[e] = sum of gz[s]   (residual: gys)
  *   gated    dg = gh up act'(gate), du = gh act(gate);  gxs[s] = Wg[e]^T dg[s] + Wu[e]^T du[s],  gWg, gWu, gbg, gbu likewise
@@ -634,8 +634,9 @@ ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scr
  * probability, by a hash of seed, step, the tensor's index and the value's: equal inputs give equal bits.  A root above zero (2^-63 and
  * above) has no code of zero; smaller ones count as 0, so that eps has to be at least 1e-15.  Infinities and NaN become NaN and stay with
  * their value.
- * step: int64[1] on the device, steps done: the call adds one.  done: int32[1] on the device, 0 between calls.  lr_at, scale, skip: one value on the device, read when the
- * step runs (NULL: lr, 1, 0); where *skip is not 0 nothing changes, steps done neither.  Tensors may overlap neither one another nor the gradients.
+ * step: int64[1] on the device, steps done, one count for all tensors, whether they had a gradient in every step or not: the call adds one.
+ * done: int32[1] on the device, 0 between calls.  lr_at, scale, skip: one value on the device, read when the step runs (NULL: lr, 1, 0);
+ * where *skip is not 0 nothing changes, steps done neither.  Tensors may overlap neither one another nor the gradients.
  * tensors and grads are read before the call returns.  Calls with the same tensors or step array must not overlap on the GPU.
  */
 typedef struct ws_adamw_tensor {

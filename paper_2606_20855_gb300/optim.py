@@ -20,7 +20,9 @@ BLOCK = 256  # values that share a scale where states have 8 bits
 
 
 class AdamW:
-    """AdamW over ``params``, contiguous float32 tensors on one device.  For every value, t being the number of the step:
+    """AdamW over ``params``, contiguous float32 tensors on one device.  For every value, t being the number of the step, one count for all
+    tensors (also for one that has had no gradient until now: its first change is then up to (1 - b1) / sqrt(1 - b2) lr, 3.2 lr with
+    the default betas, where a count of its own would make it lr; a gradient of zeros counts as one):
 
         m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
         p = p (1 - lr weight_decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
