@@ -11,10 +11,13 @@ import ctypes
 import struct
 
 import torch
-from torch.autograd.graph import increment_version
 
 from . import _abi
 from .routing import _ROW_DTYPES, _queue_of, _span
+
+# of every gradient in turn: to call the methods themselves takes the host less
+_numel, _contiguous, _place, _address = torch.Tensor.numel, torch.Tensor.is_contiguous, torch.Tensor.get_device, torch.Tensor.data_ptr
+_written_to = torch._C._increment_version  # of a list of tensors, as torch.autograd.graph.increment_version
 
 BLOCK = 256  # values that share a scale where states have 8 bits
 
@@ -109,9 +112,7 @@ class AdamW:
         self._at_pointers = ctypes.addressof(self._pointers)
         self._written = [t for t in (*params, *copies) if t is not None]  # what a backward pass may need as it was
 
-    def _one(self, t: torch.Tensor | None, dtype, name: str) -> int:
-        if t is None:
-            return 0
+    def _one(self, t: torch.Tensor, dtype, name: str) -> int:
         if t.dtype != dtype or t.numel() != 1 or t.get_device() != self._index:
             raise TypeError(f"{name} must be one {dtype} value on the parameters' device")
         return t.data_ptr()
@@ -132,10 +133,13 @@ class AdamW:
         if raw not in self._seen:
             self._record(raw)
         held = None  # copies, until the launch has been queued
-        if not any([g is None for g in grads]) and [g.numel() for g in grads] == self._sizes and \
-                all([g.is_contiguous() for g in grads]):  # the usual: all of them, as they are
-            kinds, places = {g.dtype for g in grads}, {g.get_device() for g in grads}
-            at, written = [g.data_ptr() for g in grads], self._written
+        try:  # the usual: all of them, as they are
+            usual = [*map(_numel, grads)] == self._sizes and all(map(_contiguous, grads))
+        except TypeError:  # None among them
+            usual = False
+        if usual:
+            kinds, places = {g.dtype for g in grads}, set(map(_place, grads))
+            at, written = [*map(_address, grads)], self._written
         else:
             held = [g if g is None or g.is_contiguous() else g.contiguous() for g in grads]
             kinds, places = {g.dtype for g in held if g is not None}, {g.get_device() for g in held if g is not None}
@@ -153,11 +157,13 @@ class AdamW:
         lr, at_lr = self.lr, 0
         if isinstance(lr, torch.Tensor):
             lr, at_lr = 0.0, self._one(lr, torch.float32, "lr")
-        call = _abi.ADAMW_CALL.pack(self._at_table, self._at_pointers, len(self._sizes), self._at_step, self._at_done, at_lr,
-                                    self._one(scale, torch.float32, "scale"), self._one(skip, torch.int32, "skip"), lr, *self.betas,
-                                    self.eps, self.seed, self.bits, _ROW_DTYPES[kind] if kind is not None else _abi.WS_F32, self._copy_type)
+        at_scale = 0 if scale is None else self._one(scale, torch.float32, "scale")
+        at_skip = 0 if skip is None else self._one(skip, torch.int32, "skip")
+        call = _abi.ADAMW_CALL.pack(self._at_table, self._at_pointers, len(at), self._at_step, self._at_done, at_lr, at_scale, at_skip, lr,
+                                    *self.betas, self.eps, self.seed, self.bits, _ROW_DTYPES[kind] if kind is not None else _abi.WS_F32,
+                                    self._copy_type)
         _abi.ws_adamw(call, raw)
-        increment_version(written)  # 1 us of the host for ten tensors
+        _written_to(written)
 
     def _record(self, raw: int) -> None:
         """The tensors stay allocated until the current stream, a new one, is done with them."""
