@@ -9,8 +9,8 @@
 //
 // One persistent CTA per SM: one warp's lane fetches operand tiles with TMA
 // (128-byte swizzle, a ring of stages), one lane issues the matrix
-// instructions, four warps store finished tiles while the next one is
-// multiplied (two accumulators).  How many rows an expert has is known on the
+// instructions, four warps, or with an epilogue eight or twelve, finish and
+// store tiles while the next one is multiplied (two accumulators).  How many rows an expert has is known on the
 // device only, so every CTA counts the tiles of all experts itself and takes
 // every gridDim-th one.  Operands are read as they lie in memory: an operand
 // whose contraction index runs along its rows (W in `rows`, both in `weights`)
@@ -108,10 +108,12 @@ struct Tile {
 constexpr int kListed = 32;
 
 // A warp that copies, one that multiplies, four that store; where rows are summed over, one that clears.  Where a result is finished before it is
-// stored that takes longer than the products (32,768 rows of 32 experts, 1024 -> 2048, bias, gelu, sums kept: the products alone 97 us): twelve
-// warps take 127 us, eight 139.  Sixteen need the room of a sixth stage, without which the products alone take 10% longer.  Gated blocks, twelve | eight:
-// 44,272 rows of nine experts, 64 -> 1152, silu 51 | 61, gelu with kept sums 82 | 97; 8198 of eight, 512 -> 4096 55 | 57, 77 | 88; 32,768 of 32,
-// 1024 -> 2048, silu, sums kept 197 | 192, gelu 199 | 206; 2048 -> 4096, sums kept 185 | 183.
+// stored that takes longer than the products, and is bound by no unit but by each warp's chain of loads, sums and stores, which more warps
+// hide (32,768 rows of 32 experts, 1024 -> 2048, bias, gelu, sums kept, 125 us: tensor cores 55% of the cycles, issue slots 36%, DRAM 41%; the
+// products alone 93): twelve warps 127 us, eight 139, when both were measured.  Sixteen need the room of a sixth stage, without which the
+// products alone take 10% longer.  Gated blocks, twelve | eight: 44,272 rows of nine experts, 64 -> 1152, silu 51 | 61, gelu with kept sums
+// 82 | 97; 8198 of eight, 512 -> 4096 55 | 57, 77 | 88, 2048 -> 4096, sums kept 185 | 183; 32,768 of 32, 1024 -> 2048, silu, sums kept
+// 197 | 192 (the one that loses more than noise), gelu 199 | 206.
 template <int BN, int kRows, bool kPair, int kEpi>
 constexpr int kStorers = kRows != kRowsM || kEpi == kPlain ? 4 : kPair || BN <= 128 ? 12 : 8;
 template <int BN, int kRows, bool kPair, int kEpi>
@@ -325,10 +327,11 @@ __device__ __forceinline__ void add_row(float (&f)[32], const uint4 (&w)[4], boo
 }
 
 // A lane's row of 32 columns, 32 bytes at a time (the address is a multiple of that): of what an epilogue stores no piece of shared memory is
-// waited for, and no fence waits.  us, so | by the copy engine: 15,190 rows of 14 experts, 48 -> 3792, gated, sums kept 117 | 143 (with eight
-// warps; 96 with twelve), linear, gelu, sums kept 88 | 104; 32,768 rows of 32 experts, 1024 -> 2048, linear, gelu, sums kept 133 | 137.  By the engine where there is a
-// residual, whose loads such stores hold up (32,768 rows as above 128 | 121, 40,000 of eight, 64 -> 4096, 199 | 189), and where products of
-// pairs of gated tiles have more than kDirectSteps stages (8191 rows, 4096 -> 4096, sums kept: 303 | 298; of 16 stages 219 | 217).
+// waited for, and no fence waits.  us, so | by the copy engine, with eight storing warps: 15,190 rows of 14 experts, 48 -> 3792, gated, sums
+// kept 117 | 143 (84 with twelve, so), linear, gelu, sums kept 88 | 104; 32,768 rows of 32 experts, 1024 -> 2048, linear, gelu, sums kept
+// 133 | 137.  By the engine where there is a residual, whose loads such stores hold up (32,768 rows as above 128 | 121, 40,000 of eight,
+// 64 -> 4096, 199 | 189), and where products of pairs of gated tiles have more than kDirectSteps stages (8191 rows, 4096 -> 4096, sums kept:
+// 303 | 298; of 16 stages 219 | 217).
 constexpr int kDirectSteps = 8;
 __device__ __forceinline__ void store_row32(uint16_t* to, const uint32_t (&w)[16]) {
 #pragma unroll
@@ -1041,10 +1044,9 @@ constexpr int kThinThreads = 256;
 constexpr int kThinWarps = kThinThreads / 32;
 constexpr int kFewPieces = 6;
 
-//
 // kGated: 16 features, each in both matrices.  kAny: rows of x and W start at any multiple of 2 bytes and are read as they are, so that W is read
 // once (a copy of it to aligned rows reads and writes it besides: 64 x 2048 x 1001 in both matrices for one row each, 262 MB each,
-// 347 us with copies, 162 without).
+// 347 us with copies, 170 without; rows of 1000, which are aligned, 104).
 template <int kEpi>
 struct ThinExtra {
   const uint16_t* second;
