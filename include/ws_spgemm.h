@@ -627,7 +627,7 @@ ws_status_t ws_adapters(const ws_adapters_call* call, void* scratch, int64_t scr
  *   g = grad * scale;  m' = beta1 m + (1 - beta1) g;  v' = beta2 v + (1 - beta2) g^2;
  *   p' = p (1 - lr decay) - lr / (1 - beta1^t) * m' / (sqrt(v' / (1 - beta2^t)) + eps);  copy = p' rounded to 16 bits.
  * p: float[n], in place.  grads: `count` arrays of grad_dtype (float, bfloat16, half).  copy: copy_dtype (bfloat16 or half), or
- * NULL.  All arithmetic is in 32 bits.
+ * NULL.  All arithmetic is in 32 bits.  eps: 0, or at least 2^-126.
  * bits 32: m, v float[n]; m_scale, v_scale are not read.
  * bits 8: m, v uint8[n], e4m3 codes of m and of r = sqrt(v); m_scale, v_scale float[(n + 255) / 256], the scales of blocks of 256
  * values: the largest magnitude / 448, 0 below 1e-30.  Codes are rounded up with their share of the way to the next one as

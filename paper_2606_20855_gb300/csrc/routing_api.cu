@@ -530,6 +530,8 @@ ws_status_t ws_adamw(const ws_adamw_call* call, ws_stream_t stream) {
   if (!row_type(c.grad_dtype)) return routing_fail(WS_ERR_DTYPE, "gradients are float, bfloat16 or half");
   if (!(c.beta1 >= 0 && c.beta1 < 1 && c.beta2 >= 0 && c.beta2 < 1 && c.eps >= 0))
     return routing_fail(WS_ERR_INVALID_ARG, "beta1 and beta2 must be in [0, 1), eps not negative");
+  if (c.eps > 0 && c.eps < 0x1p-126)  // the kernel's reciprocal takes it for 0, and 0 / eps would be NaN
+    return routing_fail(WS_ERR_INVALID_ARG, "eps must be 0 or at least 2^-126");
   if (c.bits == 8 && c.eps < 1e-15) return routing_fail(WS_ERR_INVALID_ARG, "with states of 8 bits eps must be at least 1e-15");
   const uintptr_t gsize = c.grad_dtype == WS_F32 ? 4 : 2, ssize = c.bits == 32 ? 4 : 1;
   const auto off = [](const void* p, uintptr_t size) { return reinterpret_cast<uintptr_t>(p) % size != 0; };

@@ -31,7 +31,7 @@ class AdamW:
         p = p (1 - lr weight_decay) - lr / (1 - b1^t) m / (sqrt(v / (1 - b2^t)) + eps)
 
     lr: a number, or a float32 tensor of one value on the device (read when a step runs, also in a captured graph); it may be
-    replaced between steps.  weight_decay: a number, or one for every tensor.
+    replaced between steps.  weight_decay: a number, or one for every tensor.  eps: 0, or at least 2^-126.
     copies: bfloat16 or float16 tensors of the parameters' sizes (or None), which get the new values rounded.
     bits: 32, m and v are float32; or 8, m and sqrt(v) are float8_e4m3fn codes with a float32 scale for every 256 values of a
     tensor, rounded stochastically by a hash of seed, step, tensor and place (equal inputs give equal bits); eps is at least 1e-15
@@ -55,6 +55,8 @@ class AdamW:
         beta1, beta2 = (float(b) for b in betas)
         if not (0 <= beta1 < 1 and 0 <= beta2 < 1 and eps >= 0):
             raise ValueError(f"betas must be in [0, 1) and eps not negative, got {betas} and {eps}")
+        if 0 < eps < 2.0 ** -126:
+            raise ValueError(f"eps must be 0 or a normal number of 32 bits, got {eps}")
         if bits == 8 and eps < 1e-15:
             raise ValueError(f"with states of 8 bits eps must be at least 1e-15, got {eps}")
         self.device, self._index = params[0].device, params[0].get_device()
